@@ -68,8 +68,8 @@ const char* sq_last_error(void);
 /*
  * sq_time_next_call -- measurement hook, not part of the method.  Arms two events for
  * the next call of sq_had_quant_act(_ex), sq_pack_w4(_ex), sq_w4a4_linear, sq_w4a8_linear,
- * sq_w4a4_linear_swiglu, sq_qk_had_kvquant(_ex) or sq_attn_decode_kv4(_ex)
- * made by this host thread: start_event takes the start time of the first kernel that
+ * sq_w4a4_linear_swiglu, sq_qk_had_kvquant(_ex), sq_attn_decode_kv4(_ex),
+ * sq_rope_kv_write, sq_kv_read, sq_attn_paged or sq_attn_prompt made by this host thread: start_event takes the start time of the first kernel that
  * call launches and stop_event the end time of its last kernel (hipExtLaunchKernel
  * events), so hipEventElapsedTime(start, stop) is the call's time on the device without
  * marker packets between kernels.
@@ -366,6 +366,152 @@ sq_status sq_attn_decode_kv4_split_noalloc(const void* q_rot, const uint8_t* k_q
                                            const void* k_beta, const uint8_t* v_q, const void* v_alpha,
                                            const void* v_beta, int64_t B, int64_t S, int64_t H, int64_t D,
                                            float scale, int32_t param_bits, void* out, void* stream);
+
+/*
+ * The paged cache.  A serving program's K/V cache is a pool of pages of `page` tokens, handed to
+ * sequences as they grow, with Hkv key/value heads that Hq >= Hkv query heads share (Hq % Hkv == 0;
+ * query head h uses key/value head h / (Hq / Hkv)).  Arguments common to the four calls below:
+ *
+ *   k_q, v_q   device uint8 [pages, Hkv, page, D*bits/8], 16-byte aligned: 4-bit codes packed as
+ *              everywhere, or 8-bit codes
+ *   params     device [pages, Hkv, page, 4], 16-byte (param_bits 16: 8-byte) aligned: k_alpha, k_beta,
+ *              v_alpha, v_beta of each token and head, fp32 or fp16 as in sq_qk_had_kvquant_ex
+ *   pages, page, Hkv   1 <= pages < 2^31; page a power of two, 16 <= page <= 2^20; 1 <= Hkv <= 2^16;
+ *              pages * page * Hkv <= 2^40
+ *   bits, param_bits   4 or 8; 32 or 16 (others: SQ_ERR_UNSUPPORTED)
+ *   block_table device int32 [B, ld_table], 4-byte aligned: entry i < max_blocks of row b is the page
+ *              that holds the positions i*page .. i*page + page - 1 of sequence b
+ *              (1 <= max_blocks <= ld_table).  An entry outside [0, pages), and a position past the
+ *              table, has no page: nothing is written there, it reads as zeros, and attention leaves
+ *              it out.  Pages may be shared by sequences that only read them.
+ *   lens       device int32 [B]: tokens of each sequence in the cache, the ones of this call included
+ *   cu         device int32 [B + 1], ascending: the rows cu[b] .. cu[b+1] - 1 of a packed call belong
+ *              to sequence b and are its LAST ones: row t has position lens[b] - cu[b+1] + t.  A row
+ *              that belongs to no sequence (before cu[0], from cu[B] on), or whose position is
+ *              negative, is left alone: none of its outputs is written.
+ *   D          128 (others: SQ_ERR_UNSUPPORTED)
+ *   ld*        elements from one token's heads to the next one's, >= heads * D and < 2^24, a multiple
+ *              of 8: a tensor may be a slice of a fused projection's output
+ * lens, cu and the table stay on the device, so that a captured graph can be replayed as sequences
+ * grow.  No value in them makes a call read or write outside the tensors.
+ */
+
+/*
+ * sq_rope_frequencies -- host helper: the angle per position of each pair of dims,
+ * f_i = theta^(-2 i / rotary_dim), i < rotary_dim / 2, in out_host[rotary_dim / 2] (HOST memory).
+ *   rotary_dim 16 .. 128, a multiple of 16
+ *   theta      base, finite and > 0 (a longer base is given here directly)
+ *   scaling    0: none; 1: positions interpolated, f_i / factor; 2: by parts: with r = original_len
+ *              f_i / (2 pi) turns within the original context, f_i is kept where r >= high, divided
+ *              by factor where r <= low, and between the two mixed linearly in r
+ *   factor     >= 1, finite (scaling 1, 2);  low < high, original_len > 0, finite (scaling 2)
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED (other scalings).
+ */
+sq_status sq_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double low, double high,
+                              double original_len, double* out_host);
+
+/*
+ * sq_rope_kv_write -- rotary positions and R3 (Sec. 3.1) on the queries and keys of new tokens, per
+ * head, and the quantized write of their keys and values into the pages (eq. 1, one group per
+ * token and head):
+ *     (u, w) -> (u c - w s, w c + u s),  c = magnitude cos(p f_i),  s = magnitude sin(p f_i)
+ * for the pair i of the first rotary_dim dims at position p, then y = x S_128 / sqrt(128).
+ *   q          device fp16 [T, ldq]: Hq heads of D;  k, v  device fp16 [T, ldk], [T, ldv]: Hkv heads
+ *              of D; 16-byte aligned, BEFORE the rotary positions
+ *   T          >= 0 rows (0 is a no-op), < 2^31;  1 <= Hq <= 2^16
+ *   cu         may be NULL: row t is the one new token of sequence t (T == B)
+ *   freq       device fp64 [rotary_dim / 2], radians per position, 8-byte aligned (sq_rope_frequencies
+ *              gives them); NULL iff rotary_dim == 0 (no positions: R3 and the write alone)
+ *   rotary_dim 0 .. 128, a multiple of 16: the leading dims that turn
+ *   interleaved  0: pair i is (i, i + rotary_dim / 2); 1: (2 i, 2 i + 1)
+ *   magnitude  finite factor of the turned dims (1 unless a long-context scaling asks for another)
+ *   k_clip, v_clip   clipping ratios in (0, 1] as in sq_qk_had_kvquant_ex
+ *   q_rot      device fp16 [T, Hq, D] contiguous, 16-byte aligned
+ *   k_rot      optional device fp16 [T, Hkv, D] contiguous: the turned keys before quantization
+ *              (what a prompt's own attention reads); NULL to skip
+ * Angles, and keys up to their one rounding to fp32, are computed in 64 bits: positions of any size
+ * keep their angle, and the codes are eq. 1's 32-bit steps on that fp32 key.  Two rows of one call
+ * must not meet in one slot (a page in two sequences at a position both write): such a slot holds
+ * bytes of either.
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_ALIGN, SQ_ERR_ALIAS, SQ_ERR_HIP.
+ */
+sq_status sq_rope_kv_write(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                           int64_t T, int64_t Hq, int64_t D, const int32_t* cu, const int32_t* lens, int64_t B,
+                           const int32_t* block_table, int64_t ld_table, int64_t max_blocks,
+                           uint8_t* k_q, uint8_t* v_q, void* params, int64_t pages, int64_t page, int64_t Hkv,
+                           int32_t bits, int32_t param_bits,
+                           const double* freq, int32_t rotary_dim, int32_t interleaved, float magnitude,
+                           float k_clip, float v_clip, void* q_rot, void* k_rot, void* stream);
+
+/*
+ * sq_kv_read -- keys and values of the sequences' last tokens out of the pages: alpha c + beta of
+ * eq. 1, rounded to fp16, in packed rows, as sq_attn_prompt reads them.
+ *   T          >= 0 rows (0 is a no-op), < 2^31
+ *   plain_basis  0: keys as stored, in R3's basis (for rotated queries); 1: turned back
+ *   k, v       device fp16 [T, ldk], [T, ldv]: Hkv heads of D, 16-byte aligned
+ * Errors as sq_rope_kv_write.
+ */
+sq_status sq_kv_read(const int32_t* cu, const int32_t* lens, int64_t B, int64_t T,
+                     const int32_t* block_table, int64_t ld_table, int64_t max_blocks,
+                     const uint8_t* k_q, const uint8_t* v_q, const void* params, int64_t pages, int64_t page, int64_t Hkv,
+                     int64_t D, int32_t bits, int32_t param_bits, int32_t plain_basis,
+                     void* k, int64_t ldk, void* v, int64_t ldv, void* stream);
+
+/*
+ * sq_attn_paged -- attention of one query per sequence and head over its pages, the step that
+ * follows sq_rope_kv_write for generated tokens:
+ *     out[b,h,:] = fp16( sum_t softmax_t(scale * q[b,h,:] . K_t) V_t ),  t < min(lens[b], max_len),
+ * K_t and V_t of key/value head h / (Hq / Hkv).  A sequence without tokens (or without pages) gets
+ * zeros.  No parameter alpha of the cache may be negative (the library writes none).
+ *   q          device fp16 [B, ldq]: Hq heads of D, 16-byte aligned (q_rot of the write)
+ *   B          >= 0 (0 is a no-op), B * Hq < 2^24
+ *   max_len    1 <= max_len < 2^30, at least the longest length: it fixes the split of the sequence and
+ *              with it the workspace and the order of additions
+ *   scale      finite score scale, e.g. 1/sqrt(128)
+ *   out        device fp16 [B, ldo]: Hq heads of D, 16-byte aligned
+ *   workspace  device memory, 16-byte aligned, at least the bytes sq_attn_paged_workspace gives (NULL
+ *              allowed when that is 0); scratch, must not overlap any argument; calls that share
+ *              one must be ordered
+ * The result does not depend on the run.  Errors as sq_rope_kv_write; SQ_ERR_SHAPE for a workspace
+ * too small.
+ */
+sq_status sq_attn_paged(const void* q, int64_t ldq, const int32_t* lens, int64_t B,
+                        const int32_t* block_table, int64_t ld_table, int64_t max_blocks,
+                        const uint8_t* k_q, const uint8_t* v_q, const void* params, int64_t pages, int64_t page, int64_t Hkv,
+                        int64_t Hq, int64_t D, int32_t bits, int32_t param_bits, int64_t max_len, float scale,
+                        void* out, int64_t ldo, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of sq_attn_paged's workspace on the CURRENT device.  Errors: SQ_ERR_NULL, SQ_ERR_SHAPE,
+ * SQ_ERR_UNSUPPORTED, SQ_ERR_HIP. */
+sq_status sq_attn_paged_workspace(int64_t B, int64_t max_len, int64_t Hq, int64_t Hkv, int64_t D, uint64_t* bytes);
+
+/*
+ * sq_attn_prompt -- attention of packed sequences in fp16 on the matrix cores: the rows
+ * cu_q[b] .. cu_q[b+1] - 1 of q over the rows cu_k[b] .. cu_k[b+1] - 1 of k and v.  With n queries
+ * and m keys, query i (from 0) sees the keys t < m (causal 0) or t <= m - n + i (causal 1): the
+ * queries are the last n tokens, so a chunk of a prompt comes with the keys of what went before.
+ * A query that sees no key gets zeros.  Values and keys that a query does not see have no part in
+ * its result, NaN and infinities among them.
+ *   q          device fp16 [Tq, ldq]: Hq heads of D;  k, v  device fp16 [Tk, ldk], [Tk, ldv]: Hkv heads
+ *              of D; 16-byte aligned
+ *   cu_q, cu_k device int32 [B + 1], ascending, within [0, Tq] and [0, Tk] (entries beyond are taken as
+ *              the end).  Rows of q outside the sequences are left as they were in out.
+ *   Tq, Tk     >= 0, < 2^31 (Tq == 0 or B == 0 is a no-op; with Tk == 0 k and v may be NULL)
+ *   Hq, Hkv    1 <= Hkv <= Hq <= 2^16, Hq % Hkv == 0; Tq * Hq + 256 * B * Hkv < 2^31
+ *   scale      finite score scale
+ *   out        device fp16 [Tq, ldo]: Hq heads of D, 16-byte aligned
+ *   workspace  as in sq_attn_paged, sized by sq_attn_prompt_workspace (0 where there are rows enough
+ *              to fill the device)
+ * The result does not depend on the run.  Errors as sq_attn_paged.
+ */
+sq_status sq_attn_prompt(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                         const int32_t* cu_q, const int32_t* cu_k, int64_t B, int64_t Tq, int64_t Tk,
+                         int64_t Hq, int64_t Hkv, int64_t D, float scale, int32_t causal, void* out, int64_t ldo,
+                         void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of sq_attn_prompt's workspace on the CURRENT device.  Errors: SQ_ERR_NULL, SQ_ERR_SHAPE,
+ * SQ_ERR_UNSUPPORTED, SQ_ERR_HIP. */
+sq_status sq_attn_prompt_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D, uint64_t* bytes);
 
 #ifdef __cplusplus
 }

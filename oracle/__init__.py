@@ -13,10 +13,11 @@ Modules
   quant     eq. 1 min-max quantizer (asymmetric and symmetric), nibble packing
   linear    the rotated W4A4 linear layer: act quant, weight prep, exact GEMM, epilogue
   kv        R3 on post-RoPE Q/K and 4-bit asymmetric K/V cache quantization
+  paged     rotary positions, the paged cache, attention over it and over packed prompts
 
 Parity status: every function is pinned by the "not gpu" tests (closed forms,
 invariants, brute force, hand-worked fixtures).  Accuracy on real models
 (perplexity, zero-shot) is parity unpinned: it needs model weights and datasets.
 """
 
-from . import hadamard, rotate, quant, linear, kv  # noqa: F401
+from . import hadamard, rotate, quant, linear, kv, paged  # noqa: F401

@@ -1,0 +1,428 @@
+// Decode attention over the paged 4- or 8-bit cache with shared key/value heads: for each
+// sequence b and query head h of the key/value head hk = h / group,
+//     out = softmax_t(scale q . K_t) V,  K_t = ka_t c_t + kb_t (eq. 1), V_t = va_t e_t + vb_t,
+//     q . K_t = ka_t (q . c_t) + kb_t sum(q),
+// over the tokens t < len_b.  q . c and the weighted sum of e run on fp16 MFMA; the codes become
+// fp16 without arithmetic: an integer n < 1024 in the low mantissa bits is the subnormal
+// n 2^-24, which the matrix cores take as it is.  A word of eight 4-bit codes makes four pairs by
+// one shift and four ands, codes 0, 2, 4, 6 as n and 1, 3, 5, 7 in place as 16 n.
+//
+// A workgroup of kWaves waves serves one (sequence, key/value head, up to 16 of its query heads,
+// chunk of tokens); its waves take the chunk's blocks of 64 tokens in turn, each on its own:
+//   scores    S^T = K q^T by 16x16x32 products: lane (i, g) = (lane % 16, lane / 16) brings
+//             bytes 16 g (4 bits) or 32 g (8 bits) .. of a token's key codes straight from
+//             memory (dims 32 g .. 32 g + 31) and ends with the scores of head i for the 16
+//             tokens 16 g .. 16 g + 15 of the block: products j = 0 .. 3 hold the tokens
+//             16 (row / 4) + 4 j + row % 4.
+//   softmax   in base 2.  V's scale goes into the weight, w_t = 2^(s_t + log2 va_t - m), with m
+//             the running maximum of that exponent: the fp16 weights of the second product are
+//             then near 1 at their largest whatever the size of V.  The sums are
+//             l = sum w_t / va_t and b = sum w_t vb_t / va_t in fp32, over unrounded w.  m moves
+//             (and everything is rescaled) only when it would grow by more than kSlack.
+//   values    O^T += V^T w^T: the block's value codes go through LDS as they are (64 or 128
+//             bytes a token) and come back transposed (ds_read_b64_tr_b4 / _b8): lane (i, g)
+//             gets the codes of dim 16 dt + i of its 16 tokens, the order its weights are in.
+// HBM bounds it: a token and key/value head are 144 bytes (4 bits, fp32 parameters), and the
+// arithmetic is a fraction of the time they take to arrive.
+#include "paged_device.h"
+#include "paged_plan.h"
+#include "sq_internal.h"
+
+namespace sq {
+namespace {
+
+constexpr int kWaves = kPagedWaves;
+constexpr int kBlock = kPagedBlock;  // tokens of a wave's step
+constexpr float kSlack = 3.0f;      // log2: weights stay below 2^(kWeightBits + kSlack) < 65504
+constexpr float kWeightBits = 12.0f;
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// 2^(a - b), 0 when a is -inf (an empty state)
+__device__ __forceinline__ float rescale(float a, float b) { return a == -INFINITY ? 0.0f : exp2_fast(__fsub_rn(a, b)); }
+
+// maximum / sum over the four lanes with the same lane % 16
+template <typename Op>
+__device__ __forceinline__ float groups_all(float v, Op op) {
+  const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(s16[0]), __uint_as_float(s16[1]));
+  const auto s32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
+}
+
+__device__ __forceinline__ v8h operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_bit_cast(v8h, v4u{a, b, c, d});
+}
+
+// LDS of a wave: value codes of a block, then four rows of 64 token coefficients (a, b, 1 / va,
+// vb / va with s_t + log2 va_t = a_t (q . c_t) + b_t sum(q) + lv_t, five rows with lv).
+template <int BITS>
+struct WaveLds {
+  static constexpr int ROW = BITS * 16;          // bytes of a token's value codes
+  static constexpr int CODES = kBlock * ROW;
+  static constexpr int BYTES = CODES + 5 * kBlock * 4;
+};
+
+constexpr int kDimRow = 132;  // floats of a head in the merge
+
+template <int BITS>
+constexpr int paged_lds() {
+  const int merge = kWaves * 16 * (kDimRow + 2) * 4, codes = kWaves * WaveLds<BITS>::BYTES;
+  return merge > codes ? merge : codes;
+}
+
+template <int BITS, bool P16>
+__global__ void __launch_bounds__(64 * kWaves)
+attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, uint32_t magic_chunks, uint32_t magic_tiles,
+                uint32_t magic_heads, PagedAttnArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  using W = WaveLds<BITS>;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  // workgroup: key/value head fastest (its chunk's neighbours in a page), then tile of heads,
+  // sequence, chunk: chunks that a short sequence lacks end at the back of the grid
+  uint32_t rest, hk, tile, b, c;
+  div_rem(blockIdx.x, a.cache.heads, magic_heads, rest, hk);
+  div_rem(rest, tiles, magic_tiles, rest, tile);
+  div_rem(rest, chunks, magic_chunks, b, c);
+  const int len = min(max(lens[b], 0), a.max_len);
+  const int first = static_cast<int>(c) * a.chunk_tokens;
+  if (c > 0 && first >= len) return;  // the workgroup leaves together
+  const int last = min(len, first + a.chunk_tokens);
+  const int heads = min(16, a.group - 16 * static_cast<int>(tile));  // of this workgroup
+  const int h0 = static_cast<int>(hk) * a.group + 16 * static_cast<int>(tile);
+
+  // the query of head i (rows past the heads repeat the last one and are not stored), dims
+  // 32 g .. 32 g + 31, in the codes' pair order, and its sum over all dims
+  v8h qf[4];
+  float qsum = 0.0f;
+  {
+    const v4u* qv = reinterpret_cast<const v4u*>(q + b * a.ldq + static_cast<int64_t>(h0 + min(i, heads - 1)) * 128 + 32 * g);
+    v4u raw[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) raw[x] = qv[x];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        qsum += h2f(static_cast<uint16_t>(raw[x][y])) + h2f(static_cast<uint16_t>(raw[x][y] >> 16));
+    qsum = groups_all(qsum, [](float u, float v) { return __fadd_rn(u, v); });
+    if constexpr (BITS == 4) {
+      // word x holds dims 8 x ..: even products take (0, 4), (2, 6), odd ones (1, 5), (3, 7)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const v4u u = raw[2 * e], v = raw[2 * e + 1];
+        qf[2 * e] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x05040100u), __builtin_amdgcn_perm(u[3], u[1], 0x05040100u),
+                            __builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x05040100u));
+        qf[2 * e + 1] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[1], 0x07060302u),
+                                __builtin_amdgcn_perm(v[2], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u));
+      }
+    } else {
+      // a word holds dims 4 x .. 4 x + 3: pairs (0, 2) and (1, 3)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        qf[x] = operand(__builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x05040100u), __builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x07060302u),
+                        __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x05040100u), __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x07060302u));
+    }
+  }
+
+  uint8_t* const vlds = lds + w * W::BYTES;
+  float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
+  const int32_t* const table = a.cache.table + b * a.cache.ldt;
+  const int page = 1 << a.cache.shift;
+  constexpr int KW = BITS == 4 ? 1 : 2;  // 16-byte loads of a lane's key codes
+  // 2^24 undoes the codes' subnormal scale
+  const float cs = a.scale_log2e, cs24 = a.scale_log2e * 16777216.0f;
+
+  v4u kc[4][KW], vc[4][KW];
+  float4 par;
+  bool par_ok;
+  // Page of the block's 16-token group n, -1 past the chunk or the pool (pages hold 16 tokens or
+  // more, so a group lies in one page).
+  auto page_of = [&](int t) -> int32_t {
+    if (t >= last) return -1;
+    const int32_t col = table_column(a.cache, t);
+    return col < 0 ? -1 : valid_page(a.cache, table[col]);
+  };
+  auto load = [&](int t0) {
+    // lane's group for keys: i / 4; for values and parameters: 16-token groups by lane / 16
+    const int32_t mine = page_of(t0 + 16 * g);
+    int32_t pg[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) pg[n] = __builtin_amdgcn_readlane(mine, 16 * n);
+    const int n = i >> 2;
+    const int32_t pk = n == 0 ? pg[0] : n == 1 ? pg[1] : n == 2 ? pg[2] : pg[3];
+    // tokens that are not there read token 0 of page 0 and are masked below
+    const int64_t kslot = pk < 0 ? 0 : token_slot(a.cache, pk, hk, t0 + 16 * n + (i & 3));
+    const uint8_t* kp = a.cache.kq + kslot * W::ROW + (BITS == 4 ? 16 : 32) * g;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 0; x < KW; ++x)
+        kc[j][x] = *reinterpret_cast<const v4u*>(kp + (pk < 0 ? 0 : 4 * j * W::ROW) + 16 * x);
+    // value codes: load n brings group n, four (eight) lanes a token
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int x = 0; x < KW; ++x) {
+        const int row = BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3);
+        const int unit = BITS == 4 ? lane & 3 : lane & 7;
+        const int64_t vslot = pg[m] < 0 ? 0 : token_slot(a.cache, pg[m], hk, t0 + 16 * m + row);
+        vc[m][x] = *reinterpret_cast<const v4u*>(a.cache.vq + vslot * W::ROW + 16 * unit);
+      }
+    // parameters: lane's token is t0 + lane
+    par_ok = mine >= 0 && t0 + lane < last;
+    const int64_t pslot = par_ok ? token_slot(a.cache, mine, hk, t0 + lane) : 0;
+    if constexpr (P16) {
+      const uint2 p = static_cast<const uint2*>(a.cache.params)[pslot];
+      par = make_float4(h2f(static_cast<uint16_t>(p.x)), h2f(static_cast<uint16_t>(p.x >> 16)),
+                        h2f(static_cast<uint16_t>(p.y)), h2f(static_cast<uint16_t>(p.y >> 16)));
+    } else {
+      par = static_cast<const float4*>(a.cache.params)[pslot];
+    }
+  };
+
+  float m = -INFINITY, l = 0.0f, bsum = 0.0f;
+  v4f acc[8];
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt) acc[dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const int step = kWaves * kBlock;
+  int t0 = first + w * kBlock;
+  if (t0 < last) load(t0);
+  for (; t0 < last; t0 += step) {
+    // value codes and coefficients to LDS (this wave's own: no barrier, its LDS operations are
+    // in order); unit u of a row of 4 (8) units lies at u xor (row / 4) % 4 (u xor row % 8)
+#pragma unroll
+    for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+      for (int x = 0; x < KW; ++x) {
+        const int row = 16 * mm + (BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3));
+        const int unit = BITS == 4 ? (lane & 3) ^ ((row >> 2) & 3) : (lane & 7) ^ (row & 7);
+        *reinterpret_cast<v4u*>(vlds + row * W::ROW + 16 * unit) = vc[mm][x];
+      }
+    const float rva = par_ok ? __fdiv_rn(1.0f, par.z) : 0.0f;
+    coef[0 * kBlock + lane] = par_ok ? par.x * cs24 : 0.0f;
+    coef[1 * kBlock + lane] = par_ok ? par.y * cs : 0.0f;
+    coef[2 * kBlock + lane] = par_ok ? __builtin_amdgcn_logf(par.z) : -INFINITY;
+    coef[3 * kBlock + lane] = rva;
+    coef[4 * kBlock + lane] = par_ok ? par.w * rva : 0.0f;
+    v4u kn[4][KW];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 0; x < KW; ++x) kn[j][x] = kc[j][x];
+    if (t0 + step < last) load(t0 + step);
+    asm volatile("" ::: "memory");
+
+    // scores of 16 tokens of head i
+    float s[16];
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 ca = *reinterpret_cast<const float4*>(coef + 0 * kBlock + 16 * g + 4 * j);
+      const float4 cb = *reinterpret_cast<const float4*>(coef + 1 * kBlock + 16 * g + 4 * j);
+      const float4 cl = *reinterpret_cast<const float4*>(coef + 2 * kBlock + 16 * g + 4 * j);
+      const float* fa = &ca.x;
+      const float* fb = &cb.x;
+      const float* fl = &cl.x;
+      v4f se = {0.0f, 0.0f, 0.0f, 0.0f}, so = {0.0f, 0.0f, 0.0f, 0.0f};
+      if constexpr (BITS == 4) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t u = kn[j][0][2 * e], v = kn[j][0][2 * e + 1], u8 = u >> 8, v8 = v >> 8;
+          se = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              operand(u & 0x000F000Fu, u8 & 0x000F000Fu, v & 0x000F000Fu, v8 & 0x000F000Fu), qf[2 * e], se, 0, 0, 0);
+          so = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              operand(u & 0x00F000F0u, u8 & 0x00F000F0u, v & 0x00F000F0u, v8 & 0x00F000F0u), qf[2 * e + 1], so, 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t u = kn[j][x / 2][2 * (x & 1)], v = kn[j][x / 2][2 * (x & 1) + 1];
+          v4f& acc_s = x & 1 ? so : se;
+          acc_s = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              operand(u & 0x00FF00FFu, (u >> 8) & 0x00FF00FFu, v & 0x00FF00FFu, (v >> 8) & 0x00FF00FFu), qf[x], acc_s, 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float dot = BITS == 4 ? __fmaf_rn(so[r], 0.0625f, se[r]) : __fadd_rn(se[r], so[r]);
+        s[4 * j + r] = __fmaf_rn(fa[r], dot, __fmaf_rn(fb[r], qsum, fl[r]));
+        top = fmaxf(top, s[4 * j + r]);
+      }
+    }
+    top = groups_all(top, [](float u, float v) { return fmaxf(u, v); });
+    if (__ballot(top > m + kSlack)) {  // (m = -inf: any token)
+      const float mn = fmaxf(m, top);
+      const float f = rescale(m, mn);
+      l *= f;
+      bsum *= f;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) acc[dt] *= f;
+      m = mn;
+    }
+    const float base = (m == -INFINITY ? 0.0f : m) - kWeightBits;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 cr = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 4 * j);
+      const float4 cv = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 4 * j);
+      const float* fr = &cr.x;
+      const float* fv = &cv.x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = exp2_fast(s[4 * j + r] - base);
+        s[4 * j + r] = p;
+        l = __fmaf_rn(p, fr[r], l);
+        bsum = __fmaf_rn(p, fv[r], bsum);
+      }
+    }
+    // weights in the value codes' pair order, rounded to fp16 (2^-12 of a weight, as the output)
+    v8h pf[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float* p = s + 8 * x;
+      if constexpr (BITS == 4)
+        pf[x] = operand(f2h2(p[0], p[4]), f2h2(p[1] * 0.0625f, p[5] * 0.0625f), f2h2(p[2], p[6]), f2h2(p[3] * 0.0625f, p[7] * 0.0625f));
+      else
+        pf[x] = operand(f2h2(p[0], p[2]), f2h2(p[1], p[3]), f2h2(p[4], p[6]), f2h2(p[5], p[7]));
+    }
+    typedef __attribute__((address_space(3))) v2i* lds_v2i;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      if constexpr (BITS == 4) {
+        const int row = 16 * g + i;
+        const uint8_t* p = vlds + row * W::ROW + 16 * ((dt >> 1) ^ ((row >> 2) & 3)) + 8 * (dt & 1);
+        const v2i c2 = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i)(uintptr_t)(p));
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t u = static_cast<uint32_t>(c2[x]), u8 = u >> 8;
+          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(u & 0x000F000Fu, u & 0x00F000F0u, u8 & 0x000F000Fu, u8 & 0x00F000F0u),
+                                                           pf[x], acc[dt], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int row = 16 * g + 8 * x + (i >> 1);
+          const uint8_t* p = vlds + row * W::ROW + 16 * (dt ^ (row & 7)) + 8 * (i & 1);
+          const v2i c2 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(p));
+          const uint32_t u = static_cast<uint32_t>(c2[0]), v = static_cast<uint32_t>(c2[1]);
+          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              operand(u & 0x00FF00FFu, (u >> 8) & 0x00FF00FFu, v & 0x00FF00FFu, (v >> 8) & 0x00FF00FFu), pf[x], acc[dt], 0, 0, 0);
+        }
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+  const auto add = [](float u, float v) { return __fadd_rn(u, v); };
+  l = groups_all(l, add);
+  bsum = groups_all(bsum, add);
+
+  // the waves' states of each head meet in LDS: dims finished but for the division
+  __syncthreads();
+  float* const red = reinterpret_cast<float*>(lds);                  // [wave][head][kDimRow]
+  float* const red_ml = red + kWaves * 16 * kDimRow;                 // [wave][head][2]
+  if (g == 0) {
+    red_ml[(w * 16 + i) * 2] = m;
+    red_ml[(w * 16 + i) * 2 + 1] = l;
+  }
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt) {
+    v4f o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = __fmaf_rn(acc[dt][r], 16777216.0f, bsum);
+    *reinterpret_cast<v4f*>(red + (w * 16 + i) * kDimRow + 16 * dt + 4 * g) = o;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < heads * 32; x += 64 * kWaves) {
+    const int hh = x >> 5, d = 4 * (x & 31);
+    float M = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) M = fmaxf(M, red_ml[(v * 16 + hh) * 2]);
+    float L = 0.0f;
+    v4f D = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+      const float f = rescale(red_ml[(v * 16 + hh) * 2], M);
+      L = __fmaf_rn(red_ml[(v * 16 + hh) * 2 + 1], f, L);
+      const v4f o = *reinterpret_cast<const v4f*>(red + (v * 16 + hh) * kDimRow + d);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) D[r] = __fmaf_rn(o[r], f, D[r]);
+    }
+    const int64_t head = h0 + hh;
+    if (chunks == 1) {
+      uint16_t* o = a.out + b * a.ldo + head * 128 + d;
+      if (M == -INFINITY)  // no token
+        *reinterpret_cast<v2u*>(o) = v2u{0u, 0u};
+      else
+        *reinterpret_cast<v2u*>(o) = v2u{f2h2(__fdiv_rn(D[0], L), __fdiv_rn(D[1], L)), f2h2(__fdiv_rn(D[2], L), __fdiv_rn(D[3], L))};
+    } else {
+      float* pr = a.part + ((b * static_cast<int64_t>(a.hq) + head) * chunks + c) * kAttnPart;
+      if (d == 0) {
+        pr[0] = M;
+        pr[1] = L;
+      }
+      *reinterpret_cast<v4f*>(pr + 4 + d) = D;
+    }
+  }
+}
+
+// One wave per (sequence, query head): the chunks that its length reaches, in chunk order.
+__global__ void __launch_bounds__(64)
+attn_paged_combine(const float* part, const int32_t* lens, uint16_t* out, int64_t ldo, int hq, int chunks, int chunk_tokens,
+                   int max_len, uint32_t magic_hq) {
+  const int lane = threadIdx.x;
+  uint32_t b, h;
+  div_rem(blockIdx.x, hq, magic_hq, b, h);
+  const int len = min(max(lens[b], 0), max_len);
+  const int n = max(1, (len + chunk_tokens - 1) / chunk_tokens);  // chunk 0 is always written
+  const float* pr = part + (b * static_cast<int64_t>(hq) + h) * chunks * kAttnPart;
+  float M = -INFINITY;
+  for (int c = lane; c < n; c += 64) M = fmaxf(M, pr[static_cast<int64_t>(c) * kAttnPart]);
+  M = wave_max(M);
+  float L = 0.0f, D0 = 0.0f, D1 = 0.0f;
+#pragma unroll 8
+  for (int c = 0; c < n; ++c) {
+    const float* p = pr + static_cast<int64_t>(c) * kAttnPart;
+    const float f = rescale(p[0], M);
+    const float2 d = reinterpret_cast<const float2*>(p + 4)[lane];
+    L = __fmaf_rn(p[1], f, L);
+    D0 = __fmaf_rn(d.x, f, D0);
+    D1 = __fmaf_rn(d.y, f, D1);
+  }
+  reinterpret_cast<uint32_t*>(out + b * ldo + static_cast<int64_t>(h) * 128)[lane] =
+      M == -INFINITY ? 0u : f2h2(__fdiv_rn(D0, L), __fdiv_rn(D1, L));
+}
+
+template <int BITS, bool P16>
+hipError_t launch_part(const PagedAttnArgs& a, hipStream_t stream) {
+  constexpr auto kern = attn_paged_part<BITS, P16>;
+  constexpr int lds = paged_lds<BITS>();
+  const hipError_t init = set_max_lds<kern>(lds);
+  if (init != hipSuccess) return init;
+  const int tiles = (a.group + 15) / 16;
+  const unsigned blocks = static_cast<unsigned>(a.B * a.cache.heads * tiles * a.chunks);
+  return launch(kern, dim3(blocks), dim3(64 * kWaves), lds, stream, a.q, a.lens, a.chunks, tiles,
+                div_magic(static_cast<uint32_t>(a.chunks)), div_magic(static_cast<uint32_t>(tiles)),
+                div_magic(static_cast<uint32_t>(a.cache.heads)), a);
+}
+
+}  // namespace
+
+hipError_t launch_attn_paged(const PagedAttnArgs& a, hipStream_t stream) {
+  hipError_t e;
+  if (a.bits == 8)
+    e = a.param16 ? launch_part<8, true>(a, stream) : launch_part<8, false>(a, stream);
+  else
+    e = a.param16 ? launch_part<4, true>(a, stream) : launch_part<4, false>(a, stream);
+  if (e != hipSuccess || a.chunks == 1) return e;
+  return launch(attn_paged_combine, dim3(static_cast<unsigned>(a.B * a.hq)), dim3(64), 0, stream, a.part, a.lens, a.out, a.ldo,
+                a.hq, a.chunks, a.chunk_tokens, a.max_len, div_magic(static_cast<uint32_t>(a.hq)));
+}
+
+}  // namespace sq

@@ -1,0 +1,72 @@
+// Device helpers shared by the kernels of the paged cache.
+#pragma once
+
+#include "gemm_device.h"
+#include "paged.h"
+#include "sq_device.h"
+
+namespace sq {
+
+// value of the lane whose quad index is this lane's xor M (M = 1 or 2)
+template <int M>
+__device__ __forceinline__ float quad_swap(float v) {
+  constexpr int ctrl = (M == 1) ? 0xB1 : 0x4E;  // quad_perm [1,0,3,2] / [2,3,0,1]
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xF, 0xF, false));
+}
+template <int M>
+__device__ __forceinline__ double quad_swap(double v) {
+  constexpr int ctrl = (M == 1) ? 0xB1 : 0x4E;
+  const int lo = __builtin_amdgcn_mov_dpp(__double2loint(v), ctrl, 0xF, 0xF, false);
+  const int hi = __builtin_amdgcn_mov_dpp(__double2hiint(v), ctrl, 0xF, 0xF, false);
+  return __hiloint2double(hi, lo);
+}
+
+// Unscaled 128-point Sylvester transform of the 128 values of a quad of lanes: register r and
+// lane bits j are the index bits in any order (the transform is the same under a permutation of
+// the bits that input and output share).
+template <typename F>
+__device__ __forceinline__ void quad_fwht(F (&e)[32], int j) {
+#pragma unroll
+  for (int h = 1; h < 32; h <<= 1)
+#pragma unroll
+    for (int r = 0; r < 32; ++r)
+      if ((r & h) == 0) {
+        const F u = e[r], w = e[r + h];
+        e[r] = u + w;
+        e[r + h] = u - w;
+      }
+  const F s1 = (j & 1) ? F(-1) : F(1), s2 = (j & 2) ? F(-1) : F(1);
+#pragma unroll
+  for (int r = 0; r < 32; ++r) e[r] = fma(s1, e[r], quad_swap<1>(e[r]));
+#pragma unroll
+  for (int r = 0; r < 32; ++r) e[r] = fma(s2, e[r], quad_swap<2>(e[r]));
+}
+
+// Sequence of row t of a packed call (cu [B + 1], ascending): its index and the row its rows end
+// before; -1 for a row of none.  The whole wave searches, 64 sequences a step.
+struct RowSeq {
+  int seq;
+  int begin;
+  int end;
+};
+__device__ __forceinline__ RowSeq find_sequence(const int32_t* cu, int64_t B, int64_t t) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t b0 = 0; b0 < B; b0 += 64) {
+    const int64_t b = b0 + lane;
+    int begin = 0, end = 0;
+    if (b < B) {
+      begin = cu[b];
+      end = cu[b + 1];
+    }
+    const uint64_t past = __ballot(b < B && end > t);
+    if (past) {
+      const int first = __builtin_ctzll(past);
+      RowSeq r{static_cast<int>(b0) + first, __builtin_amdgcn_readlane(begin, first), __builtin_amdgcn_readlane(end, first)};
+      if (t < r.begin) r.seq = -1;
+      return r;
+    }
+  }
+  return {-1, 0, 0};
+}
+
+}  // namespace sq

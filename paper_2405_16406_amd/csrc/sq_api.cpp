@@ -7,33 +7,32 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
-#include <string>
 #include <vector>
 
+#include "api_check.h"
 #include "sq_internal.h"
 
 namespace {
 
-thread_local std::string g_last_error;
+thread_local char g_last_error[512];  // fixed: setting it cannot throw
 thread_local sq::LaunchTiming g_timing;
 
-// Disarms sq_time_next_call's events when the entry point returns, on every path.
-struct TimingScope {
-  ~TimingScope() { g_timing = sq::LaunchTiming{}; }
-};
+}  // namespace
+
+namespace sq::api {
+
+TimingScope::~TimingScope() { g_timing = LaunchTiming{}; }
 
 sq_status fail(sq_status s, const char* fmt, ...) {
-  char buf[512];
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
+  vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
   va_end(ap);
-  g_last_error = buf;
   return s;
 }
 
 sq_status ok() {
-  g_last_error.clear();
+  g_last_error[0] = 0;
   return SQ_OK;
 }
 
@@ -42,32 +41,16 @@ sq_status hip_status(hipError_t e, const char* what) {
   return fail(SQ_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-bool is_pow2(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
-
-struct Range {
-  const void* p;
-  uint64_t bytes;
-  const char* name;
-};
-
-bool overlap(const Range& a, const Range& b) {
-  if (!a.p || !b.p || a.bytes == 0 || b.bytes == 0) return false;
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-  return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
-}
-
-// Outputs must not overlap any input or each other.
-sq_status check_alias(const std::vector<Range>& ins, const std::vector<Range>& outs) {
-  for (size_t i = 0; i < outs.size(); ++i) {
-    for (const Range& in : ins)
-      if (overlap(outs[i], in)) return fail(SQ_ERR_ALIAS, "output %s overlaps input %s", outs[i].name, in.name);
-    for (size_t j = i + 1; j < outs.size(); ++j)
-      if (overlap(outs[i], outs[j]))
-        return fail(SQ_ERR_ALIAS, "output %s overlaps output %s", outs[i].name, outs[j].name);
-  }
+sq_status check_clip(float r, const char* name) {
+  if (!(r > 0.0f && r <= 1.0f)) return fail(SQ_ERR_SHAPE, "%s=%g outside (0, 1]", name, static_cast<double>(r));
   return SQ_OK;
 }
+
+}  // namespace sq::api
+
+namespace {
+
+using namespace sq::api;
 
 // Shared checks of the row-rotation arguments.
 sq_status check_rotation(int64_t K, int32_t a, const int8_t* H, int32_t b) {
@@ -90,12 +73,6 @@ sq_status check_rows(int64_t M, int64_t K, int64_t ld, const char* mname) {
   return SQ_OK;
 }
 
-// A range clipping ratio: finite, 0 < r <= 1.
-sq_status check_clip(float r, const char* name) {
-  if (!(r > 0.0f && r <= 1.0f)) return fail(SQ_ERR_SHAPE, "%s=%g outside (0, 1]", name, static_cast<double>(r));
-  return SQ_OK;
-}
-
 float inv_sqrt(int64_t n) { return static_cast<float>(1.0 / std::sqrt(static_cast<double>(n))); }
 
 }  // namespace
@@ -106,7 +83,7 @@ extern "C" {
 
 int32_t sq_abi_version(void) { return SQ_ABI_VERSION; }
 
-const char* sq_last_error(void) { return g_last_error.c_str(); }
+const char* sq_last_error(void) { return g_last_error; }
 
 sq_status sq_time_next_call(void* start_event, void* stop_event) {
   if (!start_event || !stop_event) return fail(SQ_ERR_NULL, "start_event and stop_event are required");

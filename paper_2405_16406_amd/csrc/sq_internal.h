@@ -8,6 +8,8 @@
 #include <cstdint>
 #include <vector>
 
+#include "paged.h"
+
 namespace sq {
 
 // Host: the library's dense Hadamard factor of order n (1, 28, 172); false if none.
@@ -170,6 +172,83 @@ struct KvArgs {
 };
 
 hipError_t launch_qk_had_kvquant(const KvArgs& a, hipStream_t stream);
+
+// Most tokens of a workgroup of the cache's write and read kernels.
+constexpr int kRopeTokens = 8;
+constexpr int kReadTokens = 64;
+
+struct RopeWriteArgs {
+  const uint16_t* q;     // fp16 [T, ldq]: hq heads of 128
+  const uint16_t* k;     // fp16 [T, ldk]: cache.heads heads of 128
+  const uint16_t* v;
+  int64_t ldq, ldk, ldv;
+  int64_t T;
+  int32_t hq;
+  const int32_t* cu;     // [B + 1] first row of each sequence; nullptr: row t is sequence t
+  const int32_t* lens;   // [B] tokens in the cache, the new ones included
+  int64_t B;
+  PagedCache cache;
+  const double* freq;    // [rotary / 2] radians per position
+  int32_t rotary, interleaved;
+  float magnitude;
+  float k_clip, v_clip;
+  int32_t bits, param16;
+  uint16_t* q_rot;       // fp16 [T, hq, 128]
+  uint16_t* k_rot;       // fp16 [T, cache.heads, 128] or nullptr
+  int32_t tokens;        // per workgroup, and the head counts' div_magic: set by the launch
+  uint32_t magic_hq, magic_hkv;
+};
+hipError_t launch_rope_kv_write(RopeWriteArgs a, hipStream_t stream);
+
+struct KvReadArgs {
+  const int32_t* cu;
+  const int32_t* lens;
+  int64_t B, T;
+  PagedCache cache;
+  int32_t bits, param16, plain_basis;
+  uint16_t* k;           // fp16 [T, ldk]
+  uint16_t* v;
+  int64_t ldk, ldv;
+  int32_t tokens;        // set by the launch
+  uint32_t magic_hkv;
+};
+hipError_t launch_kv_read(KvReadArgs a, hipStream_t stream);
+
+struct PagedAttnArgs {
+  const uint16_t* q;     // fp16 [B, ldq]: hq rotated heads of 128
+  int64_t ldq;
+  const int32_t* lens;   // [B]
+  int64_t B;
+  int32_t hq, group;     // group = hq / cache.heads query heads of one key/value head
+  PagedCache cache;
+  int32_t bits, param16;
+  int32_t max_len;       // lengths beyond it count as max_len
+  float scale_log2e;
+  uint16_t* out;         // fp16 [B, ldo]
+  int64_t ldo;
+  int32_t chunks;        // pieces of chunk_tokens tokens
+  int32_t chunk_tokens;
+  float* part;           // [B, hq, chunks, kAttnPart]; unused with one chunk
+};
+hipError_t launch_attn_paged(const PagedAttnArgs& a, hipStream_t stream);
+
+struct PromptArgs {
+  const uint16_t* q;     // fp16 [Tq, ldq]: hq heads of 128
+  const uint16_t* k;     // fp16 [Tk, ldk]: hkv heads of 128
+  const uint16_t* v;
+  int64_t ldq, ldk, ldv;
+  const int32_t* cu_q;   // [B + 1]
+  const int32_t* cu_k;
+  int64_t B, Tq, Tk;
+  int32_t hq, hkv, group;
+  float scale_log2e;
+  int32_t causal;
+  uint16_t* out;         // fp16 [Tq, ldo]
+  int64_t ldo;
+  int32_t splits;        // parts of the keys; 1: no partial states
+  float* part;
+};
+hipError_t launch_attn_prompt(const PromptArgs& a, hipStream_t stream);
 
 // Timing of one entry-point call (armed by sq_time_next_call, per host thread): the start
 // event is taken with the first kernel the call launches and the stop event with each

@@ -23,7 +23,8 @@ EXPORTS = ("sq_abi_version", "sq_last_error", "sq_time_next_call", "sq_hadamard_
            "sq_had_quant_act_ex", "sq_pack_w4", "sq_pack_w4_ex", "sq_w4a4_linear", "sq_w4a8_linear",
            "sq_w4a4_linear_swiglu", "sq_qk_had_kvquant", "sq_qk_had_kvquant_ex", "sq_attn_decode_kv4",
            "sq_attn_decode_kv4_ex", "sq_attn_decode_workspace", "sq_attn_decode_kv4_split",
-           "sq_attn_decode_kv4_split_noalloc")
+           "sq_attn_decode_kv4_split_noalloc", "sq_rope_frequencies", "sq_rope_kv_write", "sq_kv_read",
+           "sq_attn_paged", "sq_attn_paged_workspace", "sq_attn_prompt", "sq_attn_prompt_workspace")
 
 
 class SqError(RuntimeError):
@@ -36,7 +37,9 @@ _lib = None
 _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I32 = ctypes.c_int32
+_U64 = ctypes.c_uint64
 _F32 = ctypes.c_float
+_F64 = ctypes.c_double
 
 
 def lib() -> ctypes.CDLL:
@@ -94,6 +97,25 @@ def load(path: str) -> ctypes.CDLL:
     L.sq_attn_decode_kv4_split_noalloc.restype = _I32
     L.sq_attn_decode_kv4_split_noalloc.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _F32, _I32,
                                                    _P, _P]
+    L.sq_rope_frequencies.restype = _I32
+    L.sq_rope_frequencies.argtypes = [_I32, _F64, _I32, _F64, _F64, _F64, _F64, _P]
+    L.sq_rope_kv_write.restype = _I32
+    L.sq_rope_kv_write.argtypes = [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I64, _P, _P, _I64, _P, _I64, _I64,
+                                   _P, _P, _P, _I64, _I64, _I64, _I32, _I32, _P, _I32, _I32, _F32, _F32, _F32,
+                                   _P, _P, _P]
+    L.sq_kv_read.restype = _I32
+    L.sq_kv_read.argtypes = [_P, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _I64, _I64, _I64, _I64, _I32, _I32,
+                             _I32, _P, _I64, _P, _I64, _P]
+    L.sq_attn_paged.restype = _I32
+    L.sq_attn_paged.argtypes = [_P, _I64, _P, _I64, _P, _I64, _I64, _P, _P, _P, _I64, _I64, _I64, _I64, _I64, _I32,
+                                _I32, _I64, _F32, _P, _I64, _P, _U64, _P]
+    L.sq_attn_paged_workspace.restype = _I32
+    L.sq_attn_paged_workspace.argtypes = [_I64, _I64, _I64, _I64, _I64, _P]
+    L.sq_attn_prompt.restype = _I32
+    L.sq_attn_prompt.argtypes = [_P, _I64, _P, _I64, _P, _I64, _P, _P, _I64, _I64, _I64, _I64, _I64, _I64, _F32,
+                                 _I32, _P, _I64, _P, _U64, _P]
+    L.sq_attn_prompt_workspace.restype = _I32
+    L.sq_attn_prompt_workspace.argtypes = [_I64, _I64, _I64, _I64, _I64, _I64, _P]
     return L
 
 
@@ -394,4 +416,243 @@ def attn_decode_kv4(q_rot, k_q, k_alpha, k_beta, v_q, v_alpha, v_beta, scale=Non
                                            _ptr(v_alpha), _ptr(v_beta), B, S, H, D, float(scale),
                                            {torch.float16: 16}[pdt], _ptr(out), _stream(q_rot)),
                "sq_attn_decode_kv4_ex")
+    return out
+
+
+# ------------------------------------------------------------------ the paged cache
+
+_ROPE_SCALING = {"none": 0, "linear": 1, "by parts": 2}
+_PARAM_BITS = {torch.float32: 32, torch.float16: 16}
+
+
+def rope_frequencies(rotary_dim: int = 128, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     low: float = 1.0, high: float = 4.0, original_len: float = 8192.0, device=None) -> torch.Tensor:
+    """Angle per position of each pair of dims, fp64 [rotary_dim / 2] (sq_rope_frequencies) on
+    `device`.  scaling "none", "linear" (divided by factor) or "by parts" (kept above `high` turns
+    within original_len positions, divided by factor below `low`, mixed between)."""
+    out = np.empty(max(rotary_dim, 0) // 2, dtype=np.float64)
+    if scaling not in _ROPE_SCALING:
+        raise ValueError(f"scaling must be one of {sorted(_ROPE_SCALING)}")
+    _check(lib().sq_rope_frequencies(rotary_dim, theta, _ROPE_SCALING[scaling], factor, low, high, original_len,
+                                     out.ctypes.data), "sq_rope_frequencies")
+    return torch.from_numpy(out).to(device) if device is not None else torch.from_numpy(out)
+
+
+def kv_cache(pages: int, page: int, heads: int, bits: int = 4, param_dtype=torch.float32, device="cuda"):
+    """An empty paged cache (k_q, v_q, params): codes uint8 [pages, heads, page, 64 (4 bits) or 128],
+    group parameters [pages, heads, page, 4] (k_alpha, k_beta, v_alpha, v_beta).  Zeroed."""
+    k_q = torch.zeros((pages, heads, page, 16 * bits), dtype=torch.uint8, device=device)
+    return k_q, torch.zeros_like(k_q), torch.zeros((pages, heads, page, 4), dtype=param_dtype, device=device)
+
+
+class _On:
+    """Makes t's device the current one for a call, where it is not."""
+
+    __slots__ = ("guard",)
+
+    def __init__(self, t):
+        d = t.get_device()
+        self.guard = None if d == torch.cuda.current_device() else torch.cuda.device(d)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _heads(t, name):
+    """(rows, heads, ld) of fp16 [rows, heads, 128] whose heads are contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float16 or not t.is_cuda:
+        raise TypeError(f"{name} must be a torch.float16 tensor on the GPU")
+    if t.dim() != 3 or t.shape[2] != 128:
+        raise ValueError(f"{name} must be [rows, heads, 128]")
+    rows, heads, _ = t.shape
+    ld, sh, sd = t.stride()
+    if sd != 1 or (sh != 128 and heads > 1):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return rows, heads, ld if rows > 1 else heads * 128
+
+
+def _index(t, name, n=None):
+    """A contiguous int32 vector (of n entries) on the GPU."""
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or not t.is_cuda:
+        raise TypeError(f"{name} must be a torch.int32 tensor on the GPU")
+    if t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be a contiguous vector" + ("" if n is None else f" of {n} entries"))
+    return t.shape[0]
+
+
+def _cache_args(cache, table, B):
+    """The cache's arguments: table, its stride and columns, the three tensors, pages, page, heads; and
+    (bits, param_bits)."""
+    k_q, v_q, params = cache
+    _need(k_q, torch.uint8, "k_q")
+    _need(v_q, torch.uint8, "v_q")
+    if not isinstance(params, torch.Tensor) or params.dtype not in _PARAM_BITS or not params.is_cuda:
+        raise TypeError("params must be a torch.float32 or torch.float16 tensor on the GPU")
+    if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or not table.is_cuda:
+        raise TypeError("block_table must be a torch.int32 tensor on the GPU")
+    if k_q.dim() != 4 or v_q.shape != k_q.shape or params.shape != (*k_q.shape[:3], 4):
+        raise ValueError("the cache is codes [pages, heads, page, bytes] twice and parameters [pages, heads, page, 4]")
+    if not (k_q.is_contiguous() and v_q.is_contiguous() and params.is_contiguous()):
+        raise ValueError("the cache's tensors must be contiguous")
+    if table.dim() != 2 or table.shape[0] != B or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError(f"block_table must be [{B}, blocks] with unit column stride")
+    pages, heads, page, row = k_q.shape
+    if row not in (64, 128):
+        raise ValueError("a token's codes are 64 (4 bits) or 128 (8 bits) bytes")
+    cols = table.shape[1]
+    return ((table.data_ptr(), table.stride(0) if B > 1 else cols, cols, k_q.data_ptr(), v_q.data_ptr(), params.data_ptr(),
+             pages, page, heads), (row // 16, _PARAM_BITS[params.dtype]))
+
+
+def _same_device(t, *others):
+    d = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != d:
+            raise ValueError("all tensors of a call must be on one device")
+
+
+def rope_kv_write(q, k, v, cache, block_table, lens, freq=None, cu=None, interleaved: bool = False, magnitude: float = 1.0,
+                  k_clip: float = 1.0, v_clip: float = 1.0, out=None, k_out=None):
+    """Rotary positions and R3 on q, k and the quantized write of k, v into the pages
+    (sq_rope_kv_write).  q fp16 [T, Hq, 128], k, v fp16 [T, Hkv, 128] before positions (slices of a
+    fused projection are fine); lens int32 [B] with the new tokens; cu int32 [B + 1], or None for one
+    token a sequence; freq fp64 [rotary_dim / 2] (rope_frequencies), None for no positions.
+    k_out: optional fp16 [T, Hkv, 128] that takes the rotated keys.  Returns q rotated, fp16 [T, Hq, 128]."""
+    T, Hq, ldq = _heads(q, "q")
+    tk, Hkv, ldk = _heads(k, "k")
+    tv, hv, ldv = _heads(v, "v")
+    if tk != T or tv != T or hv != Hkv:
+        raise ValueError("q, k and v disagree on their rows or heads")
+    B = _index(lens, "lens")
+    if cu is not None:
+        _index(cu, "cu", B + 1)
+    args, bits = _cache_args(cache, block_table, B)
+    if args[-1] != Hkv:
+        raise ValueError("k and the cache disagree on their heads")
+    rotary = 0
+    if freq is not None:
+        _need(freq, torch.float64, "freq")
+        if freq.dim() != 1 or not freq.is_contiguous():
+            raise ValueError("freq must be a contiguous vector")
+        rotary = 2 * freq.shape[0]
+    if out is None:
+        out = q.new_empty((T, Hq, 128))
+    for t, h, n in ((out, Hq, "out"), (k_out, Hkv, "k_out")):
+        if t is not None:
+            _need(t, torch.float16, n)
+            if tuple(t.shape) != (T, h, 128) or not t.is_contiguous():
+                raise ValueError(f"{n} must be contiguous [{T}, {h}, 128]")
+    _same_device(q, k, v, *cache, block_table, lens, cu, freq, out, k_out)
+    if T == 0 or B == 0:  # an empty tensor has no address
+        return out
+    with _On(q):
+        _check(lib().sq_rope_kv_write(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, Hq, 128, _ptr(cu),
+                                      lens.data_ptr(), B, *args, *bits, _ptr(freq), rotary, int(interleaved), magnitude,
+                                      k_clip, v_clip, out.data_ptr(), _ptr(k_out), _stream(q)), "sq_rope_kv_write")
+    return out
+
+
+def kv_read(cache, block_table, lens, cu, rows: int, plain_basis: bool = False, out=None):
+    """Keys and values of the sequences' last tokens out of the pages (sq_kv_read): (k, v) fp16
+    [rows, Hkv, 128] packed by cu int32 [B + 1], keys in R3's basis, or turned back with plain_basis.
+    Rows of no sequence are left as they are in `out` (a pair of tensors; allocated unset when None)."""
+    B = _index(lens, "lens")
+    _index(cu, "cu", B + 1)
+    args, bits = _cache_args(cache, block_table, B)
+    Hkv = args[-1]
+    if out is None:
+        k = cache[2].new_empty((rows, Hkv, 128), dtype=torch.float16)
+        v = torch.empty_like(k)
+    else:
+        k, v = out
+    tk, hk, ldk = _heads(k, "k")
+    tv, hv, ldv = _heads(v, "v")
+    if (tk, hk, tv, hv) != (rows, Hkv, rows, Hkv):
+        raise ValueError(f"out must be two [{rows}, {Hkv}, 128] tensors")
+    _same_device(k, v, *cache, block_table, lens, cu)
+    if rows == 0 or B == 0:
+        return k, v
+    with _On(k):
+        _check(lib().sq_kv_read(cu.data_ptr(), lens.data_ptr(), B, rows, *args, 128, *bits, int(plain_basis), k.data_ptr(), ldk,
+                                v.data_ptr(), ldv, _stream(k)), "sq_kv_read")
+    return k, v
+
+
+def attn_paged_workspace_bytes(B, max_len, Hq, Hkv):
+    """Device bytes of attn_paged's workspace on the current device."""
+    n = _U64(0)
+    _check(lib().sq_attn_paged_workspace(B, max_len, Hq, Hkv, 128, ctypes.byref(n)), "sq_attn_paged_workspace")
+    return n.value
+
+
+def attn_paged(q, cache, block_table, lens, max_len: int, scale=None, out=None, workspace=None):
+    """Attention of one rotated query per sequence over its pages (sq_attn_paged): q fp16
+    [B, Hq, 128]; max_len at least the longest of lens.  workspace: a uint8 device tensor of at least
+    attn_paged_workspace_bytes() bytes, allocated here when None.  Returns out fp16 [B, Hq, 128]."""
+    B, Hq, ldq = _heads(q, "q")
+    _index(lens, "lens", B)
+    args, bits = _cache_args(cache, block_table, B)
+    if out is None:
+        out = q.new_empty((B, Hq, 128))
+    to, ho, ldo = _heads(out, "out")
+    if (to, ho) != (B, Hq):
+        raise ValueError(f"out must be [{B}, {Hq}, 128]")
+    if B == 0:
+        return out
+    with _On(q):
+        if workspace is None:
+            n = attn_paged_workspace_bytes(B, max_len, Hq, args[-1])
+            workspace = q.new_empty(n, dtype=torch.uint8) if n else None
+        else:
+            _need(workspace, torch.uint8, "workspace")
+        _same_device(q, *cache, block_table, lens, out, workspace)
+        _check(lib().sq_attn_paged(q.data_ptr(), ldq, lens.data_ptr(), B, *args, Hq, 128, *bits, max_len,
+                                   0.08838834764831845 if scale is None else scale, out.data_ptr(), ldo, _ptr(workspace),
+                                   0 if workspace is None else workspace.numel(), _stream(q)), "sq_attn_paged")
+    return out
+
+
+def attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv):
+    """Device bytes of attn_prompt's workspace on the current device."""
+    n = _U64(0)
+    _check(lib().sq_attn_prompt_workspace(B, Tq, Tk, Hq, Hkv, 128, ctypes.byref(n)), "sq_attn_prompt_workspace")
+    return n.value
+
+
+def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, workspace=None):
+    """Attention of packed sequences (sq_attn_prompt): q fp16 [Tq, Hq, 128], k, v fp16 [Tk, Hkv, 128],
+    sequence b the rows cu_q[b] .. of q and cu_k[b] .. of k and v (int32 [B + 1] each); causal: its
+    queries are its last tokens.  workspace: a uint8 device tensor of at least
+    attn_prompt_workspace_bytes() bytes, allocated here when None.  Returns out fp16 [Tq, Hq, 128]; rows
+    of no sequence are left as they are in `out` (allocated unset when None)."""
+    Tq, Hq, ldq = _heads(q, "q")
+    Tk, Hkv, ldk = _heads(k, "k")
+    tv, hv, ldv = _heads(v, "v")
+    if tv != Tk or hv != Hkv:
+        raise ValueError("k and v disagree on their rows or heads")
+    B = _index(cu_q, "cu_q") - 1
+    _index(cu_k, "cu_k", B + 1)
+    if out is None:
+        out = q.new_empty((Tq, Hq, 128))
+    to, ho, ldo = _heads(out, "out")
+    if (to, ho) != (Tq, Hq):
+        raise ValueError(f"out must be [{Tq}, {Hq}, 128]")
+    if Tq == 0 or B == 0:
+        return out
+    with _On(q):
+        if workspace is None:
+            n = attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv)
+            workspace = q.new_empty(n, dtype=torch.uint8) if n else None
+        else:
+            _need(workspace, torch.uint8, "workspace")
+        _same_device(q, k, v, cu_q, cu_k, out, workspace)
+        _check(lib().sq_attn_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(), cu_k.data_ptr(), B,
+                                    Tq, Tk, Hq, Hkv, 128, 0.08838834764831845 if scale is None else scale, int(causal),
+                                    out.data_ptr(), ldo, _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                    _stream(q)), "sq_attn_prompt")
     return out
