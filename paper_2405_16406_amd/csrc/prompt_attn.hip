@@ -55,6 +55,18 @@ __device__ __forceinline__ float halves(float v, Op op) {
   return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
+// Schedule of a run of N products whose first operand takes R LDS reads: reads stay AHEAD operands
+// in front (the compiler would read all of them first and run out of registers).
+template <int N, int R, int AHEAD>
+__device__ __forceinline__ void pace() {
+  __builtin_amdgcn_sched_group_barrier(0x100, R * AHEAD, 0);  // LDS reads
+  static_for<N - AHEAD>([](auto) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  });
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 // Sequence and tile of the tile number `rem` among ceil(rows / 256) tiles a sequence.
 struct PromptTile {
   int seq;          // -1: past the last
@@ -157,16 +169,15 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   const uint8_t* const kbase = reinterpret_cast<const uint8_t*>(k + k0 * a.ldk + static_cast<int64_t>(hk) * 128);
   const uint8_t* const vbase = reinterpret_cast<const uint8_t*>(v + k0 * a.ldv + static_cast<int64_t>(hk) * 128);
   typedef __attribute__((address_space(3))) void* lds_ptr;
-  auto issue = [&](int kt, int buf) {
+  auto issue = [&](int kt, int buf, bool keys_of) __attribute__((always_inline)) {
     // rows past the last key are out of the buffer and land as zeros
-    const int n = min(kTile, m - kt * kTile);
-    const __amdgpu_buffer_rsrc_t rk = buf_rsrc(kbase + static_cast<int64_t>(kt) * kTile * ldk2, static_cast<int64_t>(n - 1) * ldk2 + 256);
-    const __amdgpu_buffer_rsrc_t rv = buf_rsrc(vbase + static_cast<int64_t>(kt) * kTile * ldv2, static_cast<int64_t>(n - 1) * ldv2 + 256);
+    const int rows_here = min(kTile, m - kt * kTile), ld2 = keys_of ? ldk2 : ldv2;
+    const __amdgpu_buffer_rsrc_t rs =
+        buf_rsrc((keys_of ? kbase : vbase) + static_cast<int64_t>(kt) * kTile * ld2, static_cast<int64_t>(rows_here - 1) * ld2 + 256);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      uint8_t* dst = lds + buf * kTileBytes + (2 * w + x) * 1024;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_ptr)(uintptr_t)dst, 16, koff[x], 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_ptr)(uintptr_t)(dst + 2 * kTileBytes), 16, voff[x], 0, 0, 0);
+      uint8_t* dst = lds + (buf + (keys_of ? 0 : 2)) * kTileBytes + (2 * w + x) * 1024;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)dst, 16, keys_of ? koff[x] : voff[x], 0, 0, 0);
     }
   };
 
@@ -174,12 +185,12 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   // row 4 h + i / 4 (+ 8), dims 32 dt + 16 (gi % 2) + 4 (i % 4) .. and gets dim 32 dt + col of four keys
   const int ksw = swizzle(col);
   const int vrow = 4 * h + ((lane & 15) >> 2), vlow = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), vsub = 8 * (lane & 1);
-  auto v_read = [&](int buf, int ks, int dt, int second) -> v4s {
+  auto v_read = [&](int buf, int ks, int dt, int second) __attribute__((always_inline)) -> v4s {
     const int t = vrow + 8 * second;
     const int off = (2 + buf) * kTileBytes + ks * 16 * 256 + t * 256 + 16 * ((4 * dt + vlow) ^ swizzle(t)) + vsub;
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(lds + off));
   };
-  auto v_operand = [&](int buf, int ks, int dt) -> v8h {
+  auto v_operand = [&](int buf, int ks, int dt) __attribute__((always_inline)) -> v8h {
     const v4s x = v_read(buf, ks, dt, 0), y = v_read(buf, ks, dt, 1);
     return __builtin_bit_cast(v8h, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
   };
@@ -191,9 +202,10 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
   const float cs = a.scale_log2e;
+  v16f s[2];   // scores of a tile: keys 32 mt + 8 (r / 4) + 4 h + r % 4
+  v8h pf[4];   // its weights, an operand of the second product
 
-  auto step = [&](int kt, int buf) {
-    v16f s[2];
+  auto scores = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
@@ -204,14 +216,19 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
         s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[x], s[mt], 0, 0, 0);
       }
     }
-    // keys 64 kt + 32 mt + 8 (r / 4) + 4 h + r % 4
-    const bool masked = kt * kTile + kTile - 1 > wave_lo;  // uniform over the wave
-    if (masked) {
+    pace<16, 1, 4>();
+  };
+
+  // MASK: the tile holds keys that a row of the wave does not see
+  auto softmax = [&](int kt, auto mc) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(mc)::value;
+    if constexpr (MASK) {
+      const int left = lim - kt * kTile - 4 * h;
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (kt * kTile + 32 * mt + 8 * (r >> 2) + 4 * h + (r & 3) > lim) s[mt][r] = -INFINITY;
+          if (32 * mt + 8 * (r >> 2) + (r & 3) > left) s[mt][r] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
@@ -219,43 +236,85 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[1][r]);
     top = halves(top, [](float x, float y) { return fmaxf(x, y); }) * cs;
-    if (__ballot(top > mx + kSlack)) {  // (mx = -inf: any score)
-      const float mn = fmaxf(mx, top);
-      const float f = rescale(mx, mn);
-      l *= f;
+    const float mn = fmaxf(mx, top);
+    const float f = rescale(mx, mn);
+    l *= f;
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt) acc[dt] *= f;
-      mx = mn;
-    }
+    for (int dt = 0; dt < 4; ++dt) acc[dt] *= f;
+    mx = mn;
     const float base = (mx == -INFINITY ? 0.0f : mx) - kWeightBits;
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[mt][r] = exp2_fast(__fmaf_rn(s[mt][r], cs, -base));
-        l += s[mt][r];
-      }
-    v8h pf[4];
+    // the sum is that of the rounded weights: their rounding then moves the mean of the values
+    // seen, not its size
+    float l0 = 0.0f, l1 = 0.0f;
+    const v2h ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
       uint32_t p[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) p[r] = f2h2(s[ks >> 1][8 * (ks & 1) + 2 * r], s[ks >> 1][8 * (ks & 1) + 2 * r + 1]);
+      for (int r = 0; r < 4; ++r) {
+        const float x = exp2_fast(__fmaf_rn(s[ks >> 1][8 * (ks & 1) + 2 * r], cs, -base));
+        const float y = exp2_fast(__fmaf_rn(s[ks >> 1][8 * (ks & 1) + 2 * r + 1], cs, -base));
+        p[r] = f2h2(x, y);
+        float& lr = r & 1 ? l1 : l0;
+        lr = __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, p[r]), ones, lr, false);
+      }
       pf[ks] = __builtin_bit_cast(v8h, v4u{p[0], p[1], p[2], p[3]});
     }
-    // A weight of 0 does not hide a value that is not finite, and in a masked tile some rows must
-    // not see what others do: there, such values are taken out of the product and added by hand.
-    if (masked) {
-      uint32_t odd = 0;
+    l += l0 + l1;
+  };
+
+  // A weight of 0 does not hide a value that is not finite, and in a masked tile some rows must not
+  // see what others do: there, such values stay out of the product and are added by hand, in the
+  // lane's own place of the result, which the end takes up (`odd`).
+  bool odd = false;
+  typename std::conditional<SPLIT, float, uint16_t>::type* own;
+  if constexpr (SPLIT)
+    own = a.part + ((qrow * a.hq + head) * a.splits + split) * kAttnPart + 4 + 4 * h;
+  else
+    own = a.out + qrow * a.ldo + head * 128 + 4 * h;
+  auto own_get = [&](int d) -> float {
+    if constexpr (SPLIT) return own[d];
+    else return h2f(own[d]);
+  };
+  auto own_set = [&](int d, float x) {
+    if constexpr (SPLIT) own[d] = x;
+    else own[d] = f2h(x);
+  };
+  auto add_odd = [&](int kt, int buf) __attribute__((always_inline)) {
+    const bool mine = row < rows;
+    if (!odd && mine)
+#pragma unroll 1
+      for (int d = 0; d < 128; d += 8)
+        for (int e = 0; e < 4; ++e) own_set(d + e, 0.0f);
+    odd = true;
+#pragma unroll 1
+    for (int t = 0; t < kTile; ++t) {
+      if (kt * kTile + t > lim || !mine) continue;
+#pragma unroll 1
+      for (int c = 0; c < 16; ++c) {
+        const v2u u = *reinterpret_cast<const v2u*>(lds + (2 + buf) * kTileBytes + t * 256 + 16 * (c ^ swizzle(t)) + 8 * h);
+        for (int e = 0; e < 4; ++e) {
+          const uint16_t x = static_cast<uint16_t>(u[e >> 1] >> (16 * (e & 1)));
+          if ((x & 0x7C00u) == 0x7C00u) own_set(8 * c + e, own_get(8 * c + e) + h2f(x));
+        }
+      }
+    }
+  };
+  auto values = [&](int kt, int buf, auto mc) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(mc)::value;
+    if constexpr (MASK) {
+      uint32_t any = 0;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) {
           const v4u u = __builtin_bit_cast(v4u, v_operand(buf, ks, dt));
 #pragma unroll
-          for (int y = 0; y < 4; ++y) odd |= (u[y] & 0x7C007C00u) + 0x04000400u;
+          for (int y = 0; y < 4; ++y) any |= (u[y] & 0x7C007C00u) + 0x04000400u;
         }
-      if (__ballot((odd & 0x80008000u) != 0)) {
+      pace<16, 2, 4>();
+      if (__builtin_expect(__ballot((any & 0x80008000u) != 0) != 0, 0)) {
+        add_odd(kt, buf);
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
@@ -264,25 +323,11 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
               const uint32_t e = (u[y] & 0x7C007C00u) + 0x04000400u;
-              if (e & 0x8000u) u[y] &= 0xFFFF0000u;
-              if (e & 0x80000000u) u[y] &= 0x0000FFFFu;
+              u[y] &= ~(((e >> 15) & 0x00010001u) * 0xFFFFu);
             }
             acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, u), pf[ks], acc[dt], 0, 0, 0);
+            asm volatile("" ::: "memory");
           }
-        for (int t = 0; t < kTile; ++t) {
-          if (kt * kTile + t > lim) continue;
-#pragma unroll
-          for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const v2u u = *reinterpret_cast<const v2u*>(lds + (2 + buf) * kTileBytes + t * 256 + 16 * ((4 * dt + y) ^ swizzle(t)) + 8 * h);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint16_t x = static_cast<uint16_t>(u[e >> 1] >> (16 * (e & 1)));
-                if ((x & 0x7C00u) == 0x7C00u) acc[dt][4 * y + e] += h2f(x);
-              }
-            }
-        }
         return;
       }
     }
@@ -291,45 +336,104 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
         acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand(buf, ks, dt), pf[ks], acc[dt], 0, 0, 0);
+    pace<16, 2, 4>();
   };
 
-  if (kt0 < kt1) issue(kt0, 0);
-  for (int kt = kt0; kt < kt1; kt += 2) {
-    static_for<2>([&](auto bc) {
-      constexpr int buf = decltype(bc)::value;
-      if (kt + buf < kt1) {  // uniform over the workgroup
-        wait_vm_lgkm0<0>();  // this wave's part of tile kt + buf has landed
-        __syncthreads();     // every part has; and every wave is done with the other buffer
-        if (kt + buf + 1 < kt1) issue(kt + buf + 1, buf ^ 1);
-        if ((kt + buf) * kTile <= wave_hi) step(kt + buf, buf);
-      }
-    });
+  // Phases, a barrier after each.  Of the two waves of a SIMD the second (w >= 4) is one phase
+  // behind the first, so that one's products run beside the other's softmax: in step 2 j a wave
+  // takes the scores of tile j and the values of tile j - 1, in step 2 j + 1 the softmax of tile j.
+  // Tile j's keys are read in the phases 2 j and 2 j + 1, its values in 2 j + 2 and 2 j + 3; in
+  // phase 2 i the buffers of keys i + 1 and values i are free, and the copies have until the end of
+  // the next phase to land.
+  const int late = w >> 2;
+  const int n = kt1 - kt0;
+  const auto tiles_in = [&](int key) { return min(max((key + kTile) / kTile - kt0, 0), n); };
+  const int nw = wave_hi < 0 ? 0 : tiles_in(wave_hi);         // tiles that a row of the wave sees a key of
+  const int nf = min(nw, max((wave_lo + 1) / kTile - kt0, 0));  // those that every row sees whole
+  const auto fetch = [&](int i) __attribute__((always_inline)) {  // in phase 2 i
+    if (i + 1 < n) issue(kt0 + i + 1, (i + 1) & 1, true);
+    if (i < n) issue(kt0 + i, i & 1, false);
+  };
+  const auto meet = [&]() __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // the ends of a wave's steps 2 j and 2 j + 1
+  const auto end_products = [&](int j) __attribute__((always_inline)) {
+    if (late) {
+      wait_vm_lgkm0<0>();
+      meet();
+      fetch(j + 1);
+    } else {
+      fetch(j);  // behind the reads: the compiler waits for copies before an LDS read
+      wait_vm_lgkm0<63>();
+      meet();
+    }
+  };
+  const auto end_softmax = [&]() __attribute__((always_inline)) {
+    if (!late) wait_vm_lgkm0<0>();
+    meet();
+  };
+  if (n > 0) issue(kt0, 0, true);
+  wait_vm_lgkm0<0>();
+  meet();
+  if (late) {
+    fetch(0);
+    meet();
   }
+  if (nw > 0) {
+    scores(0);
+    end_products(0);
+    softmax(kt0, std::true_type{});
+    end_softmax();
+    int j = 1;
+    for (; j < nf; ++j) {
+      values(kt0 + j - 1, (j - 1) & 1, std::false_type{});
+      scores(j & 1);
+      end_products(j);
+      softmax(kt0 + j, std::false_type{});
+      end_softmax();
+    }
+    for (; j < nw; ++j) {
+      values(kt0 + j - 1, (j - 1) & 1, std::true_type{});
+      scores(j & 1);
+      end_products(j);
+      softmax(kt0 + j, std::true_type{});
+      end_softmax();
+    }
+    values(kt0 + nw - 1, (nw - 1) & 1, std::true_type{});
+  }
+  for (int j = nw; j < n; ++j) {  // other waves' tiles
+    end_products(j);
+    end_softmax();
+  }
+  if (!late) meet();
 
   l = halves(l, [](float x, float y) { return __fadd_rn(x, y); });
   if (row >= rows) return;
   if constexpr (SPLIT) {
-    float* pr = a.part + ((qrow * a.hq + head) * a.splits + split) * kAttnPart;
     if (h == 0) {
-      pr[0] = mx;
-      pr[1] = l;
+      own[-4] = mx;
+      own[-3] = l;
     }
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-        *reinterpret_cast<float4*>(pr + 4 + 32 * dt + 8 * y + 4 * h) =
-            make_float4(acc[dt][4 * y], acc[dt][4 * y + 1], acc[dt][4 * y + 2], acc[dt][4 * y + 3]);
-  } else {
-    const float inv = mx == -INFINITY ? 0.0f : __fdiv_rn(1.0f, l);  // a row that sees nothing is zero
-    uint16_t* o = a.out + qrow * a.ldo + head * 128 + 4 * h;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-        *reinterpret_cast<v2u*>(o + 32 * dt + 8 * y) =
-            v2u{f2h2(acc[dt][4 * y] * inv, acc[dt][4 * y + 1] * inv), f2h2(acc[dt][4 * y + 2] * inv, acc[dt][4 * y + 3] * inv)};
   }
+  const float inv = SPLIT ? 1.0f : mx == -INFINITY ? 0.0f : __fdiv_rn(1.0f, l);  // a row that sees nothing is zero
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = acc[dt][4 * y + e] * inv;
+      if (__builtin_expect(odd, 0))
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += own_get(32 * dt + 8 * y + e);
+      if constexpr (SPLIT)
+        *reinterpret_cast<float4*>(own + 32 * dt + 8 * y) = make_float4(o[0], o[1], o[2], o[3]);
+      else
+        *reinterpret_cast<v2u*>(own + 32 * dt + 8 * y) = v2u{f2h2(o[0], o[1]), f2h2(o[2], o[3])};
+    }
 }
 
 // One wave per (row of q, query head) of the sequences: the splits' states, in their order.
