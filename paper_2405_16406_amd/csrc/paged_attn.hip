@@ -17,7 +17,7 @@
 //   softmax   in base 2.  V's scale goes into the weight, w_t = 2^(s_t + log2 va_t - m), with m
 //             the running maximum of that exponent: the fp16 weights of the second product are
 //             then near 1 at their largest whatever the size of V.  The sums are
-//             l = sum w_t / va_t and b = sum w_t vb_t / va_t in fp32, over unrounded w.  m moves
+//             l = sum w_t / va_t and b = sum w_t vb_t / va_t in fp32.  m moves
 //             (and everything is rescaled) only when it would grow by more than kSlack.
 //   values    O^T += V^T w^T: the block's value codes go through LDS as they are (64 or 128
 //             bytes a token) and come back transposed (ds_read_b64_tr_b4 / _b8): lane (i, g)
@@ -90,8 +90,11 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
   div_rem(blockIdx.x, a.cache.heads, magic_heads, rest, hk);
   div_rem(rest, tiles, magic_tiles, rest, tile);
   div_rem(rest, chunks, magic_chunks, b, c);
-  const int len = min(max(lens[b], 0), a.max_len);
   const int first = static_cast<int>(c) * a.chunk_tokens;
+  const int32_t* const table = a.cache.table + b * a.cache.ldt;
+  const int32_t first_col = table_column(a.cache, first + w * kBlock + 16 * g);
+  const int32_t first_entry = first_col < 0 ? -1 : table[first_col];
+  const int len = min(max(lens[b], 0), a.max_len);
   if (c > 0 && first >= len) return;  // the workgroup leaves together
   const int last = min(len, first + a.chunk_tokens);
   const int heads = min(16, a.group - 16 * static_cast<int>(tile));  // of this workgroup
@@ -133,8 +136,6 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
 
   uint8_t* const vlds = lds + w * W::BYTES;
   float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
-  const int32_t* const table = a.cache.table + b * a.cache.ldt;
-  const int page = 1 << a.cache.shift;
   constexpr int KW = BITS == 4 ? 1 : 2;  // 16-byte loads of a lane's key codes
   // 2^24 undoes the codes' subnormal scale
   const float cs = a.scale_log2e, cs24 = a.scale_log2e * 16777216.0f;
@@ -142,42 +143,37 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
   v4u kc[4][KW], vc[4][KW];
   float4 par;
   bool par_ok;
-  // Page of the block's 16-token group n, -1 past the chunk or the pool (pages hold 16 tokens or
-  // more, so a group lies in one page).
-  auto page_of = [&](int t) -> int32_t {
-    if (t >= last) return -1;
-    const int32_t col = table_column(a.cache, t);
-    return col < 0 ? -1 : valid_page(a.cache, table[col]);
+  // A block's pages: each lane holds that of its 16-token group, lane / 16 (pages hold 16 tokens or
+  // more, so a group lies in one).  The table entry is read a block ahead of the codes, and for the
+  // first block beside the length.
+  auto entry_of = [&](int t0) -> int32_t {
+    const int32_t col = table_column(a.cache, t0 + 16 * g);
+    return col < 0 ? -1 : table[col];
   };
-  auto load = [&](int t0) {
-    // lane's group for keys: i / 4; for values and parameters: 16-token groups by lane / 16
-    const int32_t mine = page_of(t0 + 16 * g);
+  auto load = [&](int t0, int32_t entry) __attribute__((always_inline)) {
+    // tokens without a page, or past the chunk, read page 0 and are masked below
+    const int32_t mine = valid_page(a.cache, entry);
+    par_ok = mine >= 0 && t0 + lane < last;
+    const int32_t safe = max(mine, 0);
     int32_t pg[4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) pg[n] = __builtin_amdgcn_readlane(mine, 16 * n);
-    const int n = i >> 2;
+    for (int n = 0; n < 4; ++n) pg[n] = __builtin_amdgcn_readlane(safe, 16 * n);
+    const int n = i >> 2;  // keys: the lane's token is one of group i / 4
     const int32_t pk = n == 0 ? pg[0] : n == 1 ? pg[1] : n == 2 ? pg[2] : pg[3];
-    // tokens that are not there read token 0 of page 0 and are masked below
-    const int64_t kslot = pk < 0 ? 0 : token_slot(a.cache, pk, hk, t0 + 16 * n + (i & 3));
-    const uint8_t* kp = a.cache.kq + kslot * W::ROW + (BITS == 4 ? 16 : 32) * g;
+    const uint8_t* kp = a.cache.kq + token_slot(a.cache, pk, hk, t0 + 16 * n + (i & 3)) * W::ROW + (BITS == 4 ? 16 : 32) * g;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int x = 0; x < KW; ++x)
-        kc[j][x] = *reinterpret_cast<const v4u*>(kp + (pk < 0 ? 0 : 4 * j * W::ROW) + 16 * x);
-    // value codes: load n brings group n, four (eight) lanes a token
+      for (int x = 0; x < KW; ++x) kc[j][x] = *reinterpret_cast<const v4u*>(kp + 4 * j * W::ROW + 16 * x);
+    // values: load m brings group m, four (eight) lanes a token
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int m = 0; m < 4; ++m) {
+      const uint8_t* vp = a.cache.vq + token_slot(a.cache, pg[m], hk, t0 + 16 * m) * W::ROW + 16 * lane;
 #pragma unroll
-      for (int x = 0; x < KW; ++x) {
-        const int row = BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3);
-        const int unit = BITS == 4 ? lane & 3 : lane & 7;
-        const int64_t vslot = pg[m] < 0 ? 0 : token_slot(a.cache, pg[m], hk, t0 + 16 * m + row);
-        vc[m][x] = *reinterpret_cast<const v4u*>(a.cache.vq + vslot * W::ROW + 16 * unit);
-      }
+      for (int x = 0; x < KW; ++x) vc[m][x] = *reinterpret_cast<const v4u*>(vp + 1024 * x);
+    }
     // parameters: lane's token is t0 + lane
-    par_ok = mine >= 0 && t0 + lane < last;
-    const int64_t pslot = par_ok ? token_slot(a.cache, mine, hk, t0 + lane) : 0;
+    const int64_t pslot = token_slot(a.cache, safe, hk, t0 + lane);
     if constexpr (P16) {
       const uint2 p = static_cast<const uint2*>(a.cache.params)[pslot];
       par = make_float4(h2f(static_cast<uint16_t>(p.x)), h2f(static_cast<uint16_t>(p.x >> 16)),
@@ -194,7 +190,11 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
 
   const int step = kWaves * kBlock;
   int t0 = first + w * kBlock;
-  if (t0 < last) load(t0);
+  int32_t entry = -1;
+  if (t0 < last) {
+    load(t0, first_entry);
+    entry = entry_of(t0 + step);
+  }
   for (; t0 < last; t0 += step) {
     // value codes and coefficients to LDS (this wave's own: no barrier, its LDS operations are
     // in order); unit u of a row of 4 (8) units lies at u xor (row / 4) % 4 (u xor row % 8)
@@ -202,7 +202,7 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
     for (int mm = 0; mm < 4; ++mm)
 #pragma unroll
       for (int x = 0; x < KW; ++x) {
-        const int row = 16 * mm + (BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3));
+        const int row = 16 * mm + (BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3));  // 16 bytes a lane, in order
         const int unit = BITS == 4 ? (lane & 3) ^ ((row >> 2) & 3) : (lane & 7) ^ (row & 7);
         *reinterpret_cast<v4u*>(vlds + row * W::ROW + 16 * unit) = vc[mm][x];
       }
@@ -217,7 +217,10 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int x = 0; x < KW; ++x) kn[j][x] = kc[j][x];
-    if (t0 + step < last) load(t0 + step);
+    if (t0 + step < last) {
+      load(t0 + step, entry);
+      entry = entry_of(t0 + 2 * step);
+    }
     asm volatile("" ::: "memory");
 
     // scores of 16 tokens of head i
@@ -267,31 +270,43 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
       for (int dt = 0; dt < 8; ++dt) acc[dt] *= f;
       m = mn;
     }
+    // Weights in the value codes' pair order, rounded to fp16.  l and b sum the rounded ones: their
+    // rounding then moves the mean of the values seen by 2^-12 of their spread; against unrounded
+    // sums it would be 2^-12 of sum w e, whose bulk cancels against b (errors of the output 0.4 -
+    // 0.8e-3 over long caches instead of 0.2 - 0.3e-3).
     const float base = (m == -INFINITY ? 0.0f : m) - kWeightBits;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 cr = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 4 * j);
-      const float4 cv = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 4 * j);
-      const float* fr = &cr.x;
-      const float* fv = &cv.x;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float p = exp2_fast(s[4 * j + r] - base);
-        s[4 * j + r] = p;
-        l = __fmaf_rn(p, fr[r], l);
-        bsum = __fmaf_rn(p, fv[r], bsum);
-      }
-    }
-    // weights in the value codes' pair order, rounded to fp16 (2^-12 of a weight, as the output)
-    v8h pf[2];
+    uint32_t pw[8];
+    float l16 = 0.0f, b16 = 0.0f;  // of the tokens whose weights are kept as 1 / 16
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const float* p = s + 8 * x;
-      if constexpr (BITS == 4)
-        pf[x] = operand(f2h2(p[0], p[4]), f2h2(p[1] * 0.0625f, p[5] * 0.0625f), f2h2(p[2], p[6]), f2h2(p[3] * 0.0625f, p[7] * 0.0625f));
-      else
-        pf[x] = operand(f2h2(p[0], p[2]), f2h2(p[1], p[3]), f2h2(p[4], p[6]), f2h2(p[5], p[7]));
+      const float4 cr0 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 8 * x);
+      const float4 cr1 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 8 * x + 4);
+      const float4 cv0 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 8 * x);
+      const float4 cv1 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 8 * x + 4);
+      const float fr[8] = {cr0.x, cr0.y, cr0.z, cr0.w, cr1.x, cr1.y, cr1.z, cr1.w};
+      const float fv[8] = {cv0.x, cv0.y, cv0.z, cv0.w, cv1.x, cv1.y, cv1.z, cv1.w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        // pairs of tokens: 4 bits (0, 4), (1, 5) / 16, (2, 6), (3, 7) / 16; 8 bits (0, 2), (1, 3), ..
+        const int t0 = BITS == 4 ? y : 4 * (y >> 1) + (y & 1), t1 = t0 + (BITS == 4 ? 4 : 2);
+        const bool sixteenth = BITS == 4 && (y & 1);
+        const float by = sixteenth ? base + 4.0f : base;
+        const uint32_t p2 = f2h2(exp2_fast(s[8 * x + t0] - by), exp2_fast(s[8 * x + t1] - by));
+        pw[4 * x + y] = p2;
+        const v2h ph = __builtin_bit_cast(v2h, p2);
+        float& ls = sixteenth ? l16 : l;
+        float& bs = sixteenth ? b16 : bsum;
+        ls = __fmaf_rn(static_cast<float>(ph[0]), fr[t0], ls);
+        ls = __fmaf_rn(static_cast<float>(ph[1]), fr[t1], ls);
+        bs = __fmaf_rn(static_cast<float>(ph[0]), fv[t0], bs);
+        bs = __fmaf_rn(static_cast<float>(ph[1]), fv[t1], bs);
+      }
     }
+    if constexpr (BITS == 4) {
+      l = __fmaf_rn(16.0f, l16, l);
+      bsum = __fmaf_rn(16.0f, b16, bsum);
+    }
+    const v8h pf[2] = {operand(pw[0], pw[1], pw[2], pw[3]), operand(pw[4], pw[5], pw[6], pw[7])};
     typedef __attribute__((address_space(3))) v2i* lds_v2i;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
