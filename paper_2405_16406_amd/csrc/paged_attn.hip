@@ -76,7 +76,7 @@ constexpr int paged_lds() {
 }
 
 template <int BITS, bool P16>
-__global__ void __launch_bounds__(64 * kWaves)
+__global__ void __launch_bounds__(64 * kWaves, BITS == 4 ? 3 : 2)
 attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, uint32_t magic_chunks, uint32_t magic_tiles,
                 uint32_t magic_heads, PagedAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -387,26 +387,64 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
   }
 }
 
-// One wave per (sequence, query head): the chunks that its length reaches, in chunk order.
-__global__ void __launch_bounds__(64)
+// One workgroup per (sequence, query head) over the chunks that its length reaches: wave w adds the
+// chunks w, w + kJoin, ..., then the waves' sums are added in their order.
+constexpr int kJoin = 8;
+__global__ void __launch_bounds__(64 * kJoin)
 attn_paged_combine(const float* part, const int32_t* lens, uint16_t* out, int64_t ldo, int hq, int chunks, int chunk_tokens,
                    int max_len, uint32_t magic_hq) {
-  const int lane = threadIdx.x;
+  __shared__ float red_m[kJoin], red_l[kJoin];
+  __shared__ float2 red_d[kJoin][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   uint32_t b, h;
   div_rem(blockIdx.x, hq, magic_hq, b, h);
   const int len = min(max(lens[b], 0), max_len);
   const int n = max(1, (len + chunk_tokens - 1) / chunk_tokens);  // chunk 0 is always written
   const float* pr = part + (b * static_cast<int64_t>(hq) + h) * chunks * kAttnPart;
-  float M = -INFINITY;
-  for (int c = lane; c < n; c += 64) M = fmaxf(M, pr[static_cast<int64_t>(c) * kAttnPart]);
-  M = wave_max(M);
-  float L = 0.0f, D0 = 0.0f, D1 = 0.0f;
-#pragma unroll 8
-  for (int c = 0; c < n; ++c) {
-    const float* p = pr + static_cast<int64_t>(c) * kAttnPart;
-    const float f = rescale(p[0], M);
-    const float2 d = reinterpret_cast<const float2*>(p + 4)[lane];
-    L = __fmaf_rn(p[1], f, L);
+  float M = -INFINITY, L = 0.0f, D0 = 0.0f, D1 = 0.0f;
+  constexpr int kAhead = 8;  // chunks whose loads are in flight together
+  for (int c0 = w; c0 < n; c0 += kJoin * kAhead) {
+    float2 ml[kAhead], d[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {  // a chunk past the last is the last again, with weight 0
+      const float* p = pr + static_cast<int64_t>(min(c0 + kJoin * x, n - 1)) * kAttnPart;
+      ml[x] = *reinterpret_cast<const float2*>(p);
+      d[x] = reinterpret_cast<const float2*>(p + 4)[lane];
+    }
+    float top = M;
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      if (c0 + kJoin * x >= n) ml[x].x = -INFINITY;
+      top = fmaxf(top, ml[x].x);
+    }
+    const float f0 = rescale(M, top);
+    L *= f0;
+    D0 *= f0;
+    D1 *= f0;
+    M = top;
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const float f = rescale(ml[x].x, M);
+      L = __fmaf_rn(ml[x].y, f, L);
+      D0 = __fmaf_rn(d[x].x, f, D0);
+      D1 = __fmaf_rn(d[x].y, f, D1);
+    }
+  }
+  red_d[w][lane] = make_float2(D0, D1);
+  if (lane == 0) {
+    red_m[w] = M;
+    red_l[w] = L;
+  }
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int v = 0; v < kJoin; ++v) M = fmaxf(M, red_m[v]);
+  L = D0 = D1 = 0.0f;
+#pragma unroll
+  for (int v = 0; v < kJoin; ++v) {
+    const float f = rescale(red_m[v], M);
+    const float2 d = red_d[v][lane];
+    L = __fmaf_rn(red_l[v], f, L);
     D0 = __fmaf_rn(d.x, f, D0);
     D1 = __fmaf_rn(d.y, f, D1);
   }
@@ -436,7 +474,7 @@ hipError_t launch_attn_paged(const PagedAttnArgs& a, hipStream_t stream) {
   else
     e = a.param16 ? launch_part<4, true>(a, stream) : launch_part<4, false>(a, stream);
   if (e != hipSuccess || a.chunks == 1) return e;
-  return launch(attn_paged_combine, dim3(static_cast<unsigned>(a.B * a.hq)), dim3(64), 0, stream, a.part, a.lens, a.out, a.ldo,
+  return launch(attn_paged_combine, dim3(static_cast<unsigned>(a.B * a.hq)), dim3(64 * kJoin), 0, stream, a.part, a.lens, a.out, a.ldo,
                 a.hq, a.chunks, a.chunk_tokens, a.max_len, div_magic(static_cast<uint32_t>(a.hq)));
 }
 
