@@ -45,15 +45,6 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // 2^(a - b), 0 when a is -inf (an empty state)
 __device__ __forceinline__ float rescale(float a, float b) { return a == -INFINITY ? 0.0f : exp2_fast(__fsub_rn(a, b)); }
 
-// maximum / sum over the four lanes with the same lane % 16
-template <typename Op>
-__device__ __forceinline__ float groups_all(float v, Op op) {
-  const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = op(__uint_as_float(s16[0]), __uint_as_float(s16[1]));
-  const auto s32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return op(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
-}
-
 __device__ __forceinline__ v8h operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(v8h, v4u{a, b, c, d});
 }
@@ -114,7 +105,7 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
 #pragma unroll
       for (int y = 0; y < 4; ++y)
         qsum += h2f(static_cast<uint16_t>(raw[x][y])) + h2f(static_cast<uint16_t>(raw[x][y] >> 16));
-    qsum = groups_all(qsum, [](float u, float v) { return __fadd_rn(u, v); });
+    qsum = rows_all(qsum, [](float u, float v) { return __fadd_rn(u, v); });
     if constexpr (BITS == 4) {
       // word x holds dims 8 x ..: even products take (0, 4), (2, 6), odd ones (1, 5), (3, 7)
 #pragma unroll
@@ -260,7 +251,7 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
         top = fmaxf(top, s[4 * j + r]);
       }
     }
-    top = groups_all(top, [](float u, float v) { return fmaxf(u, v); });
+    top = rows_all(top, [](float u, float v) { return fmaxf(u, v); });
     if (__ballot(top > m + kSlack)) {  // (m = -inf: any token)
       const float mn = fmaxf(m, top);
       const float f = rescale(m, mn);
@@ -335,8 +326,8 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
     asm volatile("" ::: "memory");
   }
   const auto add = [](float u, float v) { return __fadd_rn(u, v); };
-  l = groups_all(l, add);
-  bsum = groups_all(bsum, add);
+  l = rows_all(l, add);
+  bsum = rows_all(bsum, add);
 
   // the waves' states of each head meet in LDS: dims finished but for the division
   __syncthreads();

@@ -3,10 +3,12 @@
 // rope_kv_write: rotary positions on queries and keys, R3 of both (Sec. 3.1), eq. 1 codes of keys
 // and values into the pages.  With position p and pair frequency f_i, the pair (u, w) of dims
 // becomes (u c - w s, w c + u s), c = m cos(p f_i), s = m sin(p f_i); then y = x S_128 / sqrt(128).
-//   * Four lanes (a quad) own a head vector; lane j holds the elements 32 k + 8 j + e, so that a
-//     16-byte load or store of the wave covers whole 64-byte lines.  A wave's 16 vectors are all
-//     queries, all keys or all values (a `task`): keys cost three times a query.
-//   * A workgroup covers TB tokens and computes their angles once for all heads: 64 lanes, one
+//   * Queries and values: four lanes (a quad) own a head vector; lane j holds the elements
+//     32 k + 8 j + e, so that a 16-byte load or store of the wave covers whole 64-byte lines, and a
+//     wave has 16 vectors.  Keys: eight lanes own one, so that its 64-bit values take 32 registers
+//     of a lane; the wave has eight.  A wave's vectors are all queries, all keys or all values (a
+//     task), and it asks for the first ones before it knows their positions.
+//   * A workgroup covers a few tokens and computes their angles once for all heads: 64 lanes, one
 //     frequency each, in 64 bits (p f of a far position has no fraction left in 32), reduced to
 //     turns so that sin and cos see at most half a turn.  They go through LDS.
 //   * Queries are rotated in 32 bits (the result is fp16).  Keys are rotated in 64: adds and fmas
@@ -23,13 +25,8 @@ namespace sq {
 namespace {
 
 constexpr int kD = 128;
-constexpr float kInvSqrtD = 0.08838834764831845f;
+constexpr double kInvSqrtD = 0.088388347648318440550;
 
-// the lane's four 16-byte chunks of a head vector: chunk k holds elements 32 k + 8 j .. + 7
-__device__ __forceinline__ void load_chunks(const uint16_t* v, int j, v4u (&raw)[4]) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) raw[k] = *reinterpret_cast<const v4u*>(v + 32 * k + 8 * j);
-}
 template <typename F>
 __device__ __forceinline__ void widen8(const v4u& raw, F* e) {
 #pragma unroll
@@ -38,6 +35,16 @@ __device__ __forceinline__ void widen8(const v4u& raw, F* e) {
     e[2 * i + 1] = static_cast<F>(h2f(static_cast<uint16_t>(raw[i] >> 16)));
   }
 }
+
+// Waves' worth of vectors of n tokens: 16 queries, 8 keys or 16 values each.
+struct RopeTasks {
+  int q, k, v;
+  __host__ __device__ int all() const { return q + k + v; }
+};
+__host__ __device__ inline RopeTasks rope_tasks(int n, int hq, int hkv) {
+  return {(n * hq + 15) / 16, (n * hkv + 7) / 8, (n * hkv + 15) / 16};
+}
+constexpr int kRopeWaves = 8;  // of a workgroup at most
 
 // How the pairs of a head vector lie in the lanes' registers.
 enum RopeForm {
@@ -48,27 +55,36 @@ enum RopeForm {
   kInterleaved,  // dims (2 i, 2 i + 1)
 };
 
-// e: the lane's elements; tab: (cos, sin) per frequency; vec: the vector in memory
-template <int FORM, typename F, typename F2>
-__device__ __forceinline__ void rotate_pairs(F (&e)[32], int j, const F2* tab, int rotary, const uint16_t* vec) {
+// Turns the pairs of a vector and scales it by 1 / sqrt(128), R3's factor, which the (cos, sin) of
+// tab hold already.  e: the lane's elements, N chunks of 8, chunk k being chunk(k) of the vector's
+// 16; vec: the vector in memory
+template <int FORM, int N, typename F, typename F2, typename C>
+__device__ __forceinline__ void rotate_pairs(F (&e)[8 * N], C chunk, const F2* tab, int rotary, const uint16_t* vec) {
+  if constexpr (FORM != kHalf128) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (FORM == kNoRope || 8 * chunk(k) >= rotary)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) e[8 * k + x] *= static_cast<F>(kInvSqrtD);
+  }
   auto turn = [&](int a, int b, const F2& cs) {
     const F u = e[a], w = e[b];
     e[a] = fma(u, cs.x, -(w * cs.y));
     e[b] = fma(w, cs.x, u * cs.y);
   };
-  if constexpr (FORM == kHalf128) {
+  if constexpr (FORM == kHalf128) {  // chunks k and k + N / 2
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < N / 2; ++k)
 #pragma unroll
-      for (int x = 0; x < 8; ++x) turn(8 * k + x, 8 * (k + 2) + x, tab[8 * (4 * k + j) + x]);
-  } else if constexpr (FORM == kHalf64) {
+      for (int x = 0; x < 8; ++x) turn(8 * k + x, 8 * (k + N / 2) + x, tab[8 * chunk(k) + x]);
+  } else if constexpr (FORM == kHalf64 && N == 4) {  // chunks 0 and 1
 #pragma unroll
-    for (int x = 0; x < 8; ++x) turn(x, 8 + x, tab[8 * j + x]);
-  } else if constexpr (FORM == kHalfAny) {
+    for (int x = 0; x < 8; ++x) turn(x, 8 + x, tab[8 * chunk(0) + x]);
+  } else if constexpr (FORM == kHalf64 || FORM == kHalfAny) {
     const int hc = rotary / 16;  // chunks of a half
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int c = 4 * k + j;
+    for (int k = 0; k < N; ++k) {
+      const int c = chunk(k);
       if (c < 2 * hc) {
         const int f = c < hc ? c : c - hc;
         F p[8];
@@ -83,39 +99,38 @@ __device__ __forceinline__ void rotate_pairs(F (&e)[32], int j, const F2* tab, i
     }
   } else if constexpr (FORM == kInterleaved) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (8 * (4 * k + j) < rotary)
+    for (int k = 0; k < N; ++k)
+      if (8 * chunk(k) < rotary)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) turn(8 * k + 2 * i, 8 * k + 2 * i + 1, tab[4 * (4 * k + j) + i]);
+        for (int i = 0; i < 4; ++i) turn(8 * k + 2 * i, 8 * k + 2 * i + 1, tab[4 * chunk(k) + i]);
   }
 }
 
-__device__ __forceinline__ void store_half(uint16_t* v, int j, const float (&e)[32], float scale) {
+template <int N, typename C>
+__device__ __forceinline__ void store_half(uint16_t* v, C chunk, const float (&e)[8 * N]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < N; ++k) {
     v4u o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = f2h2(__fmul_rn(e[8 * k + 2 * i], scale), __fmul_rn(e[8 * k + 2 * i + 1], scale));
-    *reinterpret_cast<v4u*>(v + 32 * k + 8 * j) = o;
+    for (int i = 0; i < 4; ++i) o[i] = f2h2(e[8 * k + 2 * i], e[8 * k + 2 * i + 1]);
+    *reinterpret_cast<v4u*>(v + 8 * chunk(k)) = o;
   }
 }
 
-// Eq. 1 of the quad's vector in its 32-bit steps (sq_device.h), range clipped by `clip`; codes to
-// cq, the pair (alpha, beta) to ab (fp32, or rounded to fp16 with the codes taken from the rounded
-// pair, P16).
-template <int BITS, bool P16>
-__device__ __forceinline__ void quantize(const float (&e)[32], int j, float clip, uint8_t* cq, void* ab) {
+// Eq. 1 of a vector in its 32-bit steps (sq_device.h), range clipped by `clip`; codes to cq, the
+// pair (alpha, beta) to ab by the lane `first` (fp32, or rounded to fp16 with the codes taken from
+// the rounded pair, P16).  all(v, op): op over the vector's lanes.
+template <int BITS, bool P16, int N, typename C, typename R>
+__device__ __forceinline__ void quantize(const float (&e)[8 * N], C chunk, R all, bool first, float clip, uint8_t* cq, void* ab) {
   constexpr float kL = BITS == 8 ? 255.0f : 15.0f;
   float mn = e[0], mx = e[0];
 #pragma unroll
-  for (int r = 1; r < 32; ++r) {
+  for (int r = 1; r < 8 * N; ++r) {
     mn = fminf(mn, e[r]);
     mx = fmaxf(mx, e[r]);
   }
-  mn = fminf(mn, quad_swap<1>(mn));
-  mx = fmaxf(mx, quad_swap<1>(mx));
-  mn = __fmul_rn(fminf(mn, quad_swap<2>(mn)), clip);
-  mx = __fmul_rn(fmaxf(mx, quad_swap<2>(mx)), clip);
+  mn = __fmul_rn(all(mn, [](float u, float v) { return fminf(u, v); }), clip);
+  mx = __fmul_rn(all(mx, [](float u, float v) { return fmaxf(u, v); }), clip);
   float alpha = __fdiv_rn(__fsub_rn(mx, mn), kL), beta = mn;
   if (alpha < kMinNormal) alpha = 1.0f;
   if constexpr (P16) {
@@ -124,28 +139,74 @@ __device__ __forceinline__ void quantize(const float (&e)[32], int j, float clip
     const uint16_t b16 = f2h_sat(beta);
     alpha = h2f(a16);
     beta = h2f(b16);
-    if (j == 0) *static_cast<uint32_t*>(ab) = a16 | (static_cast<uint32_t>(b16) << 16);
+    if (first) *static_cast<uint32_t*>(ab) = a16 | (static_cast<uint32_t>(b16) << 16);
   } else {
-    if (j == 0) *static_cast<float2*>(ab) = make_float2(alpha, beta);
+    if (first) *static_cast<float2*>(ab) = make_float2(alpha, beta);
   }
   const float inv = __fdiv_rn(1.0f, alpha);
-  auto arg = [&](int r) { return __builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(e[r], beta), inv), 0.0f, kL); };
+  // Codes above the top appear only where the range is clipped or its parameters are rounded;
+  // v_cvt_pk_u8_f32 (which rounds half to even) itself ends at 0 and 255.
+  const auto store = [&](auto cc) __attribute__((always_inline)) {
+    auto arg = [&](int r) {
+      const float t = __fmul_rn(__fsub_rn(e[r], beta), inv);
+      return decltype(cc)::value ? __builtin_amdgcn_fmed3f(t, 0.0f, kL) : t;
+    };
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if constexpr (BITS == 8) {
-      uint32_t w[2] = {0u, 0u};
+    for (int k = 0; k < N; ++k) {
+      if constexpr (BITS == 8) {
+        uint32_t w[2] = {0u, 0u};
 #pragma unroll
-      for (int x = 0; x < 8; ++x) w[x >> 2] = __builtin_amdgcn_cvt_pk_u8_f32(arg(8 * k + x), x & 3, w[x >> 2]);
-      *reinterpret_cast<uint2*>(cq + 32 * k + 8 * j) = make_uint2(w[0], w[1]);
-    } else {
-      uint32_t ev = 0, od = 0;  // v_cvt_pk_u8_f32 rounds half to even
+        for (int x = 0; x < 8; ++x) w[x >> 2] = __builtin_amdgcn_cvt_pk_u8_f32(arg(8 * k + x), x & 3, w[x >> 2]);
+        *reinterpret_cast<uint2*>(cq + 8 * chunk(k)) = make_uint2(w[0], w[1]);
+      } else {
+        uint32_t ev = 0, od = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ev = __builtin_amdgcn_cvt_pk_u8_f32(arg(8 * k + 2 * i), i, ev);
-        od = __builtin_amdgcn_cvt_pk_u8_f32(arg(8 * k + 2 * i + 1), i, od);
+        for (int i = 0; i < 4; ++i) {
+          ev = __builtin_amdgcn_cvt_pk_u8_f32(arg(8 * k + 2 * i), i, ev);
+          od = __builtin_amdgcn_cvt_pk_u8_f32(arg(8 * k + 2 * i + 1), i, od);
+        }
+        *reinterpret_cast<uint32_t*>(cq + 4 * chunk(k)) = ev | (od << 4);
       }
-      *reinterpret_cast<uint32_t*>(cq + 16 * k + 4 * j) = ev | (od << 4);
     }
+  };
+  if (BITS == 4 && (P16 || clip != 1.0f))
+    store(std::true_type{});
+  else
+    store(std::false_type{});
+}
+
+// The eight lanes of a key vector: lane bits 0, 4 and 5.  Loaded chunk k is 8 k + key_lane.
+__device__ __forceinline__ int key_lane(int lane) { return (lane & 1) | ((lane >> 3) & 6); }
+
+// Unscaled 128-point transform of the eight lanes' values (register 8 k + x: dim 64 k + 8 key_lane +
+// x).  The lane bits 5 and 4 are first exchanged with the register bit k, so that their butterflies
+// stay in the lane; the result's register 8 k + x is dim 64 b5 + 32 b4 + 16 k + 8 b0 + x.
+__device__ __forceinline__ void key_fwht(double (&e)[16], int lane) {
+#pragma unroll
+  for (int h = 1; h < 16; h <<= 1)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if ((r & h) == 0) {
+        const double u = e[r], w = e[r + h];
+        e[r] = u + w;
+        e[r + h] = u - w;
+      }
+  const double s1 = (lane & 1) ? -1.0 : 1.0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) e[r] = fma(s1, e[r], quad_swap<1>(e[r]));
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    swap_halves(e[r], e[r + 8]);
+    const double u = e[r], w = e[r + 8];
+    e[r] = u + w;
+    e[r + 8] = u - w;
+  }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    swap_rows(e[r], e[r + 8]);
+    const double u = e[r], w = e[r + 8];
+    e[r] = u + w;
+    e[r + 8] = u - w;
   }
 }
 
@@ -156,7 +217,7 @@ struct TokenPlace {
 };
 
 template <int BITS, bool P16, int FORM>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(64 * kRopeWaves, 3)
 rope_kv_write(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* cu, const int32_t* lens,
               int64_t t_first, RopeWriteArgs a) {
   __shared__ double2 cs[kRopeTokens][64];
@@ -165,83 +226,107 @@ rope_kv_write(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6;
-  const int j = lane & 3;
   const int64_t t0 = t_first + static_cast<int64_t>(blockIdx.x) * a.tokens;
-  const int nq = (a.tokens * a.hq + 15) / 16, nk = (a.tokens * a.cache.heads + 15) / 16;
+  const RopeTasks tasks = rope_tasks(a.tokens, a.hq, a.cache.heads);
+  enum { kQuery, kKey, kValue };
+
+  // A lane's vector of a task: token tt of the workgroup (-1: none), head h, its row in memory, and
+  // the lane's chunks of it.
+  struct Item {
+    int kind, tt;
+    uint32_t h;
+    const uint16_t* vec;
+    v4u raw[4];
+  };
+  auto fetch = [&](int task, Item& it) __attribute__((always_inline)) {
+    it.kind = task < tasks.q ? kQuery : task < tasks.q + tasks.k ? kKey : kValue;
+    const int heads = it.kind == kQuery ? a.hq : a.cache.heads;
+    const int x = it.kind == kQuery ? task * 16 + (lane >> 2)
+                  : it.kind == kKey ? (task - tasks.q) * 8 + ((lane >> 1) & 7)
+                                    : (task - tasks.q - tasks.k) * 16 + (lane >> 2);
+    uint32_t tt;
+    div_rem(x, heads, it.kind == kQuery ? a.magic_hq : a.magic_hkv, tt, it.h);
+    it.tt = static_cast<int>(tt) < a.tokens && t0 + tt < a.T ? static_cast<int>(tt) : -1;
+    const int64_t t = t0 + max(it.tt, 0);
+    it.vec = (it.kind == kQuery ? q + t * a.ldq : it.kind == kKey ? k + t * a.ldk : v + t * a.ldv) + it.h * kD;
+    const int first = it.kind == kKey ? key_lane(lane) : lane & 3, step = it.kind == kKey ? 8 : 4;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (c < 2 || it.kind != kKey) it.raw[c] = *reinterpret_cast<const v4u*>(it.vec + 8 * (first + step * c));
+  };
+  Item it, next;
+  if (wave < tasks.all()) fetch(wave, it);
 
   // positions, pages and angles: wave w takes the tokens w, w + waves, ...
   for (int tt = wave; tt < a.tokens; tt += waves) {
     const int64_t t = t0 + tt;
     RowSeq s{-1, 0, 0};
+    double f = 0.0;
+    if constexpr (FORM != kNoRope)
+      if (lane < a.rotary / 2) f = a.freq[lane];
     if (t < a.T) {
       if (cu)
-        s = find_sequence(cu, a.B, t);
+        s = find_sequence(cu, lens, a.B, t);
       else
-        s = RowSeq{static_cast<int>(t), static_cast<int>(t), static_cast<int>(t) + 1};
+        s = RowSeq{static_cast<int>(t), static_cast<int>(t) + 1, lens[t]};
     }
-    int64_t pos = -1;
-    if (s.seq >= 0) pos = row_position(lens[s.seq], s.end, t);
+    const int64_t pos = s.seq >= 0 ? row_position(s.len, s.end, t) : -1;
+    int32_t entry = -1;
+    const int32_t col = table_column(a.cache, pos);
+    if (col >= 0) entry = a.cache.table[s.seq * a.cache.ldt + col];
     if constexpr (FORM != kNoRope) {
-      if (lane < a.rotary / 2) {
-        const double turns = static_cast<double>(pos) * (a.freq[lane] * 0.15915494309189533577);
-        double sn, cn;
-        sincospi(2.0 * (turns - rint(turns)), &sn, &cn);
-        const double m = static_cast<double>(a.magnitude);
-        cs[tt][lane] = make_double2(m * cn, m * sn);
-        csf[tt][lane] = make_float2(static_cast<float>(m * cn), static_cast<float>(m * sn));
-      }
+      const double turns = static_cast<double>(pos) * (f * 0.15915494309189533577);
+      double sn, cn;
+      sincospi(2.0 * (turns - rint(turns)), &sn, &cn);
+      const double m = static_cast<double>(a.magnitude) * kInvSqrtD;
+      cs[tt][lane] = make_double2(m * cn, m * sn);
+      csf[tt][lane] = make_float2(static_cast<float>(m * cn), static_cast<float>(m * sn));
     }
-    if (lane == 0) {
-      int32_t page = -1;
-      if (pos >= 0) {
-        const int32_t col = table_column(a.cache, pos);
-        if (col >= 0) page = valid_page(a.cache, a.cache.table[s.seq * a.cache.ldt + col]);
-      }
-      place[tt] = {pos, page};
-    }
+    if (lane == 0) place[tt] = {pos, valid_page(a.cache, entry)};
   }
   __syncthreads();
 
-  for (int task = wave; task < nq + 2 * nk; task += waves) {
-    const int kind = task < nq ? 0 : task < nq + nk ? 1 : 2;  // queries, keys, values
-    const int heads = kind == 0 ? a.hq : a.cache.heads;
-    uint32_t tt, h;
-    div_rem((task - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * 16 + lane / 4, heads, kind == 0 ? a.magic_hq : a.magic_hkv,
-            tt, h);
-    if (static_cast<int>(tt) >= a.tokens || t0 + tt >= a.T) continue;  // the quad's lanes leave together
-    const TokenPlace pl = place[tt];
+  for (int task = wave; task < tasks.all(); task += waves) {
+    if (task != wave) it = next;
+    if (task + waves < tasks.all()) fetch(task + waves, next);  // while this one is worked on
+    if (it.tt < 0) continue;  // a vector's lanes leave together
+    const TokenPlace pl = place[it.tt];
     if (pl.pos < 0) continue;
-    const int64_t t = t0 + tt;
-    const uint16_t* vec = (kind == 0 ? q + t * a.ldq : kind == 1 ? k + t * a.ldk : v + t * a.ldv) + h * kD;
-    const int64_t slot = pl.page >= 0 ? token_slot(a.cache, pl.page, h, pl.pos) : -1;
-    v4u raw[4];
-    load_chunks(vec, j, raw);
-    float e[32];
-    if (kind == 0) {
+    const int64_t t = t0 + it.tt;
+    const int64_t slot = token_slot(a.cache, pl.page, it.h, pl.pos);
+    const auto quad_chunk = [&](int c) { return 4 * c + (lane & 3); };
+    const auto quad_all = [](float x, auto op) {
+      x = op(x, quad_swap<1>(x));
+      return op(x, quad_swap<2>(x));
+    };
+    if (it.kind == kKey) {
+      double d[16];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) widen8(raw[c], e + 8 * c);
-      rotate_pairs<FORM>(e, j, csf[tt], a.rotary, vec);
-      quad_fwht(e, j);
-      store_half(a.q_rot + (t * a.hq + h) * kD, j, e, kInvSqrtD);
+      for (int c = 0; c < 2; ++c) widen8(it.raw[c], d + 8 * c);
+      rotate_pairs<FORM, 2>(d, [&](int c) { return 8 * c + key_lane(lane); }, cs[it.tt], a.rotary, it.vec);
+      key_fwht(d, lane);
+      const auto chunk = [&](int c) { return (lane & 1) + 2 * c + ((lane >> 2) & 12); };
+      float e[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) e[r] = static_cast<float>(d[r]);
+      if (a.k_rot) store_half<2>(a.k_rot + (t * a.cache.heads + it.h) * kD, chunk, e);
+      if (pl.page < 0) continue;
+      const auto all = [](float x, auto op) { return rows_all(op(x, quad_swap<1>(x)), op); };
+      void* ab = static_cast<uint8_t*>(a.cache.params) + 4 * slot * (P16 ? 2 : 4);
+      quantize<BITS, P16, 2>(e, chunk, all, (lane & 49) == 0, a.k_clip, a.cache.kq + slot * (kD * BITS / 8), ab);
       continue;
     }
-    if (kind == 1) {
-      double d[32];
+    float e[32];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) widen8(raw[c], d + 8 * c);
-      rotate_pairs<FORM>(d, j, cs[tt], a.rotary, vec);
-      quad_fwht(d, j);
-#pragma unroll
-      for (int r = 0; r < 32; ++r) e[r] = static_cast<float>(d[r] * 0.088388347648318440550);
-      if (a.k_rot) store_half(a.k_rot + (t * a.cache.heads + h) * kD, j, e, 1.0f);
-    } else {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) widen8(raw[c], e + 8 * c);
+    for (int c = 0; c < 4; ++c) widen8(it.raw[c], e + 8 * c);
+    if (it.kind == kQuery) {
+      rotate_pairs<FORM, 4>(e, quad_chunk, csf[it.tt], a.rotary, it.vec);
+      quad_fwht(e, lane & 3);
+      store_half<4>(a.q_rot + (t * a.hq + it.h) * kD, quad_chunk, e);
+    } else if (pl.page >= 0) {
+      void* ab = static_cast<uint8_t*>(a.cache.params) + (4 * slot + 2) * (P16 ? 2 : 4);
+      quantize<BITS, P16, 4>(e, quad_chunk, quad_all, (lane & 3) == 0, a.v_clip, a.cache.vq + slot * (kD * BITS / 8), ab);
     }
-    if (slot < 0) continue;
-    uint8_t* codes = (kind == 1 ? a.cache.kq : a.cache.vq) + slot * (kD * BITS / 8);
-    void* ab = static_cast<uint8_t*>(a.cache.params) + (4 * slot + 2 * (kind - 1)) * (P16 ? 2 : 4);
-    quantize<BITS, P16>(e, j, kind == 1 ? a.k_clip : a.v_clip, codes, ab);
   }
 }
 
@@ -256,11 +341,11 @@ kv_read(const int32_t* cu, const int32_t* lens, int64_t t_first, KvReadArgs a) {
   for (int tt = wave; tt < a.tokens; tt += 4) {
     const int64_t t = t0 + tt;
     RowSeq s{-1, 0, 0};
-    if (t < a.T) s = find_sequence(cu, a.B, t);
+    if (t < a.T) s = find_sequence(cu, lens, a.B, t);
     if (lane == 0) {
       int64_t pos = -1;
       int32_t page = -1;
-      if (s.seq >= 0) pos = row_position(lens[s.seq], s.end, t);
+      if (s.seq >= 0) pos = row_position(s.len, s.end, t);
       if (pos >= 0) {
         const int32_t col = table_column(a.cache, pos);
         if (col >= 0) page = valid_page(a.cache, a.cache.table[s.seq * a.cache.ldt + col]);
@@ -289,6 +374,10 @@ kv_read(const int32_t* cu, const int32_t* lens, int64_t t_first, KvReadArgs a) {
         const float4 p = static_cast<const float4*>(a.cache.params)[slot];
         ab[0] = p.x, ab[1] = p.y, ab[2] = p.z, ab[3] = p.w;
       }
+      if constexpr (PLAIN) {
+        ab[0] = __fmul_rn(ab[0], static_cast<float>(kInvSqrtD));
+        ab[1] = __fmul_rn(ab[1], static_cast<float>(kInvSqrtD));
+      }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const uint8_t* codes = (s ? a.cache.vq : a.cache.kq) + slot * (kD * BITS / 8);
@@ -311,22 +400,28 @@ kv_read(const int32_t* cu, const int32_t* lens, int64_t t_first, KvReadArgs a) {
 #pragma unroll
       for (int r = 0; r < 32; ++r) e[0][r] = e[1][r] = 0.0f;
     }
-    if constexpr (PLAIN) quad_fwht(e[0], j);
-    store_half(a.k + t * a.ldk + h * kD, j, e[0], PLAIN ? kInvSqrtD : 1.0f);
-    store_half(a.v + t * a.ldv + h * kD, j, e[1], 1.0f);
+    if constexpr (PLAIN) quad_fwht(e[0], j);  // its 1 / sqrt(128) is in the parameters
+    const auto chunk = [&](int c) { return 4 * c + j; };
+    store_half<4>(a.k + t * a.ldk + h * kD, chunk, e[0]);
+    store_half<4>(a.v + t * a.ldv + h * kD, chunk, e[1]);
   }
 }
 
 }  // namespace
 
 hipError_t launch_rope_kv_write(RopeWriteArgs a, hipStream_t stream) {
-  // Tokens of a workgroup: as many as give each of its (at most 16) waves one task of 16 vectors.
+  // Many rows: workgroups of four waves with up to four tasks each, the next one's vectors on their
+  // way while one is worked on, as long as 1024 of them (four a CU) are left.  Few rows (a decode
+  // step): a wave for each task, for the shortest way through.  Measured, us with the read back:
+  // 17034 rows of 32 + 32 heads 237 (four waves of four tasks), 241 (eight of four), 284 (sixteen
+  // of one).
+  constexpr int kMany = 1024, kLoop = 4;
+  const auto tasks_of = [&](int n) { return rope_tasks(n, a.hq, a.cache.heads).all(); };
   int tokens = 1;
-  const auto tasks_of = [&](int n) { return (n * a.hq + 15) / 16 + 2 * ((n * a.cache.heads + 15) / 16); };
-  while (tokens < kRopeTokens && tokens < a.T && tasks_of(2 * tokens) <= 16) tokens *= 2;
+  while (2 * tokens <= kRopeTokens && a.T >= 2 * tokens * kMany && tasks_of(2 * tokens) <= kLoop * kLoop) tokens *= 2;
   a.tokens = tokens;
-  const int tasks = tasks_of(tokens);
-  const int threads = 64 * (tasks < 16 ? tasks : 16);
+  const int most = a.T >= kMany ? kLoop : kRopeWaves, tasks = tasks_of(tokens);
+  const int threads = 64 * (tasks < most ? tasks : most);
   a.magic_hq = div_magic(static_cast<uint32_t>(a.hq));
   a.magic_hkv = div_magic(static_cast<uint32_t>(a.cache.heads));
   const int form = a.rotary == 0 ? kNoRope : a.interleaved ? kInterleaved : a.rotary == 128 ? kHalf128 : a.rotary == 64 ? kHalf64 : kHalfAny;

@@ -443,7 +443,7 @@ attn_prompt_combine(const float* part, const int32_t* cu_q, int64_t B, int hq, i
   const int lane = threadIdx.x;
   uint32_t t, head;
   div_rem(blockIdx.x, hq, magic_hq, t, head);
-  if (find_sequence(cu_q, B, t).seq < 0) return;  // a row of no sequence is left as it was
+  if (find_sequence(cu_q, cu_q, B, t).seq < 0) return;  // a row of no sequence is left as it was
   const float* pr = part + static_cast<int64_t>(blockIdx.x) * splits * kAttnPart;
   float M = -INFINITY;
   for (int s = lane; s < splits; s += 64) M = fmaxf(M, pr[static_cast<int64_t>(s) * kAttnPart]);
