@@ -182,17 +182,34 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   };
 
   // LDS reads: K row `col` of each half tile, chunk 2 s + h; V: lane (i, gi) of 16 reads 8 bytes of
-  // row 4 h + i / 4 (+ 8), dims 32 dt + 16 (gi % 2) + 4 (i % 4) .. and gets dim 32 dt + col of four keys
-  const int ksw = swizzle(col);
-  const int vrow = 4 * h + ((lane & 15) >> 2), vlow = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), vsub = 8 * (lane & 1);
-  auto v_read = [&](int buf, int ks, int dt, int second) __attribute__((always_inline)) -> v4s {
-    const int t = vrow + 8 * second;
-    const int off = (2 + buf) * kTileBytes + ks * 16 * 256 + t * 256 + 16 * ((4 * dt + vlow) ^ swizzle(t)) + vsub;
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(lds + off));
+  // row 4 h + i / 4 (+ 8), dims 32 dt + 16 (gi % 2) + 4 (i % 4) .. and gets dim 32 dt + col of four
+  // keys.  The lane's 16 addresses stay in registers; buffer, half tile and key step are offsets of
+  // the instructions.
+  uint32_t kadr[8], vadr[4][2];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) kadr[x] = col * 256 + 16 * ((2 * x + h) ^ swizzle(col));
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int second = 0; second < 2; ++second) {
+      const int t = 4 * h + ((lane & 15) >> 2) + 8 * second;
+      const int c = 4 * dt + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      vadr[dt][second] = t * 256 + 16 * (c ^ swizzle(t)) + 8 * (lane & 1);
+    }
+#pragma unroll
+  for (int x = 0; x < 8; ++x) asm("" : "+v"(kadr[x]), "+v"(vadr[x >> 1][x & 1]));  // not derived from each other
+  typedef __attribute__((address_space(3))) uint8_t* lds_bytes;
+  const lds_bytes lds3 = (lds_bytes)(uintptr_t)lds;
+  auto k_operand = [&](int buf, int mt, int x) __attribute__((always_inline)) -> v8h {
+    return *(__attribute__((address_space(3))) const v8h*)(lds3 + kadr[x] + (buf * kTileBytes + mt * 32 * 256));
   };
   auto v_operand = [&](int buf, int ks, int dt) __attribute__((always_inline)) -> v8h {
-    const v4s x = v_read(buf, ks, dt, 0), y = v_read(buf, ks, dt, 1);
-    return __builtin_bit_cast(v8h, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    v4s x[2];
+#pragma unroll
+    for (int second = 0; second < 2; ++second)
+      x[second] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) v4s*)(lds3 + vadr[dt][second] + ((2 + buf) * kTileBytes + ks * 16 * 256)));
+    return __builtin_bit_cast(v8h, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
 
   float mx = -INFINITY, l = 0.0f;
@@ -212,8 +229,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       for (int r = 0; r < 16; ++r) s[mt][r] = 0.0f;
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
-        const v8h kf = *reinterpret_cast<const v8h*>(lds + buf * kTileBytes + (32 * mt + col) * 256 + 16 * ((2 * x + h) ^ ksw));
-        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[x], s[mt], 0, 0, 0);
+        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_operand(buf, mt, x), qf[x], s[mt], 0, 0, 0);
       }
     }
     pace<16, 1, 4>();
@@ -236,12 +252,14 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[1][r]);
     top = halves(top, [](float x, float y) { return fmaxf(x, y); }) * cs;
-    const float mn = fmaxf(mx, top);
-    const float f = rescale(mx, mn);
-    l *= f;
+    if (__builtin_expect(__ballot(top > mx + kSlack) != 0, 0)) {  // (mx = -inf: any score)
+      const float mn = fmaxf(mx, top);
+      const float f = rescale(mx, mn);
+      l *= f;
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) acc[dt] *= f;
-    mx = mn;
+      for (int dt = 0; dt < 4; ++dt) acc[dt] *= f;
+      mx = mn;
+    }
     const float base = (mx == -INFINITY ? 0.0f : mx) - kWeightBits;
     // the sum is that of the rounded weights: their rounding then moves the mean of the values
     // seen, not its size
@@ -388,14 +406,18 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     softmax(kt0, std::true_type{});
     end_softmax();
     int j = 1;
-    for (; j < nf; ++j) {
-      values(kt0 + j - 1, (j - 1) & 1, std::false_type{});
-      scores(j & 1);
+    const auto whole = [&](int j, int buf) __attribute__((always_inline)) {
+      values(kt0 + j - 1, buf ^ 1, std::false_type{});
+      scores(buf);
       end_products(j);
       softmax(kt0 + j, std::false_type{});
       end_softmax();
+    };
+    for (; j + 1 < nf; j += 2) {
+      whole(j, 1);
+      whole(j + 1, 0);
     }
-    for (; j < nw; ++j) {
+    for (; j < nw; ++j) {  // (and a whole tile left over)
       values(kt0 + j - 1, (j - 1) & 1, std::true_type{});
       scores(j & 1);
       end_products(j);
