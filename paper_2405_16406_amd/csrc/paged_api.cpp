@@ -90,12 +90,12 @@ sq_status check_paged_sizes(int64_t B, int64_t max_len, int64_t Hq, int64_t Hkv,
   return SQ_OK;
 }
 
-sq_status prompt_split_here(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int32_t& splits, uint64_t& bytes) {
+sq_status prompt_plan_here(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, sq::PromptPlan& plan, uint64_t& bytes) {
   int cus = 0;
   const hipError_t e = sq::device_cus(&cus);
   if (e != hipSuccess) return hip_status(e, "compute-unit count of the current device");
-  splits = sq::prompt_splits(B, Tq, Tk, static_cast<int32_t>(Hq), static_cast<int32_t>(Hkv), cus);
-  bytes = splits > 1 ? static_cast<uint64_t>(Tq) * Hq * splits * (sq::kAttnPart * 4) : 0;
+  plan = sq::prompt_plan(B, Tq, Tk, static_cast<int32_t>(Hq), static_cast<int32_t>(Hkv), cus);
+  bytes = plan.splits > 1 ? static_cast<uint64_t>(Tq) * Hq * plan.splits * (sq::kAttnPart * 4) : 0;
   return SQ_OK;
 }
 
@@ -297,9 +297,9 @@ sq_status sq_attn_prompt_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq
   if (!bytes) return fail(SQ_ERR_NULL, "bytes is required");
   sq_status s = check_prompt_sizes(B, Tq, Tk, Hq, Hkv, D);
   if (s != SQ_OK) return s;
-  int32_t splits = 1;
+  sq::PromptPlan plan{};
   uint64_t need = 0;
-  if ((s = prompt_split_here(B, Tq, Tk, Hq, Hkv, splits, need)) != SQ_OK) return s;
+  if ((s = prompt_plan_here(B, Tq, Tk, Hq, Hkv, plan, need)) != SQ_OK) return s;
   *bytes = need;
   return ok();
 }
@@ -324,8 +324,12 @@ sq_status sq_attn_prompt(const void* q, int64_t ldq, const void* k, int64_t ldk,
   if (s != SQ_OK) return s;
   if (Tq == 0 || B == 0) return ok();
   sq::PromptArgs a{};
+  sq::PromptPlan plan{};
   uint64_t need = 0;
-  if ((s = prompt_split_here(B, Tq, Tk, Hq, Hkv, a.splits, need)) != SQ_OK) return s;
+  if ((s = prompt_plan_here(B, Tq, Tk, Hq, Hkv, plan, need)) != SQ_OK) return s;
+  a.half = plan.half;
+  a.splits = plan.splits;
+  a.per = plan.per;
   if ((s = check_workspace(workspace, workspace_bytes, need)) != SQ_OK) return s;
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);

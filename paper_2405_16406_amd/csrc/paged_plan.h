@@ -29,17 +29,48 @@ inline void paged_split(int64_t B, int64_t max_len, int32_t hq, int32_t hkv, int
 constexpr int kPromptRows = 256;  // (token, query head) rows of a prompt workgroup
 constexpr int kPromptTile = 64;   // keys of its step
 
-// Prompts: parts that the keys are split into where the rows do not fill the device, eight steps
-// or more each on an average sequence.
-inline int32_t prompt_splits(int64_t B, int64_t Tq, int64_t Tk, int32_t hq, int32_t hkv, int cus) {
-  if (B < 1) return 1;
+// Prompts.  half: workgroups of half the rows, whose two groups of waves share the keys.  splits > 1:
+// the keys go out in parts of `per` tiles (more where a sequence would have over `splits` of them).
+//   Workgroups of 256 rows for more of them than compute units: they move the fewest bytes through
+//   the caches (prompt of 4096 tokens of 32 heads: 149 us, halves 166; 8192: 522, 571).
+//   Up to one a compute unit, the longest of a causal prompt decides: halves (2048 tokens 54 us,
+//   whole 60; 1024: 25, 36; 512: 18, 26).
+//   Few rows over many keys: parts, a unit each, where by the estimate below they are through
+//   sooner, partial states included (37 and 4 tokens over 16000 and 6000 keys of 8 heads 37 us).
+struct PromptPlan {
+  int32_t half, splits, per;
+};
+
+inline PromptPlan prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int32_t hq, int32_t hkv, int cus) {
+  if (B < 1 || Tq < 1 || Tk < 1) return {0, 1, 0};
   const int64_t tiles = (Tq * (hq / hkv) + kPromptRows - 1) / kPromptRows;
   const int64_t groups = (tiles > B ? tiles : B) * hkv;
-  if (groups >= cus) return 1;
-  int64_t s = cus / groups;
-  const int64_t most = Tk / B / (8 * kPromptTile);
-  if (s > most) s = most;
-  return static_cast<int32_t>(s < 1 ? 1 : s);
+  if (groups > cus) return {0, 1, 0};
+  const int64_t keys = (Tk + kPromptTile - 1) / kPromptTile;
+  // A part of each sequence, row tile and head is half empty on average; four tiles or more.
+  const int64_t work = keys * hkv * ((tiles + B - 1) / B), units = cus - groups / 2;
+  int64_t per = (work + units - 1) / units;
+  if (per < 4) per = 4;
+  int64_t splits = (keys + per - 1) / per;
+  // partial states of 132 floats a row and part: at most 2^18 of them
+  const int64_t rows = Tq * hq, most = (int64_t{1} << 18) / rows;
+  if (splits > most) splits = most;
+  if (splits < 2) return {1, 1, 0};
+  // In steps of a tile (2 us): halves take every second tile of an average sequence, in one or two
+  // rounds; parts their own, three more steps, and the states' way to memory and back (3 TB/s).
+  const int64_t halves = (keys / B + 1) / 2 * ((2 * groups + cus - 1) / cus);
+  const int64_t parts = per + 3 + rows * splits * 1056 / 6000000;
+  if (halves <= parts) return {1, 1, 0};
+  return {0, static_cast<int32_t>(splits), static_cast<int32_t>(per)};
+}
+
+// Tiles of a part of a sequence (or of a tile of its rows) with `tiles` of them.
+#if defined(__HIPCC__)
+__host__ __device__
+#endif
+inline int32_t prompt_part(int32_t tiles, int32_t splits, int32_t per) {
+  const int32_t least = (tiles + splits - 1) / splits;
+  return per > least ? per : least;
 }
 
 }  // namespace sq

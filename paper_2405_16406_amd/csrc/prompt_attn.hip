@@ -33,10 +33,16 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kTile = kPromptTile;          // keys of a tile
 constexpr int kTileBytes = kTile * 256;     // of K, and of V
-constexpr int kLds = 4 * kTileBytes;        // two tiles of each
 constexpr float kSlack = 8.0f;              // log2: weights stay below 2^(kWeightBits + kSlack) < 65504
 constexpr float kWeightBits = 7.0f;         // the largest weight when m has just moved
-static_assert(kPromptRows == 32 * kWaves, "a wave owns 32 rows");
+
+// KG groups of waves share a workgroup's rows and take its tiles of keys in turn.
+template <int KG>
+struct Prompt {
+  static constexpr int ROWS = 32 * kWaves / KG;   // of the workgroup, 32 of a wave
+  static constexpr int LDS = KG * 4 * kTileBytes;  // two tiles of K and of V for each group
+  static constexpr int COPIES = 2 * KG;            // 1 KB copies of a wave for a tile of K, or V
+};
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -67,47 +73,66 @@ __device__ __forceinline__ void pace() {
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
-// Sequence and tile of the tile number `rem` among ceil(rows / 256) tiles a sequence.
+// Inclusive sum over the lanes of a wave up to each: rows of 16 by shifts, then the rows' totals.
+__device__ __forceinline__ int wave_scan(int v) {
+  const auto add = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+  };
+  using std::integral_constant;
+  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});  // row_shr:1
+  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15
+  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
+  return v;
+}
+
+// Sequence and tile of the tile number `rem` among ceil(rows / ROWS) tiles a sequence.
 struct PromptTile {
   int seq;          // -1: past the last
   int tile, tiles;
   int q0, n;        // first row of q and rows of the sequence
+  int k0, m;        // first row of k and its keys
 };
-__device__ __forceinline__ PromptTile find_tile(const int32_t* cu_q, int64_t B, int64_t Tq, int group, int rem) {
+template <int ROWS>
+__device__ __forceinline__ PromptTile find_tile(const int32_t* cu_q, const int32_t* cu_k, int64_t B, int64_t Tq, int64_t Tk, int group,
+                                                int rem) {
   const int lane = threadIdx.x & 63;
   for (int64_t b0 = 0; b0 < B; b0 += 64) {
-    int q0 = 0, n = 0;
-    if (b0 + lane < B) {  // clamped to the tensor, whatever cu_q holds
-      const int last = static_cast<int>(Tq);
-      q0 = min(max(cu_q[b0 + lane], 0), last);
-      n = max(min(cu_q[b0 + lane + 1], last) - q0, 0);
+    int q0 = 0, n = 0, k0 = 0, m = 0;
+    if (b0 + lane < B) {  // clamped to the tensors, whatever cu_q and cu_k hold
+      const int lq = static_cast<int>(Tq), lk = static_cast<int>(Tk);
+      const int a = cu_q[b0 + lane], b = cu_q[b0 + lane + 1], c = cu_k[b0 + lane], d = cu_k[b0 + lane + 1];
+      q0 = min(max(a, 0), lq);
+      n = max(min(b, lq) - q0, 0);
+      k0 = min(max(c, 0), lk);
+      m = max(min(d, lk) - k0, 0);
     }
-    const int tiles = (n * group + kPromptRows - 1) / kPromptRows;
-    int upto = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
-    }
+    const int tiles = (n * group + ROWS - 1) / ROWS;
+    const int upto = wave_scan(tiles);
     const uint64_t past = __ballot(upto > rem);
     if (past) {
       const int f = __builtin_ctzll(past);
-      const int t = __builtin_amdgcn_readlane(tiles, f);
-      return {static_cast<int>(b0) + f, rem - (__builtin_amdgcn_readlane(upto, f) - t), t, __builtin_amdgcn_readlane(q0, f),
-              __builtin_amdgcn_readlane(n, f)};
+      const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+      return {static_cast<int>(b0) + f, rem - (of(upto) - of(tiles)), of(tiles), of(q0), of(n), of(k0), of(m)};
     }
     rem -= __builtin_amdgcn_readlane(upto, 63);
   }
-  return {-1, 0, 0, 0, 0};
+  return {-1, 0, 0, 0, 0, 0, 0};
 }
 
-template <bool SPLIT>
+template <bool SPLIT, int KG>
 __global__ void __launch_bounds__(64 * kWaves, 2)
 attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* cu_q, const int32_t* cu_k,
                  uint32_t magic_heads, uint32_t magic_group, uint32_t magic_splits, PromptArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  using P = Prompt<KG>;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int late = w >> 2;              // the second of a SIMD's two waves
+  const int rw = KG == 1 ? w : w & 3;   // which rows,
+  const int kg = KG == 1 ? 0 : late;    // and which group of waves
   const int col = lane & 31, h = lane >> 5;
   uint32_t rest, hk, split = 0;
   div_rem(blockIdx.x, a.hkv, magic_heads, rest, hk);
@@ -116,15 +141,14 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     div_rem(rest, a.splits, magic_splits, r2, split);
     rest = r2;
   }
-  const PromptTile pt = find_tile(cu_q, a.B, a.Tq, a.group, static_cast<int>(rest));
+  const PromptTile pt = find_tile<P::ROWS>(cu_q, cu_k, a.B, a.Tq, a.Tk, a.group, static_cast<int>(rest));
   if (pt.seq < 0) return;  // the workgroup leaves together
   const int tile = a.causal ? pt.tiles - 1 - pt.tile : pt.tile;  // the longest first
-  const int k0 = min(max(cu_k[pt.seq], 0), static_cast<int>(a.Tk));
-  const int m = max(min(cu_k[pt.seq + 1], static_cast<int>(a.Tk)) - k0, 0);
+  const int k0 = pt.k0, m = pt.m;
   const int rows = pt.n * a.group;
 
   // this lane's row: rows past the last repeat it and are not stored
-  const int row = tile * kPromptRows + 32 * w + col;
+  const int row = tile * P::ROWS + 32 * rw + col;
   uint32_t tok, gh;
   div_rem(static_cast<uint32_t>(min(row, rows - 1)), a.group, magic_group, tok, gh);
   const int64_t head = static_cast<int64_t>(hk) * a.group + gh;
@@ -137,14 +161,15 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     return min(m - pt.n + static_cast<int>(t), m - 1);
   };
   const int lim = limit(row);
-  const int wave_lo = limit(tile * kPromptRows + 32 * w), wave_hi = limit(tile * kPromptRows + 32 * w + 31);
-  const int keys = limit(tile * kPromptRows + kPromptRows - 1) + 1;  // of the workgroup
+  const int wave_lo = limit(tile * P::ROWS + 32 * rw), wave_hi = limit(tile * P::ROWS + 32 * rw + 31);
+  const int keys = limit(tile * P::ROWS + P::ROWS - 1) + 1;  // of the workgroup
   const int tiles_all = keys > 0 ? (keys + kTile - 1) / kTile : 0;
   int kt0 = 0, kt1 = tiles_all;
   if constexpr (SPLIT) {
-    const int per = (tiles_all + a.splits - 1) / a.splits;
+    const int per = prompt_part(tiles_all, a.splits, a.per);
     kt0 = min(static_cast<int>(split) * per, tiles_all);
     kt1 = min(kt0 + per, tiles_all);
+    if (split > 0 && kt0 == kt1) return;  // the workgroup leaves together; part 0 is always there
   }
 
   // Q^T operands: lane (row, h) holds dims 16 s + 8 h .. + 7
@@ -155,13 +180,12 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const v8h*>(qp + 16 * s);
   }
 
-  // copies: instruction x of a tile brings rows 4 x .. 4 x + 3; wave w takes x = 2 w, 2 w + 1 of K
-  // and of V
+  // copies: copy x of a tile brings rows 4 x .. 4 x + 3; wave rw of the group takes COPIES of them
   const int ldk2 = static_cast<int>(a.ldk * 2), ldv2 = static_cast<int>(a.ldv * 2);
-  int koff[2], voff[2];
+  int koff[P::COPIES], voff[P::COPIES];
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const int r = 4 * (2 * w + x) + (lane >> 4);
+  for (int x = 0; x < P::COPIES; ++x) {
+    const int r = 4 * (P::COPIES * rw + x) + (lane >> 4);
     const int c = (lane & 15) ^ swizzle(r);
     koff[x] = r * ldk2 + 16 * c;
     voff[x] = r * ldv2 + 16 * c;
@@ -175,9 +199,10 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     const __amdgpu_buffer_rsrc_t rs =
         buf_rsrc((keys_of ? kbase : vbase) + static_cast<int64_t>(kt) * kTile * ld2, static_cast<int64_t>(rows_here - 1) * ld2 + 256);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      uint8_t* dst = lds + (buf + (keys_of ? 0 : 2)) * kTileBytes + (2 * w + x) * 1024;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)dst, 16, keys_of ? koff[x] : voff[x], 0, 0, 0);
+    for (int x = 0; x < P::COPIES; ++x) {
+      uint8_t* dst = lds + (4 * kg + buf + (keys_of ? 0 : 2)) * kTileBytes + (P::COPIES * rw + x) * 1024;
+      const int off = keys_of ? koff[x] : voff[x];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(uintptr_t)dst, 16, off, 0, 0, 0);
     }
   };
 
@@ -187,14 +212,14 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   // the instructions.
   uint32_t kadr[8], vadr[4][2];
 #pragma unroll
-  for (int x = 0; x < 8; ++x) kadr[x] = col * 256 + 16 * ((2 * x + h) ^ swizzle(col));
+  for (int x = 0; x < 8; ++x) kadr[x] = 4 * kg * kTileBytes + col * 256 + 16 * ((2 * x + h) ^ swizzle(col));
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int second = 0; second < 2; ++second) {
       const int t = 4 * h + ((lane & 15) >> 2) + 8 * second;
       const int c = 4 * dt + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-      vadr[dt][second] = t * 256 + 16 * (c ^ swizzle(t)) + 8 * (lane & 1);
+      vadr[dt][second] = 4 * kg * kTileBytes + t * 256 + 16 * (c ^ swizzle(t)) + 8 * (lane & 1);
     }
 #pragma unroll
   for (int x = 0; x < 8; ++x) asm("" : "+v"(kadr[x]), "+v"(vadr[x >> 1][x & 1]));  // not derived from each other
@@ -279,41 +304,31 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       pf[ks] = __builtin_bit_cast(v8h, v4u{p[0], p[1], p[2], p[3]});
     }
     l += l0 + l1;
+    // done here: not beside the products of the next phase, which belong to the other wave's softmax
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(pf[ks]));
+    asm volatile("" : "+v"(l));
   };
 
   // A weight of 0 does not hide a value that is not finite, and in a masked tile some rows must not
-  // see what others do: there, such values stay out of the product and are added by hand, in the
-  // lane's own place of the result, which the end takes up (`odd`).
-  bool odd = false;
-  typename std::conditional<SPLIT, float, uint16_t>::type* own;
-  if constexpr (SPLIT)
-    own = a.part + ((qrow * a.hq + head) * a.splits + split) * kAttnPart + 4 + 4 * h;
-  else
-    own = a.out + qrow * a.ldo + head * 128 + 4 * h;
-  auto own_get = [&](int d) -> float {
-    if constexpr (SPLIT) return own[d];
-    else return h2f(own[d]);
-  };
-  auto own_set = [&](int d, float x) {
-    if constexpr (SPLIT) own[d] = x;
-    else own[d] = f2h(x);
-  };
+  // see what others do: there, such values stay out of the product, and what a row sees of them is
+  // kept as a bit for each of the lane's 64 dims (4 y + e of chunk y): +inf, -inf, or both for NaN.
+  uint64_t up = 0, down = 0;
   auto add_odd = [&](int kt, int buf) __attribute__((always_inline)) {
-    const bool mine = row < rows;
-    if (!odd && mine)
-#pragma unroll 1
-      for (int d = 0; d < 128; d += 8)
-        for (int e = 0; e < 4; ++e) own_set(d + e, 0.0f);
-    odd = true;
 #pragma unroll 1
     for (int t = 0; t < kTile; ++t) {
-      if (kt * kTile + t > lim || !mine) continue;
+      if (kt * kTile + t > lim) continue;
 #pragma unroll 1
       for (int c = 0; c < 16; ++c) {
-        const v2u u = *reinterpret_cast<const v2u*>(lds + (2 + buf) * kTileBytes + t * 256 + 16 * (c ^ swizzle(t)) + 8 * h);
+        const v2u u = *reinterpret_cast<const v2u*>(lds + (4 * kg + 2 + buf) * kTileBytes + t * 256 + 16 * (c ^ swizzle(t)) + 8 * h);
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint16_t x = static_cast<uint16_t>(u[e >> 1] >> (16 * (e & 1)));
-          if ((x & 0x7C00u) == 0x7C00u) own_set(8 * c + e, own_get(8 * c + e) + h2f(x));
+          const uint32_t x = (u[e >> 1] >> (16 * (e & 1))) & 0xFFFFu;
+          if ((x & 0x7C00u) != 0x7C00u) continue;
+          const uint64_t bit = uint64_t{1} << (4 * c + e);
+          const bool nan = (x & 0x3FFu) != 0;
+          if (nan || !(x & 0x8000u)) up |= bit;
+          if (nan || (x & 0x8000u)) down |= bit;
         }
       }
     }
@@ -363,18 +378,22 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   // Tile j's keys are read in the phases 2 j and 2 j + 1, its values in 2 j + 2 and 2 j + 3; in
   // phase 2 i the buffers of keys i + 1 and values i are free, and the copies have until the end of
   // the next phase to land.
-  const int late = w >> 2;
-  const int n = kt1 - kt0;
-  const auto tiles_in = [&](int key) { return min(max((key + kTile) / kTile - kt0, 0), n); };
-  const int nw = wave_hi < 0 ? 0 : tiles_in(wave_hi);         // tiles that a row of the wave sees a key of
-  const int nf = min(nw, max((wave_lo + 1) / kTile - kt0, 0));  // those that every row sees whole
+  // With two groups of waves (KG 2) a group's tiles are every second one, in buffers of its own.
+  const auto tile_of = [&](int j) { return kt0 + KG * j + kg; };
+  const auto count = [&](int end) { return max((end - kt0 - kg + KG - 1) / KG, 0); };  // of its tiles before `end`
+  const int n = (kt1 - kt0 + KG - 1) / KG;                   // steps of the workgroup
+  const int ng = count(kt1);                                 // tiles of the group,
+  const int nw = wave_hi < 0 ? 0 : min(ng, count(wave_hi / kTile + 1));  // that a row of the wave sees a key of,
+  const int nf = wave_lo < 0 ? 0 : min(nw, count((wave_lo + 1) / kTile));  // and that every row sees whole
   const auto fetch = [&](int i) __attribute__((always_inline)) {  // in phase 2 i
-    if (i + 1 < n) issue(kt0 + i + 1, (i + 1) & 1, true);
-    if (i < n) issue(kt0 + i, i & 1, false);
+    if (i + 1 < ng) issue(tile_of(i + 1), (i + 1) & 1, true);
+    if (i < ng) issue(tile_of(i), i & 1, false);
   };
   const auto meet = [&]() __attribute__((always_inline)) {
     asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
   };
   // the ends of a wave's steps 2 j and 2 j + 1
@@ -393,7 +412,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     if (!late) wait_vm_lgkm0<0>();
     meet();
   };
-  if (n > 0) issue(kt0, 0, true);
+  if (ng > 0) issue(tile_of(0), 0, true);
   wait_vm_lgkm0<0>();
   meet();
   if (late) {
@@ -403,14 +422,14 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   if (nw > 0) {
     scores(0);
     end_products(0);
-    softmax(kt0, std::true_type{});
+    softmax(tile_of(0), std::true_type{});
     end_softmax();
     int j = 1;
     const auto whole = [&](int j, int buf) __attribute__((always_inline)) {
-      values(kt0 + j - 1, buf ^ 1, std::false_type{});
+      values(tile_of(j - 1), buf ^ 1, std::false_type{});
       scores(buf);
       end_products(j);
-      softmax(kt0 + j, std::false_type{});
+      softmax(tile_of(j), std::false_type{});
       end_softmax();
     };
     for (; j + 1 < nf; j += 2) {
@@ -418,13 +437,13 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       whole(j + 1, 0);
     }
     for (; j < nw; ++j) {  // (and a whole tile left over)
-      values(kt0 + j - 1, (j - 1) & 1, std::true_type{});
+      values(tile_of(j - 1), (j - 1) & 1, std::true_type{});
       scores(j & 1);
       end_products(j);
-      softmax(kt0 + j, std::true_type{});
+      softmax(tile_of(j), std::true_type{});
       end_softmax();
     }
-    values(kt0 + nw - 1, (nw - 1) & 1, std::true_type{});
+    values(tile_of(nw - 1), (nw - 1) & 1, std::true_type{});
   }
   for (int j = nw; j < n; ++j) {  // other waves' tiles
     end_products(j);
@@ -433,46 +452,119 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   if (!late) meet();
 
   l = halves(l, [](float x, float y) { return __fadd_rn(x, y); });
-  if (row >= rows) return;
-  if constexpr (SPLIT) {
-    if (h == 0) {
-      own[-4] = mx;
-      own[-3] = l;
+  if constexpr (KG == 2) {  // the second group's states go to the first through LDS
+    float* const states = reinterpret_cast<float*>(lds);                       // [wave][64 dims][lane]
+    float2* const stats = reinterpret_cast<float2*>(lds + 4 * 64 * 64 * 4);    // [wave][lane]
+    uint64_t* const odds = reinterpret_cast<uint64_t*>(stats + 4 * 64);        // [wave][2][lane]
+    __syncthreads();  // every wave is done with the tiles
+    if (kg == 1) {
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) states[(rw * 64 + 16 * dt + r) * 64 + lane] = acc[dt][r];
+      stats[rw * 64 + lane] = make_float2(mx, l);
+      odds[rw * 128 + lane] = up;
+      odds[rw * 128 + 64 + lane] = down;
     }
+    __syncthreads();
+    if (kg == 1) return;
+    const float2 o = stats[rw * 64 + lane];
+    const float M = fmaxf(mx, o.x);
+    const float f0 = rescale(mx, M), f1 = rescale(o.x, M);
+    mx = M;
+    l = __fmaf_rn(o.y, f1, l * f0);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[dt][r] = __fmaf_rn(states[(rw * 64 + 16 * dt + r) * 64 + lane], f1, acc[dt][r] * f0);
+    up |= odds[rw * 128 + lane];
+    down |= odds[rw * 128 + 64 + lane];
   }
+  if (row >= rows) return;
   const float inv = SPLIT ? 1.0f : mx == -INFINITY ? 0.0f : __fdiv_rn(1.0f, l);  // a row that sees nothing is zero
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
+  for (int dt = 0; dt < 4; ++dt) acc[dt] *= inv;
+  if (__builtin_expect(__ballot((up | down) != 0) != 0, 0)) {
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      float o[4];
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = acc[dt][4 * y + e] * inv;
-      if (__builtin_expect(odd, 0))
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += own_get(32 * dt + 8 * y + e);
-      if constexpr (SPLIT)
-        *reinterpret_cast<float4*>(own + 32 * dt + 8 * y) = make_float4(o[0], o[1], o[2], o[3]);
-      else
-        *reinterpret_cast<v2u*>(own + 32 * dt + 8 * y) = v2u{f2h2(o[0], o[1]), f2h2(o[2], o[3])};
+      for (int r = 0; r < 16; ++r) {
+        const bool u = (up >> (16 * dt + r)) & 1, d = (down >> (16 * dt + r)) & 1;
+        if (u || d) acc[dt][r] += u ? (d ? NAN : INFINITY) : -INFINITY;
+      }
+  }
+  if constexpr (SPLIT) {
+    float* pr = a.part + ((qrow * a.hq + head) * a.splits + split) * kAttnPart;
+    if (h == 0) {
+      pr[0] = mx;
+      pr[1] = l;
     }
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        *reinterpret_cast<float4*>(pr + 4 + 32 * dt + 8 * y + 4 * h) =
+            make_float4(acc[dt][4 * y], acc[dt][4 * y + 1], acc[dt][4 * y + 2], acc[dt][4 * y + 3]);
+  } else {
+    uint16_t* o = a.out + qrow * a.ldo + head * 128 + 4 * h;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        *reinterpret_cast<v2u*>(o + 32 * dt + 8 * y) =
+            v2u{f2h2(acc[dt][4 * y], acc[dt][4 * y + 1]), f2h2(acc[dt][4 * y + 2], acc[dt][4 * y + 3])};
+  }
 }
 
-// One wave per (row of q, query head) of the sequences: the splits' states, in their order.
+// One wave per (row of q, query head) of the sequences: the states of the parts that its tile of
+// rows has, in their order.
 __global__ void __launch_bounds__(64)
-attn_prompt_combine(const float* part, const int32_t* cu_q, int64_t B, int hq, int splits, uint32_t magic_hq, uint16_t* out,
-                    int64_t ldo) {
+attn_prompt_combine(const float* part, const int32_t* cu_q, const int32_t* cu_k, uint32_t magic_hq, uint32_t magic_group, PromptArgs a) {
   const int lane = threadIdx.x;
   uint32_t t, head;
-  div_rem(blockIdx.x, hq, magic_hq, t, head);
-  if (find_sequence(cu_q, cu_q, B, t).seq < 0) return;  // a row of no sequence is left as it was
-  const float* pr = part + static_cast<int64_t>(blockIdx.x) * splits * kAttnPart;
+  div_rem(blockIdx.x, a.hq, magic_hq, t, head);
+  int q0 = 0, n = 0, m = 0;
+  bool found = false;
+  for (int64_t b0 = 0; b0 < a.B && !found; b0 += 64) {
+    int first = 0, rows = 0, keys = 0;
+    if (b0 + lane < a.B) {  // clamped as in find_tile
+      const int lq = static_cast<int>(a.Tq), lk = static_cast<int>(a.Tk);
+      first = min(max(cu_q[b0 + lane], 0), lq);
+      rows = max(min(cu_q[b0 + lane + 1], lq) - first, 0);
+      const int k0 = min(max(cu_k[b0 + lane], 0), lk);
+      keys = max(min(cu_k[b0 + lane + 1], lk) - k0, 0);
+    }
+    const int tt = static_cast<int>(t);
+    const uint64_t in = __ballot(tt >= first && tt < first + rows);
+    if (in) {
+      const int f = __builtin_ctzll(in);
+      q0 = __builtin_amdgcn_readlane(first, f);
+      n = __builtin_amdgcn_readlane(rows, f);
+      m = __builtin_amdgcn_readlane(keys, f);
+      found = true;
+    }
+  }
+  if (!found) return;  // a row of no sequence is left as it was
+  // the keys of the tile of 256 rows that this row is in
+  int keys = m;
+  if (a.causal) {
+    uint32_t hk, gh, tok, x;
+    div_rem(head, a.group, magic_group, hk, gh);
+    const int row = (static_cast<int>(t) - q0) * a.group + static_cast<int>(gh);
+    const int last = min(row / kPromptRows * kPromptRows + kPromptRows - 1, n * a.group - 1);
+    div_rem(static_cast<uint32_t>(last), a.group, magic_group, tok, x);
+    keys = min(m - n + static_cast<int>(tok) + 1, m);
+  }
+  const int tiles = keys > 0 ? (keys + kTile - 1) / kTile : 0;
+  const int per = prompt_part(tiles, a.splits, a.per);
+  const int parts = max(1, (tiles + per - 1) / per);
+  const float* pr = part + static_cast<int64_t>(blockIdx.x) * a.splits * kAttnPart;
   float M = -INFINITY;
-  for (int s = lane; s < splits; s += 64) M = fmaxf(M, pr[static_cast<int64_t>(s) * kAttnPart]);
+  for (int s = lane; s < parts; s += 64) M = fmaxf(M, pr[static_cast<int64_t>(s) * kAttnPart]);
   M = wave_max(M);
   float L = 0.0f, D0 = 0.0f, D1 = 0.0f;
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
+#pragma unroll 8
+  for (int s = 0; s < parts; ++s) {
     const float* p = pr + static_cast<int64_t>(s) * kAttnPart;
     const float f = rescale(p[0], M);
     const float2 d = reinterpret_cast<const float2*>(p + 4)[lane];
@@ -480,18 +572,19 @@ attn_prompt_combine(const float* part, const int32_t* cu_q, int64_t B, int hq, i
     D0 = __fmaf_rn(d.x, f, D0);
     D1 = __fmaf_rn(d.y, f, D1);
   }
-  reinterpret_cast<uint32_t*>(out + t * ldo + static_cast<int64_t>(head) * 128)[lane] =
+  reinterpret_cast<uint32_t*>(a.out + t * a.ldo + static_cast<int64_t>(head) * 128)[lane] =
       M == -INFINITY ? 0u : f2h2(__fdiv_rn(D0, L), __fdiv_rn(D1, L));
 }
 
-template <bool SPLIT>
+template <bool SPLIT, int KG>
 hipError_t launch_tiles(const PromptArgs& a, hipStream_t stream) {
-  constexpr auto kern = attn_prompt_tile<SPLIT>;
-  const hipError_t init = set_max_lds<kern>(kLds);
+  using P = Prompt<KG>;
+  constexpr auto kern = attn_prompt_tile<SPLIT, KG>;
+  const hipError_t init = set_max_lds<kern>(P::LDS);
   if (init != hipSuccess) return init;
   // as many tiles as any division of the rows among B sequences can make
-  const int64_t tiles = a.Tq * a.group / kPromptRows + a.B;
-  return launch(kern, dim3(static_cast<unsigned>(tiles * a.hkv * a.splits)), dim3(64 * kWaves), kLds, stream, a.q, a.k, a.v, a.cu_q,
+  const int64_t tiles = a.Tq * a.group / P::ROWS + a.B;
+  return launch(kern, dim3(static_cast<unsigned>(tiles * a.hkv * a.splits)), dim3(64 * kWaves), P::LDS, stream, a.q, a.k, a.v, a.cu_q,
                 a.cu_k, div_magic(static_cast<uint32_t>(a.hkv)), div_magic(static_cast<uint32_t>(a.group)),
                 div_magic(static_cast<uint32_t>(a.splits)), a);
 }
@@ -499,11 +592,11 @@ hipError_t launch_tiles(const PromptArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attn_prompt(const PromptArgs& a, hipStream_t stream) {
-  if (a.splits == 1) return launch_tiles<false>(a, stream);
-  const hipError_t e = launch_tiles<true>(a, stream);
+  if (a.splits == 1) return a.half ? launch_tiles<false, 2>(a, stream) : launch_tiles<false, 1>(a, stream);
+  const hipError_t e = launch_tiles<true, 1>(a, stream);
   if (e != hipSuccess) return e;
-  return launch(attn_prompt_combine, dim3(static_cast<unsigned>(a.Tq * a.hq)), dim3(64), 0, stream, a.part, a.cu_q, a.B, a.hq,
-                a.splits, div_magic(static_cast<uint32_t>(a.hq)), a.out, a.ldo);
+  return launch(attn_prompt_combine, dim3(static_cast<unsigned>(a.Tq * a.hq)), dim3(64), 0, stream, a.part, a.cu_q, a.cu_k,
+                div_magic(static_cast<uint32_t>(a.hq)), div_magic(static_cast<uint32_t>(a.group)), a);
 }
 
 }  // namespace sq

@@ -245,7 +245,7 @@ struct PromptArgs {
   int32_t causal;
   uint16_t* out;         // fp16 [Tq, ldo]
   int64_t ldo;
-  int32_t splits;        // parts of the keys; 1: no partial states
+  int32_t half, splits, per;  // the PromptPlan
   float* part;
 };
 hipError_t launch_attn_prompt(const PromptArgs& a, hipStream_t stream);

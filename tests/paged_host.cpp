@@ -24,7 +24,12 @@ void paged_split(int64_t B, int64_t max_len, int32_t hq, int32_t hkv, int cus, i
   sq::paged_split(B, max_len, hq, hkv, cus, out[0], out[1]);
 }
 
-int32_t prompt_splits(int64_t B, int64_t Tq, int64_t Tk, int32_t hq, int32_t hkv, int cus) {
-  return sq::prompt_splits(B, Tq, Tk, hq, hkv, cus);
+void prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int32_t hq, int32_t hkv, int cus, int32_t* out) {
+  const sq::PromptPlan p = sq::prompt_plan(B, Tq, Tk, hq, hkv, cus);
+  out[0] = p.half;
+  out[1] = p.splits;
+  out[2] = p.per;
 }
+
+int32_t prompt_part(int32_t tiles, int32_t splits, int32_t per) { return sq::prompt_part(tiles, splits, per); }
 }

@@ -301,6 +301,8 @@ PROMPT = [  # Hq, Hkv, queries, keys
     (4, 4, [3, 2], [0, 9]),                 # no keys at all
     (8, 1, [2], [9000]),                    # few rows, many keys: split
     (8, 2, [1, 7], [3000, 5000]),
+    (64, 32, [70, 1, 130, 5, 0, 64, 20, 33, 257], [70, 1, 140, 5, 0, 300, 20, 20, 257]),  # tiles of 256 rows
+    (20, 4, [3, 60], [7000, 2000]),         # tokens whose heads lie in two tiles of rows, in parts
 ]
 
 
@@ -348,26 +350,27 @@ def test_prompt_attention_of_a_fused_projection():
 
 @pytest.mark.parametrize("which", ["k", "v"])
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
-def test_prompt_values_that_a_row_does_not_see(value, which):
+@pytest.mark.parametrize("n,m,H,at", [(200, 200, 2, 77), (90, 90, 300, 77), (40, 3000, 2, 2970), (40, 3000, 2, 100)],
+                         ids=["halves", "whole", "parts", "parts_early"])
+def test_prompt_values_that_a_row_does_not_see(n, m, H, at, value, which):
     """A key or value that is not finite reaches the rows that see it and no other."""
     g = rng(22)
-    T, H, at = 200, 2, 77
-    q, k, v = (heads_of(g, T, H) for _ in range(3))
+    q, k, v = heads_of(g, n, H), heads_of(g, m, H), heads_of(g, m, H)
     (k if which == "k" else v)[at, 1, 5] = value
-    cu = ints([0, T])
-    got = f64(sq.attn_prompt(up(q), up(k), up(v), cu, cu))
+    got = f64(sq.attn_prompt(up(q), up(k), up(v), ints([0, n]), ints([0, m])))
     clean = k if which == "k" else v
     clean[at, 1, 5] = 0
-    want, weight, _ = opg.attn_prompt(q, k, v, [0, T], [0, T])
-    ok = np.ones((T, H), dtype=bool)
-    ok[at:, 1] = False
+    want, weight, _ = opg.attn_prompt(q, k, v, [0, n], [0, m])
+    ok = np.ones((n, H), dtype=bool)
+    first = max(0, at - (m - n))  # the first row that sees it
+    ok[first:, 1] = False
     tol = (2.0 ** -11 + prompt_scores(q, k, 128 ** -0.5)) * weight + 2.0 ** -11 * np.abs(want) + 2.0 ** -25
     assert np.all((np.abs(got - want) <= tol)[ok])
-    hit = got[at:, 1]
+    hit = got[first:, 1]
     if which == "v":
         assert np.all(np.isnan(hit[:, 5])) if np.isnan(value) else np.all(hit[:, 5] == value)
         others = np.arange(128) != 5
-        assert np.all((np.abs(got - want) <= tol)[at:, 1][:, others])
+        assert np.all((np.abs(got - want) <= tol)[first:, 1][:, others])
     elif np.isnan(value):
         assert np.all(np.isnan(hit))
 

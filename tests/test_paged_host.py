@@ -81,13 +81,39 @@ def test_paged_split_covers_every_token(host):
         assert B * hkv * -(-(hq // hkv) // 16) * chunks < 2 ** 31
 
 
-def test_prompt_splits_are_bounded(host):
+def plan_of(host, B, Tq, Tk, hq, hkv, cus=256):
+    out = (ctypes.c_int32 * 3)()
+    host.prompt_plan(ctypes.c_int64(B), ctypes.c_int64(Tq), ctypes.c_int64(Tk), hq, hkv, cus, out)
+    return tuple(out)
+
+
+def test_prompt_plans_are_bounded(host):
     rng = random.Random(3)
     for _ in range(3000):
         hkv = rng.choice([1, 8, 32])
         hq, B = hkv * rng.choice([1, 4, 8, 17]), int(2 ** rng.uniform(0, 10))
         Tq, Tk, cus = int(2 ** rng.uniform(0, 20)), int(2 ** rng.uniform(0, 20)), rng.choice([256, 64, 1])
-        s = host.prompt_splits(ctypes.c_int64(B), ctypes.c_int64(Tq), ctypes.c_int64(Tk), hq, hkv, cus)
-        assert 1 <= s <= max(1, cus)
-        assert s == 1 or s * 512 <= Tk // B
-    assert host.prompt_splits(ctypes.c_int64(0), ctypes.c_int64(4), ctypes.c_int64(4), 8, 8, 256) == 1
+        half, splits, per = plan_of(host, B, Tq, Tk, hq, hkv, cus)
+        assert splits >= 1 and half in (0, 1) and not (half and splits > 1)
+        if splits > 1:
+            assert per >= 4 and Tq * hq * splits <= 1 << 18
+            for tiles in (0, 1, per, per + 1, -(-Tk // 64), rng.randrange(1 << 20)):  # any sequence fits its parts
+                part = host.prompt_part(tiles, splits, per)
+                assert part >= per and part * splits >= tiles
+    assert plan_of(host, 0, 4, 4, 8, 8) == plan_of(host, 4, 0, 4, 8, 8) == plan_of(host, 4, 4, 0, 8, 8) == (0, 1, 0)
+
+
+def test_prompt_plans_of_known_sizes(host):
+    """The measured choices: whole tiles, halves, and parts."""
+    assert plan_of(host, 1, 8192, 8192, 32, 32)[:2] == (0, 1)
+    assert plan_of(host, 1, 2048, 2048, 32, 32)[:2] == (1, 1)
+    assert plan_of(host, 1, 1024, 1024, 64, 8)[:2] == (1, 1)
+    half, splits, per = plan_of(host, 2, 41, 22560, 32, 8)
+    assert half == 0 and splits > 16 and per == 12
+
+
+def test_every_prompt_form_is_tested(host):
+    """The sizes of tests/test_gpu_paged.py reach whole tiles, halves and parts."""
+    t = pytest.importorskip("test_gpu_paged")
+    plans = [plan_of(host, len(nq), sum(nq) + 3, sum(nk) + 2, hq, h) for hq, h, nq, nk in t.PROMPT]
+    assert {(half, splits > 1) for half, splits, _ in plans} == {(0, False), (1, False), (0, True)}
