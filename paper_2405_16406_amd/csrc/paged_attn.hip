@@ -8,7 +8,7 @@
 // one shift and four ands, codes 0, 2, 4, 6 as n and 1, 3, 5, 7 in place as 16 n.
 //
 // A workgroup of kWaves waves serves one (sequence, key/value head, up to 16 of its query heads,
-// chunk of tokens); its waves take the chunk's blocks of 64 tokens in turn, each on its own:
+// chunk of tokens: paged_plan.h); its waves take the chunk's blocks of 64 tokens in turn, each on its own:
 //   scores    S^T = K q^T by 16x16x32 products: lane (i, g) = (lane % 16, lane / 16) brings
 //             bytes 16 g (4 bits) or 32 g (8 bits) .. of a token's key codes straight from
 //             memory (dims 32 g .. 32 g + 31) and ends with the scores of head i for the 16
@@ -68,25 +68,29 @@ constexpr int paged_lds() {
 
 template <int BITS, bool P16>
 __global__ void __launch_bounds__(64 * kWaves, BITS == 4 ? 3 : 2)
-attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, uint32_t magic_chunks, uint32_t magic_tiles,
+attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, uint32_t magic_b, uint32_t magic_tiles,
                 uint32_t magic_heads, PagedAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   using W = WaveLds<BITS>;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 15, g = lane >> 4;
-  // workgroup: key/value head fastest (its chunk's neighbours in a page), then tile of heads,
-  // sequence, chunk: chunks that a short sequence lacks end at the back of the grid
-  uint32_t rest, hk, tile, b, c;
+  // Workgroups in the order of dispatch: the chunks from a sequence's last one back are the slowest
+  // index, from far to near, so that whole chunks come first and the sequences' short last ones
+  // fill up at the end; then sequence, tile of heads, key/value head.
+  uint32_t rest, hk, tile, b, back;
   div_rem(blockIdx.x, a.cache.heads, magic_heads, rest, hk);
   div_rem(rest, tiles, magic_tiles, rest, tile);
-  div_rem(rest, chunks, magic_chunks, b, c);
-  const int first = static_cast<int>(c) * a.chunk_tokens;
+  div_rem(rest, static_cast<int>(a.B), magic_b, back, b);
+  back = chunks - 1 - back;
+  const int len = min(max(lens[b], 0), a.max_len);
+  const int own = max(1, (len + a.chunk_tokens - 1) / a.chunk_tokens);  // chunks of the sequence
+  if (static_cast<int>(back) >= own) return;  // the workgroup leaves together
+  const int c = own - 1 - static_cast<int>(back);
+  const int first = c * a.chunk_tokens;
   const int32_t* const table = a.cache.table + b * a.cache.ldt;
   const int32_t first_col = table_column(a.cache, first + w * kBlock + 16 * g);
   const int32_t first_entry = first_col < 0 ? -1 : table[first_col];
-  const int len = min(max(lens[b], 0), a.max_len);
-  if (c > 0 && first >= len) return;  // the workgroup leaves together
   const int last = min(len, first + a.chunk_tokens);
   const int heads = min(16, a.group - 16 * static_cast<int>(tile));  // of this workgroup
   const int h0 = static_cast<int>(hk) * a.group + 16 * static_cast<int>(tile);
@@ -361,7 +365,7 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
       for (int r = 0; r < 4; ++r) D[r] = __fmaf_rn(o[r], f, D[r]);
     }
     const int64_t head = h0 + hh;
-    if (chunks == 1) {
+    if (own == 1) {
       uint16_t* o = a.out + b * a.ldo + head * 128 + d;
       if (M == -INFINITY)  // no token
         *reinterpret_cast<v2u*>(o) = v2u{0u, 0u};
@@ -378,34 +382,35 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
   }
 }
 
-// One workgroup per (sequence, query head) over the chunks that its length reaches: wave w adds the
-// chunks w, w + kJoin, ..., then the waves' sums are added in their order.
-constexpr int kJoin = 8;
-__global__ void __launch_bounds__(64 * kJoin)
+// One workgroup per (sequence, query head) with more than one chunk: wave w adds the chunks w, w + J,
+// ..., then the waves' sums are added in their order.
+template <int J>
+__global__ void __launch_bounds__(64 * J)
 attn_paged_combine(const float* part, const int32_t* lens, uint16_t* out, int64_t ldo, int hq, int chunks, int chunk_tokens,
                    int max_len, uint32_t magic_hq) {
-  __shared__ float red_m[kJoin], red_l[kJoin];
-  __shared__ float2 red_d[kJoin][64];
+  __shared__ float red_m[J], red_l[J];
+  __shared__ float2 red_d[J][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   uint32_t b, h;
   div_rem(blockIdx.x, hq, magic_hq, b, h);
   const int len = min(max(lens[b], 0), max_len);
-  const int n = max(1, (len + chunk_tokens - 1) / chunk_tokens);  // chunk 0 is always written
+  const int n = (len + chunk_tokens - 1) / chunk_tokens;
+  if (n <= 1) return;  // its workgroup has written the output
   const float* pr = part + (b * static_cast<int64_t>(hq) + h) * chunks * kAttnPart;
   float M = -INFINITY, L = 0.0f, D0 = 0.0f, D1 = 0.0f;
   constexpr int kAhead = 8;  // chunks whose loads are in flight together
-  for (int c0 = w; c0 < n; c0 += kJoin * kAhead) {
+  for (int c0 = w; c0 < n; c0 += J * kAhead) {
     float2 ml[kAhead], d[kAhead];
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) {  // a chunk past the last is the last again, with weight 0
-      const float* p = pr + static_cast<int64_t>(min(c0 + kJoin * x, n - 1)) * kAttnPart;
+      const float* p = pr + static_cast<int64_t>(min(c0 + J * x, n - 1)) * kAttnPart;
       ml[x] = *reinterpret_cast<const float2*>(p);
       d[x] = reinterpret_cast<const float2*>(p + 4)[lane];
     }
     float top = M;
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) {
-      if (c0 + kJoin * x >= n) ml[x].x = -INFINITY;
+      if (c0 + J * x >= n) ml[x].x = -INFINITY;
       top = fmaxf(top, ml[x].x);
     }
     const float f0 = rescale(M, top);
@@ -421,23 +426,25 @@ attn_paged_combine(const float* part, const int32_t* lens, uint16_t* out, int64_
       D1 = __fmaf_rn(d[x].y, f, D1);
     }
   }
-  red_d[w][lane] = make_float2(D0, D1);
-  if (lane == 0) {
-    red_m[w] = M;
-    red_l[w] = L;
-  }
-  __syncthreads();
-  if (w > 0) return;
+  if constexpr (J > 1) {
+    red_d[w][lane] = make_float2(D0, D1);
+    if (lane == 0) {
+      red_m[w] = M;
+      red_l[w] = L;
+    }
+    __syncthreads();
+    if (w > 0) return;
 #pragma unroll
-  for (int v = 0; v < kJoin; ++v) M = fmaxf(M, red_m[v]);
-  L = D0 = D1 = 0.0f;
+    for (int v = 0; v < J; ++v) M = fmaxf(M, red_m[v]);
+    L = D0 = D1 = 0.0f;
 #pragma unroll
-  for (int v = 0; v < kJoin; ++v) {
-    const float f = rescale(red_m[v], M);
-    const float2 d = red_d[v][lane];
-    L = __fmaf_rn(red_l[v], f, L);
-    D0 = __fmaf_rn(d.x, f, D0);
-    D1 = __fmaf_rn(d.y, f, D1);
+    for (int v = 0; v < J; ++v) {
+      const float f = rescale(red_m[v], M);
+      const float2 d = red_d[v][lane];
+      L = __fmaf_rn(red_l[v], f, L);
+      D0 = __fmaf_rn(d.x, f, D0);
+      D1 = __fmaf_rn(d.y, f, D1);
+    }
   }
   reinterpret_cast<uint32_t*>(out + b * ldo + static_cast<int64_t>(h) * 128)[lane] =
       M == -INFINITY ? 0u : f2h2(__fdiv_rn(D0, L), __fdiv_rn(D1, L));
@@ -452,7 +459,7 @@ hipError_t launch_part(const PagedAttnArgs& a, hipStream_t stream) {
   const int tiles = (a.group + 15) / 16;
   const unsigned blocks = static_cast<unsigned>(a.B * a.cache.heads * tiles * a.chunks);
   return launch(kern, dim3(blocks), dim3(64 * kWaves), lds, stream, a.q, a.lens, a.chunks, tiles,
-                div_magic(static_cast<uint32_t>(a.chunks)), div_magic(static_cast<uint32_t>(tiles)),
+                div_magic(static_cast<uint32_t>(a.B)), div_magic(static_cast<uint32_t>(tiles)),
                 div_magic(static_cast<uint32_t>(a.cache.heads)), a);
 }
 
@@ -465,8 +472,12 @@ hipError_t launch_attn_paged(const PagedAttnArgs& a, hipStream_t stream) {
   else
     e = a.param16 ? launch_part<4, true>(a, stream) : launch_part<4, false>(a, stream);
   if (e != hipSuccess || a.chunks == 1) return e;
-  return launch(attn_paged_combine, dim3(static_cast<unsigned>(a.B * a.hq)), dim3(64 * kJoin), 0, stream, a.part, a.lens, a.out, a.ldo,
-                a.hq, a.chunks, a.chunk_tokens, a.max_len, div_magic(static_cast<uint32_t>(a.hq)));
+  const auto join = [&](auto kern, int waves) {
+    return launch(kern, dim3(static_cast<unsigned>(a.B * a.hq)), dim3(64 * waves), 0, stream, a.part, a.lens, a.out, a.ldo, a.hq,
+                  a.chunks, a.chunk_tokens, a.max_len, div_magic(static_cast<uint32_t>(a.hq)));
+  };
+  // (4096 heads of 64 sequences in two chunks: 4 us less with one wave each than with eight)
+  return a.chunks <= 8 ? join(attn_paged_combine<1>, 1) : join(attn_paged_combine<8>, 8);
 }
 
 }  // namespace sq

@@ -9,19 +9,25 @@ namespace sq {
 constexpr int kPagedWaves = 4;    // of a decode workgroup, each on its own
 constexpr int kPagedBlock = 64;   // tokens of a wave's step
 
-// Decode: tokens of a chunk (whole steps of a workgroup) and chunks of the longest sequence, for
-// about eight workgroups of the longest length on each of `cus` compute units: lengths differ, and
-// a chunk that a sequence does not reach ends at once.
+// Decode: tokens of a chunk (whole steps of a workgroup) and chunks of the longest sequence.
+//   One sequence: two workgroups for each of `cus` compute units, one round of equal ones (131071
+//   tokens of 8 heads, us with the join: chunks of 2048 tokens 34, 1536 37, 8192 54).
+//   Several: their lengths differ as a rule, so four times as many, the sequences' short last chunks
+//   among them filling up at the end (64 sequences of 512 .. 8192 tokens, 8 heads: 2048 51, 8192 75;
+//   equal lengths lose by it, 64 of 2432: 43, uncut 38).  Chunks of one step for each wave only where
+//   there is nothing better to do for the compute units (16 sequences, 8 heads: 512 15, 256 16).
+// The lengths lie on the device, so the plan goes by the longest.
 inline void paged_split(int64_t B, int64_t max_len, int32_t hq, int32_t hkv, int cus, int32_t& chunks, int32_t& chunk_tokens) {
   constexpr int64_t unit = kPagedWaves * kPagedBlock;
   const int64_t groups = B * hkv * ((hq / hkv + 15) / 16);
-  const int64_t want = 8 * static_cast<int64_t>(cus);
-  int64_t n = groups > 0 && groups < want ? (want + groups - 1) / groups : 1;
-  const int64_t blocks = (max_len + unit - 1) / unit;
-  if (n > blocks) n = blocks;
-  if (n < 1) n = 1;
-  chunk_tokens = static_cast<int32_t>((blocks + n - 1) / n * unit);
-  if (chunk_tokens < unit) chunk_tokens = unit;
+  const int64_t tokens = groups * max_len;  // < 2^54
+  const int64_t want = static_cast<int64_t>(cus) * (B > 1 ? 8 : 2);
+  int64_t chunk = (tokens + want - 1) / want;
+  const int64_t least = tokens / unit > 4 * static_cast<int64_t>(cus) ? 2 * unit : unit;
+  if (chunk < least) chunk = least;
+  chunk = (chunk + unit - 1) / unit * unit;
+  if (chunk > max_len) chunk = (max_len + unit - 1) / unit * unit;
+  chunk_tokens = static_cast<int32_t>(chunk < unit ? unit : chunk);
   chunks = static_cast<int32_t>((max_len + chunk_tokens - 1) / chunk_tokens);
   if (chunks < 1) chunks = 1;
 }

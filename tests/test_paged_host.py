@@ -77,8 +77,7 @@ def test_paged_split_covers_every_token(host):
         assert chunks >= 1 and tokens >= 256 and tokens % 256 == 0
         assert (chunks - 1) * tokens < n <= chunks * tokens
         groups = B * hkv * -(-(hq // hkv) // 16)
-        assert chunks == 1 or chunks * groups <= 2 * max(8 * cus, groups)  # workgroups stay bounded
-        assert B * hkv * -(-(hq // hkv) // 16) * chunks < 2 ** 31
+        assert groups * chunks <= groups + 8 * cus + 4 * cus  # workgroups stay bounded
 
 
 def plan_of(host, B, Tq, Tk, hq, hkv, cus=256):
