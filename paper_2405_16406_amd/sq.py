@@ -445,31 +445,20 @@ def kv_cache(pages: int, page: int, heads: int, bits: int = 4, param_dtype=torch
     return k_q, torch.zeros_like(k_q), torch.zeros((pages, heads, page, 4), dtype=param_dtype, device=device)
 
 
-class _On:
-    """Makes t's device the current one for a call, where it is not."""
-
-    __slots__ = ("guard",)
-
-    def __init__(self, t):
-        d = t.get_device()
-        self.guard = None if d == torch.cuda.current_device() else torch.cuda.device(d)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+# A decode step is two of the calls below on small tensors, and their host time is most of it: checks
+# use each property once, and the device is switched only where another one is current.
+_F16, _U8, _I32T, _F64T = torch.float16, torch.uint8, torch.int32, torch.float64
+_current_device = torch._C._cuda_getDevice
 
 
 def _heads(t, name):
     """(rows, heads, ld) of fp16 [rows, heads, 128] whose heads are contiguous."""
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.float16 or not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or t.dtype is not _F16 or not t.is_cuda:
         raise TypeError(f"{name} must be a torch.float16 tensor on the GPU")
-    if t.dim() != 3 or t.shape[2] != 128:
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != 128:
         raise ValueError(f"{name} must be [rows, heads, 128]")
-    rows, heads, _ = t.shape
+    rows, heads, _ = shape
     ld, sh, sd = t.stride()
     if sd != 1 or (sh != 128 and heads > 1):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
@@ -478,7 +467,7 @@ def _heads(t, name):
 
 def _index(t, name, n=None):
     """A contiguous int32 vector (of n entries) on the GPU."""
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or t.dtype is not _I32T or not t.is_cuda:
         raise TypeError(f"{name} must be a torch.int32 tensor on the GPU")
     if t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n):
         raise ValueError(f"{name} must be a contiguous vector" + ("" if n is None else f" of {n} entries"))
@@ -489,31 +478,34 @@ def _cache_args(cache, table, B):
     """The cache's arguments: table, its stride and columns, the three tensors, pages, page, heads; and
     (bits, param_bits)."""
     k_q, v_q, params = cache
-    _need(k_q, torch.uint8, "k_q")
-    _need(v_q, torch.uint8, "v_q")
-    if not isinstance(params, torch.Tensor) or params.dtype not in _PARAM_BITS or not params.is_cuda:
+    if not (isinstance(k_q, torch.Tensor) and isinstance(v_q, torch.Tensor) and k_q.dtype is v_q.dtype is _U8):
+        raise TypeError("k_q and v_q must be torch.uint8 tensors on the GPU")
+    if not isinstance(params, torch.Tensor) or params.dtype not in _PARAM_BITS:
         raise TypeError("params must be a torch.float32 or torch.float16 tensor on the GPU")
-    if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or not table.is_cuda:
+    if not isinstance(table, torch.Tensor) or table.dtype is not _I32T:
         raise TypeError("block_table must be a torch.int32 tensor on the GPU")
-    if k_q.dim() != 4 or v_q.shape != k_q.shape or params.shape != (*k_q.shape[:3], 4):
+    shape = k_q.shape
+    if len(shape) != 4 or v_q.shape != shape or params.shape != (shape[0], shape[1], shape[2], 4):
         raise ValueError("the cache is codes [pages, heads, page, bytes] twice and parameters [pages, heads, page, 4]")
     if not (k_q.is_contiguous() and v_q.is_contiguous() and params.is_contiguous()):
         raise ValueError("the cache's tensors must be contiguous")
-    if table.dim() != 2 or table.shape[0] != B or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise ValueError(f"block_table must be [{B}, blocks] with unit column stride")
-    pages, heads, page, row = k_q.shape
-    if row not in (64, 128):
+    pages, heads, page, row = shape
+    if row != 64 and row != 128:
         raise ValueError("a token's codes are 64 (4 bits) or 128 (8 bits) bytes")
+    if table.dim() != 2 or table.shape[0] != B or (table.stride(1) != 1 and table.shape[1] > 1):
+        raise ValueError(f"block_table must be [{B}, blocks] with unit column stride")
     cols = table.shape[1]
     return ((table.data_ptr(), table.stride(0) if B > 1 else cols, cols, k_q.data_ptr(), v_q.data_ptr(), params.data_ptr(),
              pages, page, heads), (row // 16, _PARAM_BITS[params.dtype]))
 
 
 def _same_device(t, *others):
+    """The device of t, which all other tensors must be on."""
     d = t.get_device()
     for o in others:
         if o is not None and o.get_device() != d:
-            raise ValueError("all tensors of a call must be on one device")
+            raise ValueError("all tensors of a call must be on one GPU")
+    return d
 
 
 def rope_kv_write(q, k, v, cache, block_table, lens, freq=None, cu=None, interleaved: bool = False, magnitude: float = 1.0,
@@ -540,20 +532,24 @@ def rope_kv_write(q, k, v, cache, block_table, lens, freq=None, cu=None, interle
         if freq.dim() != 1 or not freq.is_contiguous():
             raise ValueError("freq must be a contiguous vector")
         rotary = 2 * freq.shape[0]
-    if out is None:
-        out = q.new_empty((T, Hq, 128))
     for t, h, n in ((out, Hq, "out"), (k_out, Hkv, "k_out")):
         if t is not None:
             _need(t, torch.float16, n)
             if tuple(t.shape) != (T, h, 128) or not t.is_contiguous():
                 raise ValueError(f"{n} must be contiguous [{T}, {h}, 128]")
-    _same_device(q, k, v, *cache, block_table, lens, cu, freq, out, k_out)
+    if out is None:
+        out = q.new_empty((T, Hq, 128))
+    d = _same_device(q, k, v, *cache, block_table, lens, cu, freq, out, k_out)
     if T == 0 or B == 0:  # an empty tensor has no address
         return out
-    with _On(q):
-        _check(lib().sq_rope_kv_write(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, Hq, 128, _ptr(cu),
-                                      lens.data_ptr(), B, *args, *bits, _ptr(freq), rotary, int(interleaved), magnitude,
-                                      k_clip, v_clip, out.data_ptr(), _ptr(k_out), _stream(q)), "sq_rope_kv_write")
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return rope_kv_write(q, k, v, cache, block_table, lens, freq, cu, interleaved, magnitude, k_clip, v_clip, out, k_out)
+    status = lib().sq_rope_kv_write(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, Hq, 128, _ptr(cu),
+                                    lens.data_ptr(), B, *args, *bits, _ptr(freq), rotary, int(interleaved), magnitude,
+                                    k_clip, v_clip, out.data_ptr(), _ptr(k_out), _stream(q))
+    if status:
+        _check(status, "sq_rope_kv_write")
     return out
 
 
@@ -574,12 +570,16 @@ def kv_read(cache, block_table, lens, cu, rows: int, plain_basis: bool = False, 
     tv, hv, ldv = _heads(v, "v")
     if (tk, hk, tv, hv) != (rows, Hkv, rows, Hkv):
         raise ValueError(f"out must be two [{rows}, {Hkv}, 128] tensors")
-    _same_device(k, v, *cache, block_table, lens, cu)
+    d = _same_device(k, v, *cache, block_table, lens, cu)
     if rows == 0 or B == 0:
         return k, v
-    with _On(k):
-        _check(lib().sq_kv_read(cu.data_ptr(), lens.data_ptr(), B, rows, *args, 128, *bits, int(plain_basis), k.data_ptr(), ldk,
-                                v.data_ptr(), ldv, _stream(k)), "sq_kv_read")
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return kv_read(cache, block_table, lens, cu, rows, plain_basis, (k, v))
+    status = lib().sq_kv_read(cu.data_ptr(), lens.data_ptr(), B, rows, *args, 128, *bits, int(plain_basis), k.data_ptr(), ldk,
+                              v.data_ptr(), ldv, _stream(k))
+    if status:
+        _check(status, "sq_kv_read")
     return k, v
 
 
@@ -598,22 +598,28 @@ def attn_paged(q, cache, block_table, lens, max_len: int, scale=None, out=None, 
     _index(lens, "lens", B)
     args, bits = _cache_args(cache, block_table, B)
     if out is None:
-        out = q.new_empty((B, Hq, 128))
-    to, ho, ldo = _heads(out, "out")
-    if (to, ho) != (B, Hq):
-        raise ValueError(f"out must be [{B}, {Hq}, 128]")
+        out, ldo = q.new_empty((B, Hq, 128)), Hq * 128
+    else:
+        to, ho, ldo = _heads(out, "out")
+        if (to, ho) != (B, Hq):
+            raise ValueError(f"out must be [{B}, {Hq}, 128]")
+    d = _same_device(q, *cache, block_table, lens, out, workspace)
     if B == 0:
         return out
-    with _On(q):
-        if workspace is None:
-            n = attn_paged_workspace_bytes(B, max_len, Hq, args[-1])
-            workspace = q.new_empty(n, dtype=torch.uint8) if n else None
-        else:
-            _need(workspace, torch.uint8, "workspace")
-        _same_device(q, *cache, block_table, lens, out, workspace)
-        _check(lib().sq_attn_paged(q.data_ptr(), ldq, lens.data_ptr(), B, *args, Hq, 128, *bits, max_len,
-                                   0.08838834764831845 if scale is None else scale, out.data_ptr(), ldo, _ptr(workspace),
-                                   0 if workspace is None else workspace.numel(), _stream(q)), "sq_attn_paged")
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return attn_paged(q, cache, block_table, lens, max_len, scale, out, workspace)
+    if workspace is None:
+        size = attn_paged_workspace_bytes(B, max_len, Hq, args[-1])
+        workspace = q.new_empty(size, dtype=_U8) if size else None
+    else:
+        _need(workspace, _U8, "workspace")
+        size = workspace.numel()
+    status = lib().sq_attn_paged(q.data_ptr(), ldq, lens.data_ptr(), B, *args, Hq, 128, *bits, max_len,
+                                 0.08838834764831845 if scale is None else scale, out.data_ptr(), ldo, _ptr(workspace), size,
+                                 _stream(q))
+    if status:
+        _check(status, "sq_attn_paged")
     return out
 
 
@@ -638,21 +644,26 @@ def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, 
     B = _index(cu_q, "cu_q") - 1
     _index(cu_k, "cu_k", B + 1)
     if out is None:
-        out = q.new_empty((Tq, Hq, 128))
-    to, ho, ldo = _heads(out, "out")
-    if (to, ho) != (Tq, Hq):
-        raise ValueError(f"out must be [{Tq}, {Hq}, 128]")
+        out, ldo = q.new_empty((Tq, Hq, 128)), Hq * 128
+    else:
+        to, ho, ldo = _heads(out, "out")
+        if (to, ho) != (Tq, Hq):
+            raise ValueError(f"out must be [{Tq}, {Hq}, 128]")
+    d = _same_device(q, k, v, cu_q, cu_k, out, workspace)
     if Tq == 0 or B == 0:
         return out
-    with _On(q):
-        if workspace is None:
-            n = attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv)
-            workspace = q.new_empty(n, dtype=torch.uint8) if n else None
-        else:
-            _need(workspace, torch.uint8, "workspace")
-        _same_device(q, k, v, cu_q, cu_k, out, workspace)
-        _check(lib().sq_attn_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(), cu_k.data_ptr(), B,
-                                    Tq, Tk, Hq, Hkv, 128, 0.08838834764831845 if scale is None else scale, int(causal),
-                                    out.data_ptr(), ldo, _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                    _stream(q)), "sq_attn_prompt")
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return attn_prompt(q, k, v, cu_q, cu_k, scale, causal, out, workspace)
+    if workspace is None:
+        size = attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv)
+        workspace = q.new_empty(size, dtype=_U8) if size else None
+    else:
+        _need(workspace, _U8, "workspace")
+        size = workspace.numel()
+    status = lib().sq_attn_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(), cu_k.data_ptr(), B,
+                                  Tq, Tk, Hq, Hkv, 128, 0.08838834764831845 if scale is None else scale, int(causal),
+                                  out.data_ptr(), ldo, _ptr(workspace), size, _stream(q))
+    if status:
+        _check(status, "sq_attn_prompt")
     return out
