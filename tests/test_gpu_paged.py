@@ -290,6 +290,43 @@ def test_paged_attention_of_small_and_large_values(scale_v):
     attention_close(got, want, weight, 2e-5)
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+def test_paged_attention_of_values_that_cancel(bits):
+    """Sums of the codes are as exact as fp32 beside a much larger weight: values whose mean is 0 give 0.
+
+    Of four tokens one has weight 2^12 and value 1 - 1, two a far smaller weight w, the same for all, and
+    opposite values; the last one's code and value are 0.  w has 11 bits and is at least 2^k = 8, so a
+    multiple of 2^(k - 10).  A wave has one block of 64 tokens of a chunk: its sums of w and codes, whose
+    mean is 2^(bits - 1), are at most 32 2^(bits - 1) 2^(k + 1) + 16 2^12, with 8 bits 2^24 units.  fp32
+    holds them all, so no sum is rounded.
+    """
+    g = rng(14)
+    n, page, heads = 1024, 16, 16
+    middle = 2 ** (bits - 1)
+    table, pages = spread_table(g, [n], page, spare=0)
+    at = np.arange(n) % 4
+    paired = (at == 1) | (at == 2)
+    codes = np.zeros((n, 128), dtype=np.int64)
+    codes[at == 0] = 1
+    half = g.integers(1, 2 * middle, size=(paired.sum() // 2, 128))
+    codes[paired] = np.stack([half, 2 * middle - half], axis=1).reshape(-1, 128)
+    params = np.zeros((n, 4), dtype=np.float32)
+    params[at > 0, 1] = -8
+    params[:, 2] = 1
+    params[at == 0, 3], params[paired, 3] = -1, -middle
+    cache = {"k_q": np.zeros((pages, 1, page, 16 * bits), dtype=np.uint8), "v_q": np.empty((pages, 1, page, 16 * bits), dtype=np.uint8),
+             "params": np.empty((pages, 1, page, 4), dtype=np.float32)}
+    for c, where in enumerate(table[0]):
+        cache["v_q"][where, 0] = oq.store_codes(codes[c * page:(c + 1) * page].astype(np.uint8), bits)
+        cache["params"][where, 0] = params[c * page:(c + 1) * page]
+    q = np.zeros((1, heads, 128), dtype=np.float16)
+    q[0, :, 0] = np.linspace(7.1, 8.9, heads) * np.log(2) / 8  # pairs of weight 2^(12 - 7.1) .. 2^(12 - 8.9)
+    want, _ = opg.attn_paged(q, cache, [n], table, n, 1.0)
+    assert np.abs(want).max() < 1e-12
+    got = sq.attn_paged(up(q), device_cache(cache), ints(table), ints([n]), n, scale=1.0)
+    assert torch.all(got == 0), got.abs().max()
+
+
 PROMPT = [  # Hq, Hkv, queries, keys
     (2, 2, [1], [1]),
     (4, 1, [5, 0, 1, 64, 65], [5, 0, 1, 64, 65]),
