@@ -69,10 +69,10 @@ const char* sq_last_error(void);
  * sq_time_next_call -- measurement hook, not part of the method.  Arms two events for
  * the next call of sq_had_quant_act(_ex), sq_pack_w4(_ex), sq_w4a4_linear, sq_w4a8_linear,
  * sq_w4a4_linear_swiglu, sq_qk_had_kvquant(_ex), sq_attn_decode_kv4(_ex),
- * sq_rope_kv_write, sq_kv_read, sq_attn_paged or sq_attn_prompt made by this host thread: start_event takes the start time of the first kernel that
- * call launches and stop_event the end time of its last kernel (hipExtLaunchKernel
- * events), so hipEventElapsedTime(start, stop) is the call's time on the device without
- * marker packets between kernels.
+ * sq_rope_kv_write, sq_kv_read, sq_attn_paged or sq_attn_prompt made by this host thread:
+ * start_event takes the start time of the first kernel that call launches and stop_event
+ * the end time of its last kernel (hipExtLaunchKernel events), so hipEventElapsedTime(start,
+ * stop) is the call's time on the device without marker packets between kernels.
  *   start_event, stop_event   hipEvent_t, created by the caller with timing enabled
  * The events are consumed by that next call whatever its outcome; a call that returns
  * an error, or enqueues nothing (M == 0), leaves them as they were.
@@ -448,7 +448,8 @@ sq_status sq_rope_kv_write(const void* q, int64_t ldq, const void* k, int64_t ld
  * eq. 1, rounded to fp16, in packed rows, as sq_attn_prompt reads them.
  *   T          >= 0 rows (0 is a no-op), < 2^31
  *   plain_basis  0: keys as stored, in R3's basis (for rotated queries); 1: turned back
- *   k, v       device fp16 [T, ldk], [T, ldv]: Hkv heads of D, 16-byte aligned
+ *   k, v       device fp16 [T, ldk], [T, ldv]: Hkv heads of D, 16-byte aligned; the spans of the two,
+ *              gaps between rows included, must not overlap
  * Errors as sq_rope_kv_write.
  */
 sq_status sq_kv_read(const int32_t* cu, const int32_t* lens, int64_t B, int64_t T,
@@ -462,12 +463,15 @@ sq_status sq_kv_read(const int32_t* cu, const int32_t* lens, int64_t B, int64_t 
  * follows sq_rope_kv_write for generated tokens:
  *     out[b,h,:] = fp16( sum_t softmax_t(scale * q[b,h,:] . K_t) V_t ),  t < min(lens[b], max_len),
  * K_t and V_t of key/value head h / (Hq / Hkv).  A sequence without tokens (or without pages) gets
- * zeros.  No parameter alpha of the cache may be negative (the library writes none).
+ * zeros.  The parameters v_alpha of these tokens must be positive, 2^-60 or more (the library writes
+ * no others from fp16 values; with 0 the result is NaN): a token's weight and v_alpha go into one fp16
+ * factor.  A token whose softmax weight times v_alpha is below 2^-26 of the sequence's largest such
+ * product counts with less than that factor's 11 bits, below 2^-38 not at all.
  *   q          device fp16 [B, ldq]: Hq heads of D, 16-byte aligned (q_rot of the write)
  *   B          >= 0 (0 is a no-op), B * Hq < 2^24
  *   max_len    1 <= max_len < 2^30, at least the longest length: it fixes the split of the sequence and
  *              with it the workspace and the order of additions
- *   scale      finite score scale, e.g. 1/sqrt(128)
+ *   scale      finite score scale, at most 2^40 in size, e.g. 1/sqrt(128)
  *   out        device fp16 [B, ldo]: Hq heads of D, 16-byte aligned
  *   workspace  device memory, 16-byte aligned, at least the bytes sq_attn_paged_workspace gives (NULL
  *              allowed when that is 0); scratch, must not overlap any argument; calls that share
@@ -498,7 +502,7 @@ sq_status sq_attn_paged_workspace(int64_t B, int64_t max_len, int64_t Hq, int64_
  *              the end).  Rows of q outside the sequences are left as they were in out.
  *   Tq, Tk     >= 0, < 2^31 (Tq == 0 or B == 0 is a no-op; with Tk == 0 k and v may be NULL)
  *   Hq, Hkv    1 <= Hkv <= Hq <= 2^16, Hq % Hkv == 0; Tq * Hq + 256 * B * Hkv < 2^31
- *   scale      finite score scale
+ *   scale      positive finite score scale, at most 2^40
  *   out        device fp16 [Tq, ldo]: Hq heads of D, 16-byte aligned
  *   workspace  as in sq_attn_paged, sized by sq_attn_prompt_workspace (0 where there are rows enough
  *              to fill the device)

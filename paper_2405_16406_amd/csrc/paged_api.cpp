@@ -29,8 +29,12 @@ sq_status check_heads(int64_t Hq, int64_t Hkv, int64_t D) {
   return SQ_OK;
 }
 
-sq_status check_scale(float scale) {
-  if (!(std::fabs(scale) < 3.0e38f)) return fail(SQ_ERR_SHAPE, "scale must be finite");
+// The kernels multiply by log2(e) scale, the paged one by 2^24 more: kMostScale keeps both finite.
+constexpr float kMostScale = 1099511627776.0f;  // 2^40
+sq_status check_scale(float scale, bool positive) {
+  if (!(std::fabs(scale) <= kMostScale)) return fail(SQ_ERR_SHAPE, "scale must be finite and at most 2^40 in size");
+  // (the prompt kernel takes the maximum of the unscaled scores)
+  if (positive && !(scale > 0.0f)) return fail(SQ_ERR_SHAPE, "scale must be positive");
   return SQ_OK;
 }
 
@@ -264,7 +268,7 @@ sq_status sq_attn_paged(const void* q, int64_t ldq, const int32_t* lens, int64_t
   sq_status s = check_cache(block_table, ld_table, max_blocks, k_q, v_q, params, pages, page, Hkv, D, bits, param_bits, lens, B,
                             a.cache, codes, pbytes);
   if (s != SQ_OK || (s = check_paged_sizes(B, max_len, Hq, Hkv, D)) != SQ_OK || (s = check_ld(ldq, Hq, "ldq")) != SQ_OK ||
-      (s = check_ld(ldo, Hq, "ldo")) != SQ_OK || (s = check_scale(scale)) != SQ_OK)
+      (s = check_ld(ldo, Hq, "ldo")) != SQ_OK || (s = check_scale(scale, false)) != SQ_OK)
     return s;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16))
     return fail(SQ_ERR_ALIGN, "q, out and the workspace need 16-byte alignment");
@@ -312,7 +316,7 @@ sq_status sq_attn_prompt(const void* q, int64_t ldq, const void* k, int64_t ldk,
   if (!q || !out || !cu_q || !cu_k || (Tk > 0 && (!k || !v))) return fail(SQ_ERR_NULL, "q, k, v, cu_q, cu_k and out are required");
   sq_status s = check_prompt_sizes(B, Tq, Tk, Hq, Hkv, D);
   if (s != SQ_OK || (s = check_ld(ldq, Hq, "ldq")) != SQ_OK || (s = check_ld(ldk, Hkv, "ldk")) != SQ_OK ||
-      (s = check_ld(ldv, Hkv, "ldv")) != SQ_OK || (s = check_ld(ldo, Hq, "ldo")) != SQ_OK || (s = check_scale(scale)) != SQ_OK)
+      (s = check_ld(ldv, Hkv, "ldv")) != SQ_OK || (s = check_ld(ldo, Hq, "ldo")) != SQ_OK || (s = check_scale(scale, true)) != SQ_OK)
     return s;
   if (causal != 0 && causal != 1) return fail(SQ_ERR_UNSUPPORTED, "causal=%d: 0 and 1 are implemented", causal);
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(cu_q, 4) ||

@@ -171,6 +171,21 @@ def test_no_device_is_a_hip_error(L):
     assert L.sq_attn_paged_workspace(1, 64, 8, 2, 128, ctypes.byref(n)) == sq.SQ_ERR_HIP
 
 
+@pytest.mark.parametrize("call,kw,ok", [
+    (paged, dict(scale=2.0 ** 40 * 1.001), False), (paged, dict(scale=-2.0 ** 41), False), (paged, dict(scale=3e38), False),
+    (paged, dict(scale=-0.1, B=0), True), (paged, dict(scale=0.0, B=0), True), (paged, dict(scale=2.0 ** 40, B=0), True),
+    (prompt, dict(scale=0.0), False), (prompt, dict(scale=-0.1), False), (prompt, dict(scale=-0.0), False),
+    (prompt, dict(scale=2.0 ** 40 * 1.001), False), (prompt, dict(scale=2.0 ** 40, B=0), True)])
+def test_scales(L, call, kw, ok):
+    """Scales whose base-2 factor overflows, and those that turn the order of a prompt's scores around."""
+    assert call(L, **kw) == (sq.SQ_OK if ok else sq.SQ_ERR_SHAPE)
+
+
+def test_read_into_one_tensor(L):
+    """Two outputs in one tensor's rows: their spans overlap."""
+    assert read(L, k=fake(1), ldk=512, v=fake(1, 512), ldv=512) == sq.SQ_ERR_ALIAS
+
+
 def test_binding_refuses_host_tensors():
     x = torch.zeros((2, 4, 128), dtype=torch.float16)
     lens = torch.ones(2, dtype=torch.int32)

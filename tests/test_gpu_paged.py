@@ -327,6 +327,37 @@ def test_paged_attention_of_values_that_cancel(bits):
     assert torch.all(got == 0), got.abs().max()
 
 
+@pytest.mark.parametrize("scale", [-0.1, 0.0])
+def test_paged_attention_of_scales_not_positive(scale):
+    g = rng(15)
+    lens, page = [150, 1, 0], 16
+    table, pages = spread_table(g, lens, page)
+    cache = filled(g, pages, 2, page, 4, np.float32)
+    q = heads_of(g, 3, 8)
+    got = sq.attn_paged(up(q), device_cache(cache), ints(table), ints(lens), 150, scale=scale)
+    want, weight = opg.attn_paged(q, cache, lens, table, 150, scale)
+    attention_close(got, want, weight, 2e-5)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_paged_attention_of_value_scales_far_apart(bits):
+    """Tokens whose values are 2^-18 of the others' keep their part in the softmax's sum.
+
+    Their fp16 factor, weight times v_alpha, is 2^12 at the largest product: with scores within 4 of
+    each other in base 2, and v_alpha within 2^2 of each other but for the 2^-18, it is 2^-12 or
+    more, a normal number.
+    """
+    g = rng(16)
+    lens, page = [600], 16
+    table, pages = spread_table(g, lens, page)
+    cache = filled(g, pages, 2, page, bits, np.float32)
+    cache["params"][:, :, ::3, 2:] *= 2.0 ** -18
+    q = heads_of(g, 1, 8, 0.2)
+    got = sq.attn_paged(up(q), device_cache(cache), ints(table), ints(lens), 600)
+    want, weight = opg.attn_paged(q, cache, lens, table, 600)
+    attention_close(got, want, weight, 2e-5)
+
+
 PROMPT = [  # Hq, Hkv, queries, keys
     (2, 2, [1], [1]),
     (4, 1, [5, 0, 1, 64, 65], [5, 0, 1, 64, 65]),
