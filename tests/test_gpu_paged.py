@@ -543,6 +543,92 @@ def test_another_stream_and_two_workspaces():
     assert torch.equal(got, want) and torch.equal(other, want)
 
 
+def test_two_graphs_that_share_a_workspace():
+    """Replayed in any order on one stream, with lengths that change and other work between them."""
+    g = rng(42)
+    page, most, Hq, H = 16, 2000, 16, 2
+    n = max(sq.attn_paged_workspace_bytes(b, most, Hq, H) for b in (1, 3))
+    pq, pk = [5, 20], [1500, 1900]
+    n = max(n, sq.attn_prompt_workspace_bytes(2, sum(pq), sum(pk), Hq, H))
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    calls = []
+    for B, bits in ((1, 4), (3, 8)):
+        table, pages = spread_table(g, [most] * B, page)
+        dc, dt, dl = device_cache(filled(g, pages, H, page, bits, np.float32)), ints(table), ints([most] * B)
+        q, out = up(heads_of(g, B, Hq)), torch.empty((B, Hq, 128), dtype=torch.float16, device=DEV)
+        calls.append((dl, out, lambda q=q, dc=dc, dt=dt, dl=dl, out=out, ws=ws: sq.attn_paged(q, dc, dt, dl, most, out=out, workspace=ws)))
+    q, k, v = up(heads_of(g, sum(pq), Hq)), up(heads_of(g, sum(pk), H)), up(heads_of(g, sum(pk), H))
+    cq, ck = ints([0, *np.cumsum(pq)]), ints([0, *np.cumsum(pk)])
+    out = torch.empty_like(q)
+    calls.append((None, out, lambda: sq.attn_prompt(q, k, v, cq, ck, out=out, workspace=ws)))
+    assert sq.attn_prompt_workspace_bytes(2, sum(pq), sum(pk), Hq, H) > 0
+    graphs = []
+    for _, _, call in calls:
+        call()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call()
+    for step in range(4):
+        for dl, out, _ in calls:
+            out.fill_(7.0)
+            if dl is not None:
+                dl.copy_(ints([[1, 700, most, 64][(step + b) % 4] for b in range(dl.numel())]))
+        for i in ((0, 1, 2), (2, 1, 0), (1, 0, 2), (0, 2, 1))[step]:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        got = [out.clone() for _, out, _ in calls]
+        for (_, out, call), have in zip(calls, got):
+            assert torch.equal(call(), have)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_pages_beyond_32_bits(bits):
+    """Codes and parameters that lie behind the pool's first 4 GiB of each."""
+    g = rng(43)
+    H, page, n = 2, 64, 300
+    table, used = spread_table(g, [n], page)
+    small = filled(g, used, H, page, bits, np.float32)
+    pages = (1 << 32) // (H * page * 16) + 3 * used  # 4 GiB of parameters, 16 or 32 of codes
+    dc = [torch.empty((pages, *small[x].shape[1:]), dtype=t, device=DEV) for x, t in
+          (("k_q", torch.uint8), ("v_q", torch.uint8), ("params", torch.float32))]
+    for t, x in zip(dc, ("k_q", "v_q", "params")):
+        t[-used:] = up(small[x])
+    far = ints(table + pages - used)
+    near = device_cache(small)
+    q, k, v = up(heads_of(g, 1, 4)), up(heads_of(g, 1, H)), up(heads_of(g, 1, H))
+    results = []
+    for cache, dt in ((near, ints(table)), (dc, far)):
+        qr = sq.rope_kv_write(q, k, v, cache, dt, ints([n]), sq.rope_frequencies(device=DEV))
+        out = sq.attn_paged(qr, cache, dt, ints([n]), n)
+        kk, vv = sq.kv_read(cache, dt, ints([n]), ints([0, n]), n)
+        results.append([qr, out, kk, vv, *(t[-used:] for t in cache)])
+    torch.cuda.synchronize()
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_prompt_rows_beyond_32_bits():
+    """Sequences of q, k, v and out whose rows lie behind 4 GiB."""
+    g = rng(44)
+    Hq, H, n, m, wide = 4, 2, 40, 150, 1 << 15
+    rows = (1 << 32) // (2 * wide) + 200
+    q, k, v = (heads_of(g, x, h) for x, h in ((n, Hq), (m, H), (m, H)))
+    # (the division of the keys goes by the rows of all k: not the bits of a call on the rows alone)
+    want, weight, _ = opg.attn_prompt(q, k, v, [0, n], [0, m])
+    # the four tensors are columns of one each, so that a row is 64 KiB
+    far = []
+    for x, h in ((q, Hq), (k, H), (v, H)):
+        t = torch.empty((rows, wide), dtype=torch.float16, device=DEV)[:, :h * 128].unflatten(1, (h, 128))
+        t[rows - len(x):] = up(x)
+        far.append(t)
+    out = torch.full((rows, wide), 7.0, dtype=torch.float16, device=DEV)[:, :Hq * 128].unflatten(1, (Hq, 128))
+    sq.attn_prompt(*far, ints([rows - n, rows]), ints([rows - m, rows]), out=out)
+    torch.cuda.synchronize()
+    attention_close(out[-n:], want, weight, prompt_scores(q, k, 128 ** -0.5))
+    assert torch.all(out[:-n] == 7.0)
+
+
 def test_empty_calls():
     cache, dt = sq.kv_cache(1, 16, 2), torch.zeros((0, 1), dtype=torch.int32, device=DEV)
     none = torch.empty((0, 2, 128), dtype=torch.float16, device=DEV)
