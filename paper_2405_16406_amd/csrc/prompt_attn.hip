@@ -436,14 +436,28 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       whole(j, 1);
       whole(j + 1, 0);
     }
-    for (; j < nw; ++j) {  // (and a whole tile left over)
-      values(tile_of(j - 1), (j - 1) & 1, std::true_type{});
+    if (j < nf) {
+      whole(j, 1);
+      ++j;
+    }
+    // Tiles with keys that some row does not see.  A masked tile's values are read twice (for those
+    // that are not finite), so whole ones are taken apart here too, and the one left over above:
+    // 2048 tokens of 32 heads 53 -> 49 us, 16 packed prompts 447 -> 431, 37 and 4 tokens over 16000
+    // and 6000 keys 39.7 -> 36.4.
+    for (; j < nw; ++j) {
+      if (j > nf)
+        values(tile_of(j - 1), (j - 1) & 1, std::true_type{});
+      else
+        values(tile_of(j - 1), (j - 1) & 1, std::false_type{});
       scores(j & 1);
       end_products(j);
       softmax(tile_of(j), std::true_type{});
       end_softmax();
     }
-    values(tile_of(nw - 1), (nw - 1) & 1, std::true_type{});
+    if (nw > nf)
+      values(tile_of(nw - 1), (nw - 1) & 1, std::true_type{});
+    else
+      values(tile_of(nw - 1), (nw - 1) & 1, std::false_type{});
   }
   for (int j = nw; j < n; ++j) {  // other waves' tiles
     end_products(j);
