@@ -38,11 +38,11 @@ constexpr int kPromptTile = 64;   // keys of its step
 // Prompts.  half: workgroups of half the rows, whose two groups of waves share the keys.  splits > 1:
 // the keys go out in parts of `per` tiles (more where a sequence would have over `splits` of them).
 //   Workgroups of 256 rows for more of them than compute units: they move the fewest bytes through
-//   the caches (prompt of 4096 tokens of 32 heads: 149 us, halves 166; 8192: 522, 571).
-//   Up to one a compute unit, the longest of a causal prompt decides: halves (2048 tokens 54 us,
-//   whole 60; 1024: 25, 36; 512: 18, 26).
+//   the caches (prompt of 4096 tokens of 32 heads: 143 us, halves 158; 8192: 517, 560).
+//   Up to one a compute unit, the longest of a causal prompt decides: halves (2048 tokens 50 us,
+//   whole 57; 1024: 24, 33; 512: 16, 23).
 //   Few rows over many keys: parts, a unit each, where by the estimate below they are through
-//   sooner, partial states included (37 and 4 tokens over 16000 and 6000 keys of 8 heads 37 us).
+//   sooner, partial states included (37 and 4 tokens over 16000 and 6000 keys of 8 heads 34 us).
 struct PromptPlan {
   int32_t half, splits, per;
 };

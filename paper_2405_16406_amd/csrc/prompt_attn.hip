@@ -20,6 +20,13 @@
 // bytes; its 16-byte chunk c lies at c xor swizzle(row), so that neither the 16 rows of a K read
 // nor the 4 x 64 bytes of a transposed read of V meet on a bank.
 // Weights are rounded to fp16 (2^-12 of the weight, as the output is); sums stay in fp32.
+// The matrix cores bound it where there are rows and keys enough: 2048 tokens behind 32768 (64
+// heads on 8) take 1950 us, 1.16 PFLOP/s, the rate a large library product reaches on the card.
+// Shorter prompts pay each workgroup's start (find the tile, the first keys and queries, with nothing
+// to run beside it, since the registers hold one workgroup a compute unit), the first scores and last
+// values alone, and the half of a causal prompt's last tile that nothing sees; a prompt of one tile
+// takes 7 us, and a tile of a long one 1.8.  16 packed prompts of 292 .. 4000 tokens, 32 heads on 8,
+// 431 us (0.9 PFLOP/s), 2048 tokens of 32 heads 49 us (0.7).
 //
 // Few rows over many keys (a follow-up question on a long document) would leave most of the chip
 // idle: the keys are then split over workgroups, whose fp32 states a second kernel joins.
