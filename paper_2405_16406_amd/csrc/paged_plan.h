@@ -13,7 +13,7 @@ constexpr int kPagedBlock = 64;   // tokens of a wave's step
 //   One sequence: two workgroups for each of `cus` compute units, one round of equal ones (131071
 //   tokens of 8 heads, us with the join: chunks of 2048 tokens 34, 1536 37, 8192 54).
 //   Several: their lengths differ as a rule, so four times as many, the sequences' short last chunks
-//   among them filling up at the end (64 sequences of 512 .. 8192 tokens, 8 heads: 2048 51, 8192 75;
+//   among them filling up at the end (64 sequences of 512 .. 8192 tokens, 8 heads: 2048 53, 8192 77;
 //   equal lengths lose by it, 64 of 2432: 43, uncut 38).  Chunks of one step for each wave only where
 //   there is nothing better to do for the compute units (16 sequences, 8 heads: 512 15, 256 16).
 // The lengths lie on the device, so the plan goes by the longest.

@@ -21,12 +21,15 @@
 // nor the 4 x 64 bytes of a transposed read of V meet on a bank.
 // Weights are rounded to fp16 (2^-12 of the weight, as the output is); sums stay in fp32.
 // The matrix cores bound it where there are rows and keys enough: 2048 tokens behind 32768 (64
-// heads on 8) take 1950 us, 1.16 PFLOP/s, the rate a large library product reaches on the card.
-// Shorter prompts pay each workgroup's start (find the tile, the first keys and queries, with nothing
-// to run beside it, since the registers hold one workgroup a compute unit), the first scores and last
-// values alone, and the half of a causal prompt's last tile that nothing sees; a prompt of one tile
+// heads on 8) take 1950 us, 1.16 PFLOP/s, the rate a large library product reaches on the card.  They
+// are busy for 67 % of the cycles, at 1.57 GHz: the chip's power sets the clock.  LDS is at 34 %,
+// without bank conflicts.
+// Shorter prompts add what a workgroup does once (find the tile, first keys and queries, first scores
+// and last values alone, stores) and what a causal prompt's last tile wastes: one of a single tile
 // takes 7 us, and a tile of a long one 1.8.  16 packed prompts of 292 .. 4000 tokens, 32 heads on 8,
-// 431 us (0.9 PFLOP/s), 2048 tokens of 32 heads 49 us (0.7).
+// 431 - 439 us (0.9 PFLOP/s, matrix cores busy for 46 % at 1.67 GHz), 2048 tokens of 32 heads 49 - 51
+// us (0.7).  Two workgroups of four waves a compute unit, each with its own keys, would hide one's
+// start behind the other's products: 51 - 52, 442 and 2020 - 2040 us for these three, no gain.
 //
 // Few rows over many keys (a follow-up question on a long document) would leave most of the chip
 // idle: the keys are then split over workgroups, whose fp32 states a second kernel joins.
