@@ -50,6 +50,11 @@ typedef int v2i __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A running maximum of -inf means a state without tokens: the output is zero where all states are.  One
+// with tokens whose scores are all -inf or NaN has kNoScore instead, which weighs as little beside a
+// finite maximum and keeps its sums (0 or NaN: 0 / 0 or NaN in the end, as the definition has it).
+constexpr float kNoScore = -3.402823466e38f;
+
 // 2^(a - b), 0 when a is -inf (an empty state)
 __device__ __forceinline__ float rescale(float a, float b) { return a == -INFINITY ? 0.0f : exp2_fast(__fsub_rn(a, b)); }
 
@@ -202,6 +207,7 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
   };
 
   float m = -INFINITY, l = 0.0f, bsum = 0.0f;
+  uint64_t seen = 0;  // lanes that had a token with a page
   v4f acc[8];
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt) acc[dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
@@ -224,6 +230,7 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
         const int unit = BITS == 4 ? (lane & 3) ^ ((row >> 2) & 3) : (lane & 7) ^ (row & 7);
         *reinterpret_cast<v4u*>(vlds + row * W::ROW + 16 * unit) = vc[mm][x];
       }
+    seen |= __ballot(par_ok);
     const float rva = par_ok ? __fdiv_rn(1.0f, par.z) : 0.0f;
     coef[0 * kBlock + lane] = par_ok ? par.x * cs24 : 0.0f;
     coef[1 * kBlock + lane] = par_ok ? par.y * cs : 0.0f;
@@ -349,6 +356,14 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
   const auto add = [](float u, float v) { return __fadd_rn(u, v); };
   l = rows_all(l, add);
   bsum = rows_all(bsum, add);
+  if (seen == 0) {  // masked tokens alone: a query that is not finite has made their sums NaN
+    m = -INFINITY;
+    l = bsum = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  } else if (m == -INFINITY) {
+    m = kNoScore;
+  }
 
   // the waves' states of each head meet in LDS: dims finished but for the division
   __syncthreads();
