@@ -495,7 +495,8 @@ sq_status sq_attn_paged_workspace(int64_t B, int64_t max_len, int64_t Hq, int64_
  * and m keys, query i (from 0) sees the keys t < m (causal 0) or t <= m - n + i (causal 1): the
  * queries are the last n tokens, so a chunk of a prompt comes with the keys of what went before.
  * A query that sees no key gets zeros.  Values and keys that a query does not see have no part in
- * its result, NaN and infinities among them.
+ * its result, NaN and infinities among them; of what it sees, a NaN score, one of +inf, or none above
+ * -inf makes its result NaN.
  *   q          device fp16 [Tq, ldq]: Hq heads of D;  k, v  device fp16 [Tk, ldk], [Tk, ldv]: Hkv heads
  *              of D; 16-byte aligned
  *   cu_q, cu_k device int32 [B + 1], ascending, within [0, Tq] and [0, Tk] (entries beyond are taken as

@@ -50,11 +50,6 @@ typedef int v2i __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A running maximum of -inf means a state without tokens: the output is zero where all states are.  One
-// with tokens whose scores are all -inf or NaN has kNoScore instead, which weighs as little beside a
-// finite maximum and keeps its sums (0 or NaN: 0 / 0 or NaN in the end, as the definition has it).
-constexpr float kNoScore = -3.402823466e38f;
-
 // 2^(a - b), 0 when a is -inf (an empty state)
 __device__ __forceinline__ float rescale(float a, float b) { return a == -INFINITY ? 0.0f : exp2_fast(__fsub_rn(a, b)); }
 

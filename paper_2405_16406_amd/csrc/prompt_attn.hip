@@ -505,6 +505,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     down |= odds[rw * 128 + 64 + lane];
   }
   if (row >= rows) return;
+  if (mx == -INFINITY && lim >= kt0 * kTile) mx = kNoScore;  // it sees a key of this part, but no score above -inf
   const float inv = SPLIT ? 1.0f : mx == -INFINITY ? 0.0f : __fdiv_rn(1.0f, l);  // a row that sees nothing is zero
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) acc[dt] *= inv;
