@@ -150,6 +150,15 @@ def _need(t: torch.Tensor, dtype, name: str):
         raise TypeError(f"{name} must be a {dtype} tensor on the GPU")
 
 
+def _workspace_bytes(t: torch.Tensor) -> int:
+    """The bytes of a caller's workspace: its elements must lie side by side, since the call writes as
+    many bytes from its first on (those of a strided or expanded one would be other memory)."""
+    if isinstance(t, torch.Tensor) and not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _need(t, torch.uint8, "workspace")
+    return t.numel()
+
+
 def abi_version() -> int:
     return int(lib().sq_abi_version())
 
@@ -361,11 +370,11 @@ def attn_decode_kv4_split(q_rot, k_q, k_alpha, k_beta, v_q, v_alpha, v_beta, sca
     if workspace is None:
         workspace = torch.empty(max(attn_decode_workspace_bytes(B, S, H, D), 1), dtype=torch.uint8,
                                 device=q_rot.device)
-    _need(workspace, torch.uint8, "workspace")
+    size = _workspace_bytes(workspace)
     _check(lib().sq_attn_decode_kv4_split(_ptr(q_rot), _ptr(k_q), _ptr(k_alpha), _ptr(k_beta), _ptr(v_q),
                                           _ptr(v_alpha), _ptr(v_beta), B, S, H, D, float(scale),
                                           {torch.float32: 32, torch.float16: 16}[pdt], _ptr(out), _ptr(workspace),
-                                          workspace.numel(), _stream(q_rot)), "sq_attn_decode_kv4_split")
+                                          size, _stream(q_rot)), "sq_attn_decode_kv4_split")
     return out
 
 
@@ -613,8 +622,7 @@ def attn_paged(q, cache, block_table, lens, max_len: int, scale=None, out=None, 
         size = attn_paged_workspace_bytes(B, max_len, Hq, args[-1])
         workspace = q.new_empty(size, dtype=_U8) if size else None
     else:
-        _need(workspace, _U8, "workspace")
-        size = workspace.numel()
+        size = _workspace_bytes(workspace)
     status = lib().sq_attn_paged(q.data_ptr(), ldq, lens.data_ptr(), B, *args, Hq, 128, *bits, max_len,
                                  0.08838834764831845 if scale is None else scale, out.data_ptr(), ldo, _ptr(workspace), size,
                                  _stream(q))
@@ -659,8 +667,7 @@ def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, 
         size = attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv)
         workspace = q.new_empty(size, dtype=_U8) if size else None
     else:
-        _need(workspace, _U8, "workspace")
-        size = workspace.numel()
+        size = _workspace_bytes(workspace)
     status = lib().sq_attn_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(), cu_k.data_ptr(), B,
                                   Tq, Tk, Hq, Hkv, 128, 0.08838834764831845 if scale is None else scale, int(causal),
                                   out.data_ptr(), ldo, _ptr(workspace), size, _stream(q))

@@ -198,3 +198,13 @@ def test_binding_refuses_host_tensors():
         sq.attn_paged(x, cache, lens[:, None], lens, 16)
     with pytest.raises(TypeError):
         sq.attn_prompt(x, x, x, lens, lens)
+
+
+@pytest.mark.parametrize("bad", [lambda t: t[::2], lambda t: t[:1].expand(64), lambda t: t.view(8, 8).t()], ids=["strided", "expanded", "transposed"])
+def test_workspaces_are_contiguous(bad):
+    """A workspace whose bytes are not side by side is refused before anything else is looked at."""
+    t = torch.zeros(64, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        sq._workspace_bytes(bad(t))
+    with pytest.raises(TypeError):  # on the host
+        sq._workspace_bytes(t)
