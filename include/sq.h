@@ -463,10 +463,12 @@ sq_status sq_kv_read(const int32_t* cu, const int32_t* lens, int64_t B, int64_t 
  * follows sq_rope_kv_write for generated tokens:
  *     out[b,h,:] = fp16( sum_t softmax_t(scale * q[b,h,:] . K_t) V_t ),  t < min(lens[b], max_len),
  * K_t and V_t of key/value head h / (Hq / Hkv).  A sequence without tokens (or without pages) gets
- * zeros, whatever its query holds; with tokens, a query that is not finite gives NaN.  The parameters v_alpha of these tokens must be positive, 2^-60 or more (the library writes
- * no others from fp16 values; with 0 the result is NaN): a token's weight and v_alpha go into one fp16
- * factor.  A token whose softmax weight times v_alpha is below 2^-26 of the sequence's largest such
- * product counts with less than that factor's 11 bits, below 2^-38 not at all.
+ * zeros, whatever its query holds; with tokens, a query that is not finite gives NaN.  The parameters
+ * v_alpha of these tokens must be 2^-60 or more (the library writes no others from fp16 values), or 0
+ * with value codes of 0 (a slot of a zeroed cache that was never written): a token's weight and v_alpha
+ * (1 for 0) go into one fp16 factor.  A token whose softmax weight times
+ * v_alpha is below 2^-26 of the sequence's largest such product counts with less than that factor's 11
+ * bits, below 2^-38 not at all.
  *   q          device fp16 [B, ldq]: Hq heads of D, 16-byte aligned (q_rot of the write)
  *   B          >= 0 (0 is a no-op), B * Hq < 2^24
  *   max_len    1 <= max_len < 2^30, at least the longest length: it fixes the split of the sequence and

@@ -226,6 +226,9 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
         *reinterpret_cast<v4u*>(vlds + row * W::ROW + 16 * unit) = vc[mm][x];
       }
     seen |= __ballot(par_ok);
+    // A slot of a zeroed cache that was never written: its codes are 0, so any scale gives its values.
+    // (Codes of such tokens are not looked at: a branch that clears them in LDS costs 3 % and a spill.)
+    par.z = par.z == 0.0f ? 1.0f : par.z;
     const float rva = par_ok ? __fdiv_rn(1.0f, par.z) : 0.0f;
     coef[0 * kBlock + lane] = par_ok ? par.x * cs24 : 0.0f;
     coef[1 * kBlock + lane] = par_ok ? par.y * cs : 0.0f;
