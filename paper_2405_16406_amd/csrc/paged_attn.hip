@@ -16,10 +16,10 @@
 //             tokens 16 g .. 16 g + 15 of the block: products j = 0 .. 3 hold the tokens
 //             16 (row / 4) + 4 j + row % 4.
 //   softmax   in base 2.  V's scale goes into the weight, w_t = 2^(s_t + log2 va_t - m), with m
-//             the running maximum of that exponent: the fp16 weights of the second product are
-//             then near 1 at their largest whatever the size of V.  The sums are
+//             kWeightBits below the running maximum of that exponent: the fp16 weights of the second
+//             product are then near 2^12 at their largest whatever the size of V.  The sums are
 //             l = sum w_t / va_t and b = sum w_t vb_t / va_t in fp32.  m moves
-//             (and everything is rescaled) only when it would grow by more than kSlack.
+//             (and everything is rescaled) only when the largest would grow by more than 2^kSlack.
 //   values    O^T += V^T w^T: the block's value codes go through LDS as they are (64 or 128
 //             bytes a token) and come back transposed (ds_read_b64_tr_b4 / _b8): lane (i, g)
 //             gets the codes of dim 16 dt + i of its 16 tokens, the order its weights are in.
@@ -43,6 +43,9 @@ constexpr int kWaves = kPagedWaves;
 constexpr int kBlock = kPagedBlock;  // tokens of a wave's step
 constexpr float kSlack = 3.0f;      // log2: weights stay below 2^(kWeightBits + kSlack) < 65504
 constexpr float kWeightBits = 12.0f;
+// Exponents of this size have steps of 1/2: from there on m is the maximum itself, since kWeightBits
+// below it might be rounded to more than fp16 holds (the differences s - m themselves are exact).
+constexpr float kLargeScore = 4194304.0f;  // 2^22
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -284,8 +287,8 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
       }
     }
     top = rows_all(top, [](float u, float v) { return fmaxf(u, v); });
-    if (__ballot(top > m + kSlack)) {  // (m = -inf: any token)
-      const float mn = fmaxf(m, top);
+    if (__ballot(top - m > kWeightBits + kSlack)) {  // (m = -inf: any token)
+      const float mn = fmaxf(m, fabsf(top) < kLargeScore ? top - kWeightBits : top);
       const float f = rescale(m, mn);
       l *= f;
       bsum *= f;
@@ -297,7 +300,7 @@ attn_paged_part(const uint16_t* q, const int32_t* lens, int chunks, int tiles, u
     // rounding then moves the mean of the values seen by 2^-12 of their spread; against unrounded
     // sums it would be 2^-12 of sum w e, whose bulk cancels against b (errors of the output 0.4 -
     // 0.8e-3 over long caches instead of 0.2 - 0.3e-3).
-    const float base = (m == -INFINITY ? 0.0f : m) - kWeightBits;
+    const float base = m == -INFINITY ? 0.0f : m;
     uint32_t pw[8];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {

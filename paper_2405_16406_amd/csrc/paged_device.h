@@ -7,9 +7,10 @@
 
 namespace sq {
 
-// A softmax's running maximum of -inf means a state without tokens: the output is zero where all states are.  One
-// with tokens whose scores are all -inf or NaN has kNoScore instead, which weighs as little beside a
-// finite maximum and keeps its sums (0 or NaN: 0 / 0 or NaN in the end, as the definition has it).
+// A softmax state is sums of 2^(s - m), m at or near the running maximum of s.  With m = -inf it has no
+// token: the output is zero where all states are such.  One with tokens whose scores are all -inf or
+// NaN has m = kNoScore instead, which weighs as little beside a finite m and keeps its sums (0 or NaN:
+// 0 / 0 or NaN in the end, as the definition has it).
 constexpr float kNoScore = -3.402823466e38f;
 
 // value of the lane whose quad index is this lane's xor M (M = 1 or 2)
