@@ -10,8 +10,9 @@
 //   scores   S^T = K Q^T by 32x32x16 products.  A lane then holds 32 of a tile's 64 scores of ONE
 //            row (lane % 32), so the softmax's maximum and sum are in the lane but for one
 //            exchange of the wave's halves, and its factors are one value a lane.
-//   softmax  in base 2, running maximum m and sum l in fp32.  m moves, and the output is rescaled,
-//            only where it would grow by more than kSlack.
+//   softmax  in base 2 and fp32: weights 2^(s - m), their sum l, m kWeightBits below the running
+//            maximum.  m moves, and the output is rescaled, only where the largest weight would grow
+//            by more than 2^kSlack.
 //   values   O^T += V^T P^T.  The slots of the product's inner index may hold the keys in any
 //            order, the same for both operands: in the order in which the first product leaves
 //            the scores, the rounded weights are an operand as they are; V comes from LDS by
@@ -45,6 +46,10 @@ constexpr int kTile = kPromptTile;          // keys of a tile
 constexpr int kTileBytes = kTile * 256;     // of K, and of V
 constexpr float kSlack = 8.0f;              // log2: weights stay below 2^(kWeightBits + kSlack) < 65504
 constexpr float kWeightBits = 7.0f;         // the largest weight when m has just moved
+// Scores of this size have steps of 1/2.  From there on m is the maximum itself, since kWeightBits below
+// it might be rounded to more than fp16 holds, and a weight is that of the rounded score, not of the
+// exact product with the scale, which may be far above the rounded maximum: both gave NaN.
+constexpr float kLargeScore = 4194304.0f;   // 2^22
 
 // KG groups of waves share a workgroup's rows and take its tiles of keys in turn.
 template <int KG>
@@ -254,6 +259,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
   const float cs = a.scale_log2e;
+  bool large = false;  // a row of the wave has m beyond kLargeScore
   v16f s[2];   // scores of a tile: keys 32 mt + 8 (r / 4) + 4 h + r % 4
   v8h pf[4];   // its weights, an operand of the second product
 
@@ -287,15 +293,22 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[1][r]);
     top = halves(top, [](float x, float y) { return fmaxf(x, y); }) * cs;
-    if (__builtin_expect(__ballot(top > mx + kSlack) != 0, 0)) {  // (mx = -inf: any score)
-      const float mn = fmaxf(mx, top);
+    if (__builtin_expect(__ballot(top - mx > kWeightBits + kSlack) != 0, 0)) {  // (mx = -inf: any score)
+      const float mn = fmaxf(mx, fabsf(top) < kLargeScore ? top - kWeightBits : top);
       const float f = rescale(mx, mn);
       l *= f;
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt) acc[dt] *= f;
       mx = mn;
+      large = __ballot(fabsf(mx) >= kLargeScore && mx != -INFINITY) != 0;
     }
-    const float base = (mx == -INFINITY ? 0.0f : mx) - kWeightBits;
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    float cw = cs;
+    if (__builtin_expect(large, 0)) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) s[r >> 4][r & 15] *= cs;
+      cw = 1.0f;
+    }
     // the sum is that of the rounded weights: their rounding then moves the mean of the values
     // seen, not its size
     float l0 = 0.0f, l1 = 0.0f;
@@ -305,8 +318,8 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       uint32_t p[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float x = exp2_fast(__fmaf_rn(s[ks >> 1][8 * (ks & 1) + 2 * r], cs, -base));
-        const float y = exp2_fast(__fmaf_rn(s[ks >> 1][8 * (ks & 1) + 2 * r + 1], cs, -base));
+        const float x = exp2_fast(__fmaf_rn(s[ks >> 1][8 * (ks & 1) + 2 * r], cw, -base));
+        const float y = exp2_fast(__fmaf_rn(s[ks >> 1][8 * (ks & 1) + 2 * r + 1], cw, -base));
         p[r] = f2h2(x, y);
         float& lr = r & 1 ? l1 : l0;
         lr = __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, p[r]), ones, lr, false);

@@ -12,7 +12,7 @@ import pytest
 
 from oracle import paged as opg
 from paper_2405_16406_amd import sq
-from test_gpu_paged import attention_close, device_cache, filled, ints, rng, spread_table, up
+from test_gpu_paged import attention_close, device_cache, filled, heads_of, ints, rng, spread_table, up
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,27 @@ def test_paged_attention_of_large_scores(power, lens, most, sign, bits):
     got = sq.attn_paged(up(q), device_cache(cache), ints(table), ints(lens), most, scale=scale)
     want, weight = opg.attn_paged(q, cache, lens, table, most, scale)
     attention_close(got, want, weight, 2e-5)
+
+
+# rows and keys, heads: each form of the prompt's division (halves, whole tiles, parts)
+PROMPT_FORMS = {"halves": ([200, 40], [300, 40], 2), "whole": ([90, 10], [130, 10], 300), "parts": ([40, 3], [3000, 3], 2)}
+
+
+@pytest.mark.parametrize("form", PROMPT_FORMS)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("power", [16, 20, 24, 25, 26, 28, 30, 39])
+def test_prompt_attention_of_large_scores(power, sign, form):
+    """Scores are +-(1 + j) scale, j from 0 to 2046: exact in the products, rounded once by the scale, and
+    at least 2^16 apart unless equal."""
+    nq, nk, H = PROMPT_FORMS[form]
+    g = rng(72)
+    cu_q, cu_k = (np.concatenate([[0], np.cumsum(n)]) for n in (nq, nk))
+    n, m = int(cu_q[-1]), int(cu_k[-1])
+    q, k, v = np.zeros((n, H, 128), np.float16), heads_of(g, m, H), heads_of(g, m, H)
+    k[:, :, 9] = sign * (1 + np.stack([g.permutation(m) % 2047 for _ in range(H)], axis=1))
+    q[:, :, 9] = 1
+    q[::3, :, 9] = 0  # rows of ordinary scores among them
+    scale = 1.37 * 2.0 ** power
+    got = sq.attn_prompt(up(q), up(k), up(v), ints(cu_q), ints(cu_k), scale=scale)
+    want, weight, _ = opg.attn_prompt(q, k, v, cu_q, cu_k, scale)
+    attention_close(got, want, weight, 2.0 ** -18)
