@@ -25,6 +25,7 @@
 // fifths are written, in 37 us with everything cold (4.6 TB/s) and 28 us with three inputs in turn;
 // 32236 tokens of 8 heads, 8 bits, turned back, 200 MB in 44 and 36 us.
 #include "paged_device.h"
+#include "paged_plan.h"
 #include "sq_internal.h"
 
 namespace sq {
@@ -41,16 +42,6 @@ __device__ __forceinline__ void widen8(const v4u& raw, F* e) {
     e[2 * i + 1] = static_cast<F>(h2f(static_cast<uint16_t>(raw[i] >> 16)));
   }
 }
-
-// Waves' worth of vectors of n tokens: 16 queries, 8 keys or 16 values each.
-struct RopeTasks {
-  int q, k, v;
-  __host__ __device__ int all() const { return q + k + v; }
-};
-__host__ __device__ inline RopeTasks rope_tasks(int n, int hq, int hkv) {
-  return {(n * hq + 15) / 16, (n * hkv + 7) / 8, (n * hkv + 15) / 16};
-}
-constexpr int kRopeWaves = 8;  // of a workgroup at most
 
 // How the pairs of a head vector lie in the lanes' registers.
 enum RopeForm {
@@ -416,18 +407,9 @@ kv_read(const int32_t* cu, const int32_t* lens, int64_t t_first, KvReadArgs a) {
 }  // namespace
 
 hipError_t launch_rope_kv_write(RopeWriteArgs a, hipStream_t stream) {
-  // Many rows: workgroups of four waves with up to four tasks each, the next one's vectors on their
-  // way while one is worked on, as long as 1024 of them (four a CU) are left.  Few rows (a decode
-  // step): a wave for each task, for the shortest way through.  Measured, us with the read back:
-  // 17034 rows of 32 + 32 heads 237 (four waves of four tasks), 241 (eight of four), 284 (sixteen
-  // of one).
-  constexpr int kMany = 1024, kLoop = 4;
-  const auto tasks_of = [&](int n) { return rope_tasks(n, a.hq, a.cache.heads).all(); };
-  int tokens = 1;
-  while (2 * tokens <= kRopeTokens && a.T >= 2 * tokens * kMany && tasks_of(2 * tokens) <= kLoop * kLoop) tokens *= 2;
+  const RopePlan plan = rope_plan(a.T, a.hq, a.cache.heads);
+  const int tokens = plan.tokens, threads = 64 * plan.waves;
   a.tokens = tokens;
-  const int most = a.T >= kMany ? kLoop : kRopeWaves, tasks = tasks_of(tokens);
-  const int threads = 64 * (tasks < most ? tasks : most);
   a.magic_hq = div_magic(static_cast<uint32_t>(a.hq));
   a.magic_hkv = div_magic(static_cast<uint32_t>(a.cache.heads));
   const int form = a.rotary == 0     ? kNoRope

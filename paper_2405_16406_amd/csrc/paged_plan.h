@@ -1,10 +1,40 @@
-// How the attention over the paged cache and over prompts is split over workgroups: sizes alone
-// (no HIP), so that the host compiles and checks it too.
+// How the write of the paged cache and the attention over it and over prompts are split over
+// workgroups: sizes alone (no HIP), so that the host compiles and checks it too.
 #pragma once
 
 #include <cstdint>
 
+#include "paged.h"
+
 namespace sq {
+
+// The write.  A wave's worth of vectors of n tokens (a task): 16 queries, 8 keys or 16 values each.
+struct RopeTasks {
+  int q, k, v;
+  SQ_HOST_DEVICE int all() const { return q + k + v; }
+};
+SQ_HOST_DEVICE RopeTasks rope_tasks(int n, int hq, int hkv) {
+  return {(n * hq + 15) / 16, (n * hkv + 7) / 8, (n * hkv + 15) / 16};
+}
+constexpr int kRopeWaves = 8;   // of a workgroup at most
+constexpr int kRopeTokens = 8;  // tokens of a workgroup at most
+
+// Many rows: workgroups of four waves with up to four tasks each, the next one's vectors on their way
+// while one is worked on, as long as 1024 of them (four a CU) are left.  A CU holds four only of the
+// forms with up to 128 registers (8 bits, or fp16 parameters, with rotary_dim 0 or 128 in halves), else
+// three.  Few rows (a decode step): a wave for each task, for the shortest way through.  Measured, us
+// with the read back: 17034 rows of 32 + 32 heads 237 (four waves of four tasks), 241 (eight of four),
+// 284 (sixteen of one).
+struct RopePlan {
+  int tokens, waves;  // of a workgroup
+};
+inline RopePlan rope_plan(int64_t T, int hq, int hkv) {
+  constexpr int kMany = 1024, kLoop = 4;
+  int tokens = 1;
+  while (2 * tokens <= kRopeTokens && T >= 2 * tokens * kMany && rope_tasks(2 * tokens, hq, hkv).all() <= kLoop * kLoop) tokens *= 2;
+  const int most = T >= kMany ? kLoop : kRopeWaves, tasks = rope_tasks(tokens, hq, hkv).all();
+  return {tokens, tasks < most ? tasks : most};
+}
 
 constexpr int kPagedWaves = 4;    // of a decode workgroup, each on its own
 constexpr int kPagedBlock = 64;   // tokens of a wave's step
@@ -71,10 +101,7 @@ inline PromptPlan prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int32_t hq, int
 }
 
 // Tiles of a part of a sequence (or of a tile of its rows) with `tiles` of them.
-#if defined(__HIPCC__)
-__host__ __device__
-#endif
-inline int32_t prompt_part(int32_t tiles, int32_t splits, int32_t per) {
+SQ_HOST_DEVICE int32_t prompt_part(int32_t tiles, int32_t splits, int32_t per) {
   const int32_t least = (tiles + splits - 1) / splits;
   return per > least ? per : least;
 }

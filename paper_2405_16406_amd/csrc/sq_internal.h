@@ -173,8 +173,7 @@ struct KvArgs {
 
 hipError_t launch_qk_had_kvquant(const KvArgs& a, hipStream_t stream);
 
-// Most tokens of a workgroup of the cache's write and read kernels.
-constexpr int kRopeTokens = 8;
+// Most tokens of a workgroup of the cache's read kernel.
 constexpr int kReadTokens = 64;
 
 struct RopeWriteArgs {

@@ -31,5 +31,11 @@ void prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int32_t hq, int32_t hkv, int
   out[2] = p.per;
 }
 
+void rope_plan(int64_t T, int32_t hq, int32_t hkv, int32_t* out) {
+  const sq::RopePlan p = sq::rope_plan(T, hq, hkv);
+  out[0] = p.tokens;
+  out[1] = p.waves;
+}
+
 int32_t prompt_part(int32_t tiles, int32_t splits, int32_t per) { return sq::prompt_part(tiles, splits, per); }
 }

@@ -116,3 +116,28 @@ def test_every_prompt_form_is_tested(host):
     t = pytest.importorskip("test_gpu_paged")
     plans = [plan_of(host, len(nq), sum(nq) + 3, sum(nk) + 2, hq, h) for hq, h, nq, nk in t.PROMPT]
     assert {(half, splits > 1) for half, splits, _ in plans} == {(0, False), (1, False), (0, True)}
+
+
+def test_every_looping_form_is_tested(host):
+    """The sizes of tests/test_gpu_paged_sizes.py reach writes of several tokens a workgroup and several
+    tasks a wave, waves with several blocks, the join beyond one round of its loads, and each division of a
+    prompt with more than 64 sequences."""
+    t = pytest.importorskip("test_gpu_paged_sizes")
+    out = (ctypes.c_int32 * 2)()
+    for hq, h, *_, rows, tokens in t.WRITE:
+        host.rope_plan(ctypes.c_int64(rows), hq, h, out)
+        assert out[0] == tokens
+    assert {w[-1] for w in t.WRITE} == {1, 2, 4, 8}
+    host.rope_plan(ctypes.c_int64(1100), 64, 8, out)
+    assert out[1] == 4 < 4 + 1 + 1  # waves, tasks
+    blocks, joined = set(), set()
+    for hq, h, _, bits, _, lens, most, _ in t.PAGED:
+        host.paged_split(ctypes.c_int64(len(lens)), ctypes.c_int64(most), hq, h, 256, out)
+        chunks, tokens = out
+        blocks.add((bits, min(tokens, max(lens)) // 256))
+        joined.add((chunks > 8, -(-max(lens) // tokens)))
+    assert {b for b, n in blocks if n >= 3} == {4, 8}
+    assert any(eight and 8 < n <= 64 for eight, n in joined) and any(eight and n > 64 for eight, n in joined)
+    plans = [plan_of(host, len(nq), sum(nq) + 1, sum(nk), hq, h) for hq, h, nq, nk in t.PROMPT]
+    assert [(half, splits > 1) for half, splits, _ in plans] == [(0, False), (1, False), (0, True)]
+    assert all(len(nq) > 64 for _, _, nq, _ in t.PROMPT)
