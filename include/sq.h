@@ -400,7 +400,8 @@ sq_status sq_attn_decode_kv4_split_noalloc(const void* q_rot, const uint8_t* k_q
  * sq_rope_frequencies -- host helper: the angle per position of each pair of dims,
  * f_i = theta^(-2 i / rotary_dim), i < rotary_dim / 2, in out_host[rotary_dim / 2] (HOST memory).
  *   rotary_dim 16 .. 128, a multiple of 16
- *   theta      base, finite and > 0 (a longer base is given here directly)
+ *   theta      base, finite and > 0 (a longer base is given here directly), not so small that an f_i
+ *              overflows
  *   scaling    0: none; 1: positions interpolated, f_i / factor; 2: by parts: with r = original_len
  *              f_i / (2 pi) turns within the original context, f_i is kept where r >= high, divided
  *              by factor where r <= low, and between the two mixed linearly in r

@@ -1,5 +1,6 @@
 // Host side of the paged-cache entry points of include/sq.h: argument validation and launches.
 // Every check runs before anything is enqueued.
+#include <algorithm>
 #include <cmath>
 
 #include "api_check.h"
@@ -135,6 +136,7 @@ sq_status sq_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling,
   if (scaling > 0 && (!(factor >= 1.0) || !std::isfinite(factor))) return fail(SQ_ERR_SHAPE, "factor must be finite and at least 1");
   if (scaling == 2 && (!(low < high) || !std::isfinite(low) || !std::isfinite(high) || !(original_len > 0.0) || !std::isfinite(original_len)))
     return fail(SQ_ERR_SHAPE, "need finite low < high and original_len > 0");
+  double out[64];
   for (int i = 0; i < rotary_dim / 2; ++i) {
     double f = std::pow(theta, -2.0 * i / rotary_dim);
     if (scaling == 1) f /= factor;
@@ -144,8 +146,10 @@ sq_status sq_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling,
       kept = kept < 0.0 ? 0.0 : kept > 1.0 ? 1.0 : kept;
       f = f * kept + f / factor * (1.0 - kept);
     }
-    out_host[i] = f;
+    if (!std::isfinite(f)) return fail(SQ_ERR_SHAPE, "theta=%g: the frequency of pair %d is not finite", theta, i);
+    out[i] = f;
   }
+  std::copy(out, out + rotary_dim / 2, out_host);
   return ok();
 }
 

@@ -208,3 +208,14 @@ def test_workspaces_are_contiguous(bad):
         sq._workspace_bytes(bad(t))
     with pytest.raises(TypeError):  # on the host
         sq._workspace_bytes(t)
+
+
+def test_frequencies_that_overflow(L):
+    """theta^(-126 / 128) of the smallest doubles is infinite; nothing is written then."""
+    buf = np.full(64, 7.0)
+    ptr = buf.ctypes.data_as(ctypes.c_void_p)
+    rest = (ctypes.c_double(1.0), ctypes.c_double(1.0), ctypes.c_double(4.0), ctypes.c_double(8192.0))
+    for theta, scaling in ((5e-324, 0), (5e-324, 1), (1e-320, 2)):
+        assert L.sq_rope_frequencies(128, ctypes.c_double(theta), scaling, *rest, ptr) == sq.SQ_ERR_SHAPE
+    assert np.all(buf == 7.0)
+    assert L.sq_rope_frequencies(128, ctypes.c_double(1e-300), 0, *rest, ptr) == sq.SQ_OK and np.all(np.isfinite(buf))
