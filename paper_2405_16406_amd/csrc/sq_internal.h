@@ -258,15 +258,19 @@ struct LaunchTiming {
 };
 LaunchTiming& launch_timing();
 
-// Raises the dynamic LDS limit of kernel Kern to `bytes`, once per process.  A failed
-// attempt is not remembered: the next launch tries again and reports its own status.
+// Raises the dynamic LDS limit of kernel Kern to `bytes` on the current device, whose copy of the kernel
+// it is set for: once per process and device.  A failed attempt is not remembered: the next launch
+// tries again and reports its own status.
 template <auto Kern>
 hipError_t set_max_lds(int bytes) {
-  static std::atomic<bool> done{false};
-  if (done.load(std::memory_order_acquire)) return hipSuccess;
-  const hipError_t e =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(Kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == hipSuccess) done.store(true, std::memory_order_release);
+  static std::atomic<bool> done[64] = {};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const bool known = dev >= 0 && dev < 64;
+  if (known && done[dev].load(std::memory_order_acquire)) return hipSuccess;
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(Kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess && known) done[dev].store(true, std::memory_order_release);
   return e;
 }
 
