@@ -465,11 +465,11 @@ sq_status sq_kv_read(const int32_t* cu, const int32_t* lens, int64_t B, int64_t 
  *     out[b,h,:] = fp16( sum_t softmax_t(scale * q[b,h,:] . K_t) V_t ),  t < min(lens[b], max_len),
  * K_t and V_t of key/value head h / (Hq / Hkv).  A sequence without tokens (or without pages) gets
  * zeros, whatever its query holds; with tokens, a query that is not finite gives NaN.  The parameters
- * v_alpha of these tokens must be 2^-60 or more (the library writes no others from fp16 values), or 0
- * with value codes of 0 (a slot of a zeroed cache that was never written): a token's weight and v_alpha
- * (1 for 0) go into one fp16 factor.  A token whose softmax weight times
- * v_alpha is below 2^-26 of the sequence's largest such product counts with less than that factor's 11
- * bits, below 2^-38 not at all.
+ * v_alpha of these tokens must be 2^-60 or more (the library writes no others from fp16 values with a
+ * v_clip of 2^-28 or more), or 0 with value codes of 0 (a slot of a zeroed cache that was never
+ * written): a token's weight and v_alpha (1 for 0) go into one fp16 factor.  A token whose softmax
+ * weight times v_alpha is below 2^-26 of the sequence's largest such product counts with less than
+ * that factor's 11 bits, below 2^-38 not at all (2^-14 and 2^-25 where the base-2 scores pass 2^22).
  *   q          device fp16 [B, ldq]: Hq heads of D, 16-byte aligned (q_rot of the write)
  *   B          >= 0 (0 is a no-op), B * Hq < 2^24
  *   max_len    1 <= max_len < 2^30, at least the longest length: it fixes the split of the sequence and
@@ -499,7 +499,10 @@ sq_status sq_attn_paged_workspace(int64_t B, int64_t max_len, int64_t Hq, int64_
  * queries are the last n tokens, so a chunk of a prompt comes with the keys of what went before.
  * A query that sees no key gets zeros.  Values and keys that a query does not see have no part in
  * its result, NaN and infinities among them; of what it sees, a NaN score, one of +inf, or none above
- * -inf makes its result NaN.
+ * -inf makes its result NaN, and a value that is not finite makes its dim infinite or NaN.  Softmax
+ * weights go into the second product in fp16: a key whose weight is below 2^-21 of its row's largest
+ * counts with less than fp16's 11 bits, below 2^-32 not at all (2^-14 and 2^-25 where the base-2 scores
+ * pass 2^22, at which fp32 has steps of 1/2).
  *   q          device fp16 [Tq, ldq]: Hq heads of D;  k, v  device fp16 [Tk, ldk], [Tk, ldv]: Hkv heads
  *              of D; 16-byte aligned
  *   cu_q, cu_k device int32 [B + 1], ascending, within [0, Tq] and [0, Tk] (entries beyond are taken as

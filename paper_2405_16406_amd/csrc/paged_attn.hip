@@ -26,7 +26,7 @@
 // HBM bounds it: a token and key/value head are 144 bytes (4 bits, fp32 parameters; 136 with fp16
 // ones), or 272 with 8 bits, read once for all query heads that share them.  Each wave on its own,
 // with the next block's codes in registers while one is worked on and no barrier before the end, keeps
-// twelve (8 bits: eight) waves' loads in flight on a compute unit.  The arithmetic is 490 vector
+// twelve (8 bits: eight) waves' loads in flight on a compute unit.  The arithmetic is 500 vector
 // operations and 32 products a block of 4-bit codes, whether a tile has 16 heads or one: about a third
 // of the time on a full device, and what is left to do when the last codes have come.  Measured, this
 // kernel and the join: 131071 tokens of 8 heads, 4 bits, 31 - 33 + 4 us (151 MB: 4.6 TB/s in the

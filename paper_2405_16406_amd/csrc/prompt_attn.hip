@@ -20,15 +20,17 @@
 // Tiles of K and V go from memory straight to LDS, one ahead of the products.  A tile's row is 256
 // bytes; its 16-byte chunk c lies at c xor swizzle(row), so that neither the 16 rows of a K read
 // nor the 4 x 64 bytes of a transposed read of V meet on a bank.
-// Weights are rounded to fp16 (2^-12 of the weight, as the output is); sums stay in fp32.
+// Weights are rounded to fp16, as the second product needs them: 2^-12 of a weight down to 2^-14, where
+// the largest is 2^7 to 2^15, and 2^-25 below.  Sums stay in fp32.  Outputs are off by 2.5e-4 to 2.9e-4
+// of their size, of which the output's own rounding is 2.0e-4.
 // The matrix cores bound it where there are rows and keys enough: 2048 tokens behind 32768 (64
 // heads on 8) take 1950 us, 1.16 PFLOP/s, the rate a large library product reaches on the card.  They
-// are busy for 67 % of the cycles, at 1.57 GHz: the chip's power sets the clock.  LDS is at 34 %,
+// are busy for 68 % of the cycles, at 1.53 - 1.57 GHz: the chip's power sets the clock.  LDS is at 34 %,
 // without bank conflicts.
 // Shorter prompts add what a workgroup does once (find the tile, first keys and queries, first scores
 // and last values alone, stores) and what a causal prompt's last tile wastes: one of a single tile
 // takes 7 us, and a tile of a long one 1.8.  16 packed prompts of 292 .. 4000 tokens, 32 heads on 8,
-// 431 - 439 us (0.9 PFLOP/s, matrix cores busy for 46 % at 1.67 GHz), 2048 tokens of 32 heads 49 - 51
+// 431 - 439 us (0.9 PFLOP/s, matrix cores busy for 44 - 46 % at 1.7 GHz), 2048 tokens of 32 heads 49 - 51
 // us (0.7).  Two workgroups of four waves a compute unit, each with its own keys, would hide one's
 // start behind the other's products: 51 - 52, 442 and 2020 - 2040 us for these three, no gain.
 //

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import paged as opg
+from oracle.quant import quant_asym
 from paper_2405_16406_amd import sq
 
 
@@ -102,3 +103,14 @@ def test_causal_rows():
     assert not out[:2].any() and np.allclose(out[2, 0], v[0, 0])  # 4 queries, 2 keys: the first two see none
     s = np.exp(k[2:6, 0] @ q[4, 0] / math.sqrt(128))
     assert np.allclose(out[4, 0], (s / s.sum()) @ v[2:6, 0])
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_smallest_value_scale(bits):
+    """fp16 values differ by 2^-24 or not at all: clipped to 2^-28 of the range, alpha is 2^-60 or more."""
+    x = np.zeros((3, 128), dtype=np.float16)
+    x[0, 5] = 2.0 ** -24
+    x[1, :] = np.float16(0.5)
+    x[1, 7] = np.nextafter(np.float16(0.5), np.float16(0))
+    _, alpha, _ = quant_asym(x.astype(np.float32), bits=bits, group=128, clip=2.0 ** -28)
+    assert alpha.min() >= 2.0 ** -60 and alpha[2] == 1
