@@ -69,7 +69,8 @@ const char* sq_last_error(void);
  * sq_time_next_call -- measurement hook, not part of the method.  Arms two events for
  * the next call of sq_had_quant_act(_ex), sq_pack_w4(_ex), sq_w4a4_linear, sq_w4a8_linear,
  * sq_w4a4_linear_swiglu, sq_qk_had_kvquant(_ex), sq_attn_decode_kv4(_ex),
- * sq_rope_kv_write, sq_kv_read, sq_attn_paged or sq_attn_prompt made by this host thread:
+ * sq_rope_kv_write(_ex), sq_kv_read, sq_attn_paged(_window), sq_attn_prompt(_window), sq_attn_tree,
+ * sq_tree_mask, sq_paged_release, sq_paged_grow or sq_kv_keep made by this host thread:
  * start_event takes the start time of the first kernel that call launches and stop_event
  * the end time of its last kernel (hipExtLaunchKernel events), so hipEventElapsedTime(start,
  * stop) is the call's time on the device without marker packets between kernels.
@@ -523,6 +524,204 @@ sq_status sq_attn_prompt(const void* q, int64_t ldq, const void* k, int64_t ldk,
 /* Device bytes of sq_attn_prompt's workspace on the CURRENT device.  Errors: SQ_ERR_NULL, SQ_ERR_SHAPE,
  * SQ_ERR_UNSUPPORTED, SQ_ERR_HIP. */
 sq_status sq_attn_prompt_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D, uint64_t* bytes);
+
+/*
+ * Drafted tokens, windows and the pages of a step.
+ *
+ * A draft is a token that the model has yet to check.  A sequence's drafts of a step are its last n
+ * tokens in the cache, rows cu[b] .. cu[b+1] - 1 of the packed calls (n = cu[b+1] - cu[b]), and form a
+ * tree: draft i continues its parent, a draft before it, or the text.  Its place in the cache is
+ * base + i, base = lens[b] - n; its position in the text is base + depth, depth being the number of
+ * its ancestors among the drafts.
+ *
+ * window > 0 lets a token at position p see the keys at positions t > p - window, itself the last, and
+ * besides them the first `sinks` ones, t < sinks; window == 0: all keys before it (sinks counts for
+ * nothing then).  0 <= window, sinks < 2^30.
+ */
+
+/*
+ * sq_tree_mask -- the drafts that each draft sees, and its depth, from the drafts' parents.
+ *   parents    device int32 [T]: index of the parent among the sequence's drafts; a value outside
+ *              [0, i) at draft i (e.g. -1) makes it a root, which continues the text
+ *   cu         device int32 [B + 1], ascending: the sequences' rows; rows of no sequence are left alone
+ *   lens       device int32 [B]: tokens in the cache, the drafts included; read, and required, only with
+ *              window > 0 and sinks > 0
+ *   T, B       >= 0 (0 is a no-op), < 2^31
+ *   window, sinks  as above: an ancestor `window` or more steps up is left out, unless its position is
+ *              below sinks
+ *   mask       device int32 [T, ld_mask], the first `words` words of a row written: bit j % 32 of word
+ *              j / 32 of draft i is 1 where j is i or an ancestor that i sees.  Drafts from 32 * words on
+ *              have no bits.
+ *   words, ld_mask  1 <= words <= 2^16, words <= ld_mask < 2^24
+ *   depth      device int32 [T]
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_ALIGN (4 bytes each), SQ_ERR_ALIAS, SQ_ERR_HIP.
+ */
+sq_status sq_tree_mask(const int32_t* parents, const int32_t* cu, const int32_t* lens, int64_t B, int64_t T,
+                       int32_t window, int32_t sinks, int32_t* mask, int64_t ld_mask, int64_t words, int32_t* depth,
+                       void* stream);
+
+/*
+ * sq_rope_kv_write_ex -- sq_rope_kv_write with the rows' positions apart from their places in the cache
+ * (sq_rope_kv_write is this call with depth = NULL):
+ *   depth      device int32 [T] or NULL: row t of sequence b turns by the position lens[b] - n + depth[t],
+ *              n = cu[b+1] - cu[b] (1 without cu), and is written to its place as ever.  The
+ *              position of a row that is written is taken as it is, negative ones included.
+ * Every other argument, layout and error as sq_rope_kv_write; depth is an input for the overlap check.
+ */
+sq_status sq_rope_kv_write_ex(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                              int64_t T, int64_t Hq, int64_t D, const int32_t* cu, const int32_t* lens, int64_t B,
+                              const int32_t* depth,
+                              const int32_t* block_table, int64_t ld_table, int64_t max_blocks,
+                              uint8_t* k_q, uint8_t* v_q, void* params, int64_t pages, int64_t page, int64_t Hkv,
+                              int32_t bits, int32_t param_bits,
+                              const double* freq, int32_t rotary_dim, int32_t interleaved, float magnitude,
+                              float k_clip, float v_clip, void* q_rot, void* k_rot, void* stream);
+
+/*
+ * sq_attn_tree -- attention of a sequence's last n tokens over its pages: drafts, or the tokens of a
+ * prompt's chunk, written by sq_rope_kv_write(_ex) before:
+ *     out[t,h,:] = fp16( sum_j softmax_j(scale * q[t,h,:] . K_j) V_j ),
+ * over the tokens j < min(lens[b], max_len) that row t sees.  Row t = cu[b] + i sees
+ *   with mask     the tokens before the drafts, j < base, as far as the window at position base + depth[t]
+ *                 lets it, and of the drafts exactly those whose bit is set
+ *   without       the tokens j <= base + i, as far as the window at base + i lets it
+ * A row that sees no token with a page gets zeros; one with a token that it sees and a query that is
+ * not finite gives NaN.  What a row does not see has no part in its result, NaN and infinities among
+ * the parameters included.  Precision and the range of v_alpha as in sq_attn_paged, row by row.
+ *   q          device fp16 [T, ldq]: Hq rotated heads of D, 16-byte aligned
+ *   cu         device int32 [B + 1], ascending, within [0, T] (values beyond are taken as the end).  Rows
+ *              of no sequence, and rows with base + i < 0, are left as they were in out.
+ *   mask       device int32 [T, ld_mask] or NULL, as sq_tree_mask writes it (any bits are fine: a row need
+ *              not see itself); drafts from 32 * words on are seen by none
+ *   words, ld_mask  as in sq_tree_mask (ignored without mask)
+ *   depth      device int32 [T] or NULL (depth i in row i; must be NULL without mask); read with window > 0
+ *              alone, and taken as 0 below 0 and as 2^30 above
+ *   T          >= 0, T * Hq + B * Hq < 2^24 (T == 0 or B == 0 is a no-op)
+ *   max_len    1 <= max_len < 2^30, at least the longest length: with T, B and the window it fixes the
+ *              split of the sequence, the workspace and the order of additions
+ *   out        device fp16 [T, ldo]: Hq heads of D, 16-byte aligned
+ *   workspace  as in sq_attn_paged, sized by sq_attn_tree_workspace for the same sizes
+ * Every other argument as in sq_attn_paged.  The result does not depend on the run.  Errors as
+ * sq_attn_paged.
+ */
+sq_status sq_attn_tree(const void* q, int64_t ldq, const int32_t* cu, const int32_t* lens, int64_t B, int64_t T,
+                       const int32_t* mask, int64_t ld_mask, int64_t words, const int32_t* depth,
+                       int32_t window, int32_t sinks,
+                       const int32_t* block_table, int64_t ld_table, int64_t max_blocks,
+                       const uint8_t* k_q, const uint8_t* v_q, const void* params, int64_t pages, int64_t page, int64_t Hkv,
+                       int64_t Hq, int64_t D, int32_t bits, int32_t param_bits, int64_t max_len, float scale,
+                       void* out, int64_t ldo, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of sq_attn_tree's workspace on the CURRENT device.  Errors: SQ_ERR_NULL, SQ_ERR_SHAPE,
+ * SQ_ERR_UNSUPPORTED, SQ_ERR_HIP. */
+sq_status sq_attn_tree_workspace(int64_t B, int64_t T, int64_t max_len, int32_t window, int32_t sinks, int64_t Hq, int64_t Hkv,
+                                 int64_t D, uint64_t* bytes);
+
+/*
+ * sq_attn_paged_window -- sq_attn_paged of a token that sees the last `window` tokens of its sequence and
+ * the first `sinks` ones (window 0: all of them).  Pages that lie wholly between the two may have gone
+ * back to the pool (sq_paged_release): they are not read.  Token, range of v_alpha, zeros and NaN as in
+ * sq_attn_tree.
+ *   window, sinks  as above
+ *   B          >= 0 (0 is a no-op), 2 * B * Hq < 2^24
+ *   workspace  sized by sq_attn_paged_window_workspace for the same sizes
+ * Every other argument and error as sq_attn_paged.
+ */
+sq_status sq_attn_paged_window(const void* q, int64_t ldq, const int32_t* lens, int64_t B, int32_t window, int32_t sinks,
+                               const int32_t* block_table, int64_t ld_table, int64_t max_blocks,
+                               const uint8_t* k_q, const uint8_t* v_q, const void* params, int64_t pages, int64_t page,
+                               int64_t Hkv, int64_t Hq, int64_t D, int32_t bits, int32_t param_bits, int64_t max_len,
+                               float scale, void* out, int64_t ldo, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of sq_attn_paged_window's workspace on the CURRENT device.  Errors as sq_attn_tree_workspace. */
+sq_status sq_attn_paged_window_workspace(int64_t B, int64_t max_len, int32_t window, int32_t sinks, int64_t Hq, int64_t Hkv,
+                                         int64_t D, uint64_t* bytes);
+
+/*
+ * sq_attn_prompt_window -- the causal attention of sq_attn_prompt in which query i of a sequence of n
+ * queries and m keys, at position p = m - n + i, sees the keys p - window < t <= p and t < sinks, t <= p
+ * (window 0: all up to p).  Keys outside every window of a sequence are not read.
+ *   window, sinks  as above
+ *   workspace  sized by sq_attn_prompt_window_workspace for the same sizes
+ * Every other argument and error as sq_attn_prompt with causal = 1.
+ */
+sq_status sq_attn_prompt_window(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                const int32_t* cu_q, const int32_t* cu_k, int64_t B, int64_t Tq, int64_t Tk,
+                                int64_t Hq, int64_t Hkv, int64_t D, float scale, int32_t window, int32_t sinks,
+                                void* out, int64_t ldo, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of sq_attn_prompt_window's workspace on the CURRENT device.  Errors as sq_attn_prompt_workspace. */
+sq_status sq_attn_prompt_window_workspace(int64_t B, int64_t Tq, int64_t Tk, int32_t window, int32_t sinks, int64_t Hq,
+                                          int64_t Hkv, int64_t D, uint64_t* bytes);
+
+/*
+ * The pages of the pool on the device, so that a captured step can hand them out.  Common to the two calls:
+ *   pool       device int32 [pages]: its first count[0] entries are the free pages; a page is taken from
+ *              the end and goes back there
+ *   count      device int32 [1], in and out; taken as within [0, pages]
+ *   held       device int32 [B], in and out: the blocks of each sequence that have a page, the first
+ *              held[b] columns of its row of the table; taken as within [0, max_blocks]
+ *   block_table, ld_table, max_blocks, page   as in the paged calls; in and out
+ *   B          >= 0 (0 is a no-op of sq_paged_release), <= 2^20;  max_blocks < 2^24, pages < 2^31
+ * Calls that share a pool, a table or held must be ordered.  All is decided by the values on the device;
+ * none of them makes a call read or write outside the tensors.
+ */
+
+/*
+ * sq_paged_release -- pages go back to the pool: of sequence b the held blocks whose positions all lie in
+ * first[b] .. end[b] - 1.  end may lie past the last token: at or past the end of the last held block,
+ * held[b] becomes the first block that went (what ended a sequence, first = 0, or took back its drafts,
+ * first = tokens kept); below it held[b] stays (what a window has left behind: first = sinks,
+ * end = position - window + 1).  Their entries become -1; one that is not a page of the pool goes
+ * nowhere.  The pages join the pool by sequence, then block.  A page that two sequences share must be
+ * released by one of them alone.
+ *   first, end device int32 [B]; first below 0 counts as 0
+ * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_ALIGN, SQ_ERR_ALIAS, SQ_ERR_HIP.
+ */
+sq_status sq_paged_release(const int32_t* first, const int32_t* end, int32_t* held, int64_t B,
+                           int32_t* block_table, int64_t ld_table, int64_t max_blocks, int64_t page,
+                           int32_t* pool, int32_t* count, int64_t pages, void* stream);
+
+/*
+ * sq_paged_grow -- pages, lengths and rows of a step's new tokens: sequence b has have[b] tokens in the cache
+ * and gets add[b] (below 0: 0).  Its blocks up to the last new token that have no page yet get pages of the
+ * pool, by sequence, then block; then
+ *   lens       device int32 [B]: have + add, what the calls of the step take
+ *   cu         device int32 [B + 1]: the rows of each sequence's new tokens, cu[0] = 0
+ *   pos        device int32 [T]: the position have[b] + i of row cu[b] + i; -1 in rows from cu[B] on
+ *   slots      device int64 [T]: where the row's token lies, page * (tokens of a page) + place, the index
+ *              among a head's tokens of the pool; -1 in rows from cu[B] on, and where the table's entry is
+ *              not a page of the pool
+ *   missing    device int32 [2]: the pages that the pool, or columns that the table, lacks for this, and the
+ *              rows that T lacks; (0, 0) when all is well.  Otherwise nothing is handed out: table, held and
+ *              count stay, lens is have, cu is 0, pos and slots are -1, so that the calls of the step have no
+ *              rows, and the step can be tried again when pages have come back.
+ *   T          >= 0 rows of pos and slots (0: both may be NULL), < 2^31
+ * Sums beyond 2^31 - 1 count as that many.  Errors as sq_paged_release.
+ */
+sq_status sq_paged_grow(const int32_t* have, const int32_t* add, int32_t* held, int64_t B, int64_t T,
+                        int32_t* block_table, int64_t ld_table, int64_t max_blocks, int64_t page,
+                        int32_t* pool, int32_t* count, int64_t pages,
+                        int32_t* lens, int32_t* cu, int32_t* pos, int64_t* slots, int32_t* missing, void* stream);
+
+/*
+ * sq_kv_keep -- after the check of a step's drafts: those of the accepted path become the sequence's next
+ * tokens.  Draft path[b][i], i < kept[b], moves to the place base + i, codes and parameters as they are, in
+ * all heads; the sequence then has lens_out[b] = base + kept[b] tokens.  (Draft path[b][i] of a tree has
+ * depth i, so its key is turned for the position that it moves to.)
+ *   path       device int32 [B, ld_path], the first max_kept entries of a row: indexes of drafts on the way
+ *              down a tree (parents before children, so that entry i is i or more)
+ *   kept       device int32 [B], taken as within [0, min(n, max_kept)]
+ *   max_kept   1 <= max_kept <= ld_path < 2^24
+ *   cu, lens   as in sq_attn_tree, before the move; base and places below 0 have no token
+ *   lens_out   device int32 [B], at least 0; not lens itself, which is read while it is written
+ * An entry outside [i, n), or whose place or whose draft has no page, moves nothing: the place keeps what it
+ * held.  Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_UNSUPPORTED, SQ_ERR_ALIGN, SQ_ERR_ALIAS, SQ_ERR_HIP.
+ */
+sq_status sq_kv_keep(const int32_t* cu, const int32_t* lens, int64_t B, const int32_t* path, int64_t ld_path, int64_t max_kept,
+                     const int32_t* kept, const int32_t* block_table, int64_t ld_table, int64_t max_blocks,
+                     uint8_t* k_q, uint8_t* v_q, void* params, int64_t pages, int64_t page, int64_t Hkv,
+                     int64_t D, int32_t bits, int32_t param_bits, int32_t* lens_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -52,4 +52,23 @@ SQ_HOST_DEVICE int64_t token_slot(const PagedCache& c, int32_t page, int32_t hea
   return ((static_cast<int64_t>(page) * c.heads + head) << c.shift) + (pos & ((int64_t{1} << c.shift) - 1));
 }
 
+// The tokens that rows of a sequence see, as one run of `tokens` places: the first `head` tokens, then those
+// from `start` on.  Both are whole blocks of 64, so that a block of the run is one of the sequence.
+struct TokenRun {
+  int32_t head, start, tokens;
+  SQ_HOST_DEVICE int32_t position(int32_t place) const { return place < head ? place : place - head + start; }
+};
+
+// That of rows whose earliest position is `low` and which see no token from `end` on (base + i + 1 of the
+// last row of a chain, the length where a mask decides).  window 0: all tokens.
+SQ_HOST_DEVICE TokenRun token_run(int32_t low, int32_t end, int32_t window, int32_t sinks) {
+  constexpr int32_t kWhole = ~63;
+  if (end < 0) end = 0;
+  const int32_t from = low - window + 1, head = (sinks + 63) & kWhole;
+  const int32_t start = window > 0 && from > 0 ? from & kWhole : 0;
+  if (start <= head) return {0, 0, end};
+  if (end <= start) return {0, 0, end < head ? end : head};
+  return {head, start, head + (end - start)};
+}
+
 }  // namespace sq

@@ -53,6 +53,7 @@ __device__ __forceinline__ void quad_fwht(F (&e)[32], int j) {
 // and their lengths come along (a second trip to memory would follow the first).
 struct RowSeq {
   int seq;
+  int begin;
   int end;
   int len;
 };
@@ -69,11 +70,27 @@ __device__ __forceinline__ RowSeq find_sequence(const int32_t* cu, const int32_t
     const uint64_t past = __ballot(b < B && end > t);
     if (past) {
       const int first = __builtin_ctzll(past);
-      const int seq = t < __builtin_amdgcn_readlane(begin, first) ? -1 : static_cast<int>(b0) + first;
-      return {seq, __builtin_amdgcn_readlane(end, first), __builtin_amdgcn_readlane(len, first)};
+      const int from = __builtin_amdgcn_readlane(begin, first);
+      const int seq = t < from ? -1 : static_cast<int>(b0) + first;
+      return {seq, from, __builtin_amdgcn_readlane(end, first), __builtin_amdgcn_readlane(len, first)};
     }
   }
-  return {-1, 0, 0};
+  return {-1, 0, 0, 0};
+}
+
+// Inclusive sum over the lanes of a wave up to each: rows of 16 by shifts, then the rows' totals.
+__device__ __forceinline__ int wave_scan(int v) {
+  const auto add = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+  };
+  using std::integral_constant;
+  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});  // row_shr:1
+  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15
+  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
+  return v;
 }
 
 // op over the lane's value and those of the lanes 16, 32 and 48 further (mod 64)

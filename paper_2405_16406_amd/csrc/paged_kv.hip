@@ -257,22 +257,27 @@ rope_kv_write(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int
   // positions, pages and angles: wave w takes the tokens w, w + waves, ...
   for (int tt = wave; tt < a.tokens; tt += waves) {
     const int64_t t = t0 + tt;
-    RowSeq s{-1, 0, 0};
+    RowSeq s{-1, 0, 0, 0};
     double f = 0.0;
-    if constexpr (FORM != kNoRope)
+    int32_t depth = 0;
+    if constexpr (FORM != kNoRope) {
       if (lane < a.rotary / 2) f = a.freq[lane];
+      if (a.depth && t < a.T) depth = a.depth[t];
+    }
     if (t < a.T) {
       if (cu)
         s = find_sequence(cu, lens, a.B, t);
       else
-        s = RowSeq{static_cast<int>(t), static_cast<int>(t) + 1, lens[t]};
+        s = RowSeq{static_cast<int>(t), static_cast<int>(t), static_cast<int>(t) + 1, lens[t]};
     }
     const int64_t pos = s.seq >= 0 ? row_position(s.len, s.end, t) : -1;
     int32_t entry = -1;
     const int32_t col = table_column(a.cache, pos);
     if (col >= 0) entry = a.cache.table[s.seq * a.cache.ldt + col];
     if constexpr (FORM != kNoRope) {
-      const double turns = static_cast<double>(pos) * (f * 0.15915494309189533577);
+      // with depths, the position in the text is not the place in the cache
+      const int64_t at = a.depth ? row_position(s.len, s.end, s.begin) + depth : pos;
+      const double turns = static_cast<double>(at) * (f * 0.15915494309189533577);
       double sn, cn;
       sincospi(2.0 * (turns - rint(turns)), &sn, &cn);
       const double m = static_cast<double>(a.magnitude) * kInvSqrtD;
@@ -337,7 +342,7 @@ kv_read(const int32_t* cu, const int32_t* lens, int64_t t_first, KvReadArgs a) {
   const int64_t t0 = t_first + static_cast<int64_t>(blockIdx.x) * a.tokens;
   for (int tt = wave; tt < a.tokens; tt += 4) {
     const int64_t t = t0 + tt;
-    RowSeq s{-1, 0, 0};
+    RowSeq s{-1, 0, 0, 0};
     if (t < a.T) s = find_sequence(cu, lens, a.B, t);
     if (lane == 0) {
       int64_t pos = -1;

@@ -62,6 +62,39 @@ inline void paged_split(int64_t B, int64_t max_len, int32_t hq, int32_t hkv, int
   if (chunks < 1) chunks = 1;
 }
 
+// Several rows of a sequence over its pages: workgroups of 16 * rb (row, query head) pairs, `tiles` of them
+// at most, and the tokens that they see in `chunks` pieces of chunk_tokens.
+struct TreePlan {
+  int32_t rb, tiles, chunks, chunk_tokens;
+};
+inline TreePlan tree_plan(int64_t B, int64_t T, bool single, int64_t max_len, int32_t window, int32_t sinks, int32_t hq, int32_t hkv,
+                          int cus) {
+  constexpr int64_t unit = kPagedWaves * kPagedBlock;
+  const int64_t group = hq / hkv, rows = T * group;
+  TreePlan p{};
+  // tokens of the longest run: the window of the first row, the rows behind it, and what whole blocks add
+  int64_t run = max_len;
+  if (window > 0) {
+    const int64_t most = static_cast<int64_t>(sinks) + window + (single ? 1 : T) + 2 * kPagedBlock;
+    if (run > most) run = most;
+  }
+  const int64_t each = (rows + (B > 0 ? B : 1) - 1) / (B > 0 ? B : 1);  // rows of an average sequence
+  p.rb = each <= 16 ? 1 : each <= 32 ? 2 : 4;
+  const int64_t tile = 16 * p.rb;
+  p.tiles = static_cast<int32_t>(single ? B * ((group + tile - 1) / tile) : rows / tile + B);
+  const int64_t groups = (single ? p.tiles : B * ((each + tile - 1) / tile)) * hkv;
+  const int64_t tokens = groups * run, want = static_cast<int64_t>(cus) * (B > 1 ? 8 : 2);
+  int64_t chunk = (tokens + want - 1) / want;
+  const int64_t least = tokens / unit > 4 * static_cast<int64_t>(cus) ? 2 * unit : unit;
+  if (chunk < least) chunk = least;
+  chunk = (chunk + unit - 1) / unit * unit;
+  if (chunk > run) chunk = (run + unit - 1) / unit * unit;
+  p.chunk_tokens = static_cast<int32_t>(chunk < unit ? unit : chunk);
+  p.chunks = static_cast<int32_t>((run + p.chunk_tokens - 1) / p.chunk_tokens);
+  if (p.chunks < 1) p.chunks = 1;
+  return p;
+}
+
 constexpr int kPromptRows = 256;  // (token, query head) rows of a prompt workgroup
 constexpr int kPromptTile = 64;   // keys of its step
 

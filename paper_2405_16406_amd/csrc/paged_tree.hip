@@ -1,0 +1,555 @@
+// Attention of a sequence's last tokens over its pages (paged_attn.hip has the mathematics of one row): drafts
+// of a tree, each with the drafts that it sees as bits, or a chain of tokens; and of single tokens with a
+// window.  Row (i, h) of a sequence, i < n its token and h a query head of the key/value head, sees
+//     mask:   t < base where t > base + depth_i - window or t < sinks, and the drafts base + j of its bits
+//     chain:  t <= base + i with the same window at base + i.
+//
+// A workgroup of kWaves waves serves one (sequence, key/value head, 16 RB of its rows, chunk of the tokens that
+// these rows see); its waves take the chunk's blocks of 64 tokens in turn, each on its own.  A block's codes
+// become operands once for all RB columns of 16 rows.  What a row does not see is cut out of the scores by
+// 16 bits a lane, one for each of its tokens, in the blocks alone that some row does not see whole.
+#include "paged_attn_device.h"
+
+namespace sq {
+namespace {
+
+constexpr int kWaves = kPagedWaves;
+
+template <int BITS>
+constexpr int tree_lds() {
+  const int merge = kWaves * 16 * (kDimRow + 2) * 4, codes = kWaves * WaveLds<BITS>::BYTES;
+  return merge > codes ? merge : codes;
+}
+
+// Sequence and tile of rows of the tile number `rem` among ceil(n * group / ROWS) a sequence; seq -1: past the last.
+struct TreeTile {
+  int seq, tile;
+  int q0, n, len;
+};
+template <int ROWS>
+__device__ __forceinline__ TreeTile find_tree_tile(const int32_t* cu, const int32_t* lens, int64_t B, int64_t T, int group, int rem) {
+  if (!cu) {
+    const int per = (group + ROWS - 1) / ROWS;
+    const int b = rem / per;
+    return {b, rem - b * per, b, 1, lens[b]};
+  }
+  const int lane = threadIdx.x & 63;
+  for (int64_t b0 = 0; b0 < B; b0 += 64) {
+    int q0 = 0, n = 0, len = 0;
+    if (b0 + lane < B) {  // clamped to the rows, whatever cu holds
+      const int most = static_cast<int>(T);
+      const int first = cu[b0 + lane], end = cu[b0 + lane + 1];
+      len = lens[b0 + lane];
+      q0 = min(max(first, 0), most);
+      n = max(min(end, most) - q0, 0);
+    }
+    const int tiles = (n * group + ROWS - 1) / ROWS;
+    const int upto = wave_scan(tiles);
+    const uint64_t past = __ballot(upto > rem);
+    if (past) {
+      const int f = __builtin_ctzll(past);
+      const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+      return {static_cast<int>(b0) + f, rem - (of(upto) - of(tiles)), of(q0), of(n), of(len)};
+    }
+    rem -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return {-1, 0, 0, 0, 0};
+}
+
+// Bits x of the 16 tokens t .. t + 15 with t + x < end.
+__device__ __forceinline__ uint32_t below(int end, int t) { return (1u << min(max(end - t, 0), 16)) - 1u; }
+
+template <int BITS, bool P16, int RB>
+__global__ void __launch_bounds__(64 * kWaves, RB == 1 ? (BITS == 4 ? 3 : 2) : RB == 2 ? 2 : 1)
+attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32_t magic_tiles, uint32_t magic_heads,
+               uint32_t magic_group, TreeArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  using W = WaveLds<BITS>;
+  constexpr int ROWS = 16 * RB;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  // As in attn_paged_part: chunks from a tile's last one back slowest, then tile, then key/value head (so that
+  // the tiles which share keys follow each other on one of the chip's caches).
+  uint32_t rest, hk, back, number;
+  div_rem(blockIdx.x, a.cache.heads, magic_heads, rest, hk);
+  div_rem(rest, a.plan.tiles, magic_tiles, back, number);
+  back = a.plan.chunks - 1 - back;
+  const TreeTile tt = find_tree_tile<ROWS>(cu, lens, a.B, a.T, a.group, static_cast<int>(number));
+  if (tt.seq < 0) return;  // the workgroup leaves together
+  const int all = min(max(tt.len, 0), (1 << 30) - 1), base = all - tt.n;  // (a position plus a depth stays below 2^31)
+  const int len = min(all, a.max_len);
+  const int rows = tt.n * a.group;
+  const int r0 = tt.tile * ROWS;
+  const auto token_of = [&](int r) {
+    uint32_t t, h;
+    div_rem(static_cast<uint32_t>(r), a.group, magic_group, t, h);
+    return static_cast<int>(t);
+  };
+  const int i0 = token_of(r0), i1 = token_of(min(r0 + ROWS, rows) - 1);  // first and last token of the tile
+  const TokenRun run = token_run(a.mask ? base : base + i0, a.mask ? len : min(base + i1 + 1, len), a.window, a.sinks);
+  const int own = max(1, (run.tokens + a.plan.chunk_tokens - 1) / a.plan.chunk_tokens);  // chunks of the tile
+  if (static_cast<int>(back) >= own) return;  // the workgroup leaves together
+  const int c = own - 1 - static_cast<int>(back);
+  const int first = c * a.plan.chunk_tokens;
+  const int last = min(run.tokens, first + a.plan.chunk_tokens);  // places of the run
+  const int32_t* const table = a.cache.table + tt.seq * a.cache.ldt;
+
+  // The lane's rows: r0 + 16 rb + i (past the last: that one again, not stored), dims 32 g .. 32 g + 31 of the
+  // queries in the codes' pair order, and their sums over all dims; what they see: t < hi where t >= lo or
+  // t < sinks, and the bits of mask row `bits`.
+  v8h qf[RB][4];
+  float qsum[RB];
+  int lo[RB], hi[RB];
+  const int32_t* bits[RB];
+  int lo_most = 0, hi_least = len;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    uint32_t tok, gh;
+    div_rem(static_cast<uint32_t>(min(r0 + 16 * rb + i, rows - 1)), a.group, magic_group, tok, gh);
+    const int64_t t = tt.q0 + static_cast<int64_t>(tok);
+    const v4u* qv = reinterpret_cast<const v4u*>(q + t * a.ldq + (static_cast<int64_t>(hk) * a.group + gh) * 128 + 32 * g);
+    v4u raw[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) raw[x] = qv[x];
+    int at = static_cast<int>(tok);
+    if (a.mask && a.depth && a.window > 0) at = min(max(a.depth[t], 0), 1 << 30);
+    hi[rb] = min(a.mask ? base : base + static_cast<int>(tok) + 1, len);
+    lo[rb] = a.window > 0 ? max(base + at - a.window + 1, 0) : 0;
+    bits[rb] = a.mask ? a.mask + t * a.ldm : nullptr;
+    hi_least = min(hi_least, hi[rb]);
+    lo_most = max(lo_most, lo[rb]);
+    float sum = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) sum += h2f(static_cast<uint16_t>(raw[x][y])) + h2f(static_cast<uint16_t>(raw[x][y] >> 16));
+    qsum[rb] = rows_all(sum, [](float u, float v) { return __fadd_rn(u, v); });
+    if constexpr (BITS == 4) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const v4u u = raw[2 * e], v = raw[2 * e + 1];
+        qf[rb][2 * e] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x05040100u), __builtin_amdgcn_perm(u[3], u[1], 0x05040100u),
+                                __builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x05040100u));
+        qf[rb][2 * e + 1] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[1], 0x07060302u),
+                                    __builtin_amdgcn_perm(v[2], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u));
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        qf[rb][x] = operand(__builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x05040100u), __builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x07060302u),
+                            __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x05040100u), __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x07060302u));
+    }
+  }
+  // of the whole tile (lo and hi are not negative there but for hi of a base below 0, which counts as 0)
+  lo_most = static_cast<int>(wave_all(static_cast<uint32_t>(lo_most), [](uint32_t u, uint32_t v) { return max(u, v); }));
+  hi_least = static_cast<int>(wave_all(static_cast<uint32_t>(max(hi_least, 0)), [](uint32_t u, uint32_t v) { return min(u, v); }));
+
+  uint8_t* const vlds = lds + w * W::BYTES;
+  float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
+  constexpr int KW = BITS == 4 ? 1 : 2;
+  const float cs = a.scale_log2e, cs24 = a.scale_log2e * 16777216.0f;
+
+  v4u kc[4][KW], vc[4][KW];
+  float4 par;
+  bool par_ok;
+  auto entry_of = [&](int v0) -> int32_t {
+    if (v0 >= last) return -1;
+    const int32_t col = table_column(a.cache, run.position(v0) + 16 * g);
+    return col < 0 ? -1 : table[col];
+  };
+  auto load = [&](int v0, int32_t entry) __attribute__((always_inline)) {
+    const int t0 = run.position(v0);
+    const int32_t mine = valid_page(a.cache, entry);
+    par_ok = mine >= 0 && v0 + lane < last;
+    const int32_t safe = max(mine, 0);
+    int32_t pg[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) pg[n] = __builtin_amdgcn_readlane(safe, 16 * n);
+    const int n = i >> 2;
+    const int32_t pk = n == 0 ? pg[0] : n == 1 ? pg[1] : n == 2 ? pg[2] : pg[3];
+    const uint8_t* kp = a.cache.kq + token_slot(a.cache, pk, hk, t0 + 16 * n + (i & 3)) * W::ROW + (BITS == 4 ? 16 : 32) * g;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 0; x < KW; ++x) kc[j][x] = *reinterpret_cast<const v4u*>(kp + 4 * j * W::ROW + 16 * x);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const uint8_t* vp = a.cache.vq + token_slot(a.cache, pg[m], hk, t0 + 16 * m) * W::ROW + 16 * lane;
+#pragma unroll
+      for (int x = 0; x < KW; ++x) vc[m][x] = *reinterpret_cast<const v4u*>(vp + 1024 * x);
+    }
+    const int64_t pslot = token_slot(a.cache, safe, hk, t0 + lane);
+    if constexpr (P16) {
+      const uint2 p = static_cast<const uint2*>(a.cache.params)[pslot];
+      par = make_float4(h2f(static_cast<uint16_t>(p.x)), h2f(static_cast<uint16_t>(p.x >> 16)),
+                        h2f(static_cast<uint16_t>(p.y)), h2f(static_cast<uint16_t>(p.y >> 16)));
+    } else {
+      par = static_cast<const float4*>(a.cache.params)[pslot];
+    }
+  };
+  // The lane's tokens t .. t + 15 that its row of column rb sees.
+  auto visible = [&](int rb, int t) -> uint32_t {
+    uint32_t vis = below(hi[rb], t) & (~below(lo[rb], t) | below(a.sinks, t));
+    if (a.mask && t + 15 >= base) {
+      const int j = t - base, word = j >> 5;  // (rounded down: -1 for the words before the first)
+      const auto at = [&](int x) { return x >= 0 && x < a.words ? static_cast<uint32_t>(bits[rb][x]) : 0u; };
+      const uint64_t two = at(word) | static_cast<uint64_t>(at(word + 1)) << 32;
+      vis |= static_cast<uint32_t>(two >> (j & 31)) & below(min(base + tt.n, len), t);
+    }
+    return vis & 0xFFFFu;
+  };
+
+  float m[RB], l[RB], bsum[RB];
+  uint32_t seen = 0;  // bit rb: the row sees a token with a page
+  v4f acc[RB][8];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    m[rb] = -INFINITY;
+    l[rb] = bsum[rb] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[rb][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  const int step = kWaves * kBlock;
+  int v0 = first + w * kBlock;
+  int32_t entry = -1;
+  if (v0 < last) {
+    load(v0, entry_of(v0));
+    entry = entry_of(v0 + step);
+  }
+  for (; v0 < last; v0 += step) {
+    const int t0 = run.position(v0);
+#pragma unroll
+    for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+      for (int x = 0; x < KW; ++x) {
+        const int row = 16 * mm + (BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3));
+        const int unit = BITS == 4 ? (lane & 3) ^ ((row >> 2) & 3) : (lane & 7) ^ (row & 7);
+        *reinterpret_cast<v4u*>(vlds + row * W::ROW + 16 * unit) = vc[mm][x];
+      }
+    const uint64_t there = __ballot(par_ok);
+    par.z = par.z == 0.0f ? 1.0f : par.z;  // a slot of a zeroed cache that was never written
+    const float rva = par_ok ? __fdiv_rn(1.0f, par.z) : 0.0f;
+    coef[0 * kBlock + lane] = par_ok ? par.x * cs24 : 0.0f;
+    coef[1 * kBlock + lane] = par_ok ? par.y * cs : 0.0f;
+    coef[2 * kBlock + lane] = par_ok ? __builtin_amdgcn_logf(par.z) : -INFINITY;
+    coef[3 * kBlock + lane] = rva;
+    coef[4 * kBlock + lane] = par_ok ? par.w * rva : 0.0f;
+    v4u kn[4][KW];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 0; x < KW; ++x) kn[j][x] = kc[j][x];
+    if (v0 + step < last) {
+      load(v0 + step, entry);
+      entry = entry_of(v0 + 2 * step);
+    }
+    asm volatile("" ::: "memory");
+
+    const uint32_t here = static_cast<uint32_t>(there >> (16 * g)) & 0xFFFFu;  // of the lane's tokens
+    const bool masked = t0 + kBlock > hi_least || (t0 < lo_most && t0 + kBlock > a.sinks);
+    uint32_t vis[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) vis[rb] = 0xFFFFu;
+    if (masked)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) vis[rb] = visible(rb, t0 + 16 * g);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) seen |= static_cast<uint32_t>((vis[rb] & here) != 0) << rb;
+
+    float s[RB][16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 ca = *reinterpret_cast<const float4*>(coef + 0 * kBlock + 16 * g + 4 * j);
+      const float4 cb = *reinterpret_cast<const float4*>(coef + 1 * kBlock + 16 * g + 4 * j);
+      const float4 cl = *reinterpret_cast<const float4*>(coef + 2 * kBlock + 16 * g + 4 * j);
+      const float* fa = &ca.x;
+      const float* fb = &cb.x;
+      const float* fl = &cl.x;
+      v8h ko[4];
+      if constexpr (BITS == 4) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t u = kn[j][0][2 * e], v = kn[j][0][2 * e + 1], u8 = u >> 8, v8 = v >> 8;
+          ko[2 * e] = operand(u & 0x000F000Fu, u8 & 0x000F000Fu, v & 0x000F000Fu, v8 & 0x000F000Fu);
+          ko[2 * e + 1] = operand(u & 0x00F000F0u, u8 & 0x00F000F0u, v & 0x00F000F0u, v8 & 0x00F000F0u);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t u = kn[j][x / 2][2 * (x & 1)], v = kn[j][x / 2][2 * (x & 1) + 1];
+          ko[x] = operand(u & 0x00FF00FFu, (u >> 8) & 0x00FF00FFu, v & 0x00FF00FFu, (v >> 8) & 0x00FF00FFu);
+        }
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        v4f se = {0.0f, 0.0f, 0.0f, 0.0f}, so = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          se = __builtin_amdgcn_mfma_f32_16x16x32_f16(ko[2 * e], qf[rb][2 * e], se, 0, 0, 0);
+          so = __builtin_amdgcn_mfma_f32_16x16x32_f16(ko[2 * e + 1], qf[rb][2 * e + 1], so, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float dot = BITS == 4 ? __fmaf_rn(so[r], 0.0625f, se[r]) : __fadd_rn(se[r], so[r]);
+          s[rb][4 * j + r] = __fmaf_rn(fa[r], dot, __fmaf_rn(fb[r], qsum[rb], fl[r]));
+        }
+      }
+    }
+    v8h pf[RB][2];
+    const auto weights = [&](int rb, auto mc) __attribute__((always_inline)) {
+      constexpr bool MASK = decltype(mc)::value;
+      const auto sees = [&](int x) { return (vis[rb] >> x) & 1u; };
+      if constexpr (MASK)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[rb][x] = sees(x) ? s[rb][x] : -INFINITY;
+      float top = s[rb][0];
+#pragma unroll
+      for (int x = 1; x < 16; ++x) top = fmaxf(top, s[rb][x]);
+      top = rows_all(top, [](float u, float v) { return fmaxf(u, v); });
+      if (__ballot(top - m[rb] > kWeightBits + kSlack)) {  // (m = -inf: any token)
+        const float mn = fmaxf(m[rb], fabsf(top) < kLargeScore ? top - kWeightBits : top);
+        const float f = rescale(m[rb], mn);
+        l[rb] *= f;
+        bsum[rb] *= f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) acc[rb][dt] *= f;
+        m[rb] = mn;
+      }
+      // weights rounded to fp16 in the value codes' pair order; l and b sum the rounded ones
+      const float from = m[rb] == -INFINITY ? 0.0f : m[rb];
+      uint32_t pw[8];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float4 cr0 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 8 * x);
+        const float4 cr1 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 8 * x + 4);
+        const float4 cv0 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 8 * x);
+        const float4 cv1 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 8 * x + 4);
+        const float fr[8] = {cr0.x, cr0.y, cr0.z, cr0.w, cr1.x, cr1.y, cr1.z, cr1.w};
+        const float fv[8] = {cv0.x, cv0.y, cv0.z, cv0.w, cv1.x, cv1.y, cv1.z, cv1.w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int ta = BITS == 4 ? y : 4 * (y >> 1) + (y & 1), tb = ta + (BITS == 4 ? 4 : 2);
+          const uint32_t p2 = f2h2(exp2_fast(s[rb][8 * x + ta] - from), exp2_fast(s[rb][8 * x + tb] - from));
+          pw[4 * x + y] = p2;
+          const v2h ph = __builtin_bit_cast(v2h, p2);
+          // (a weight of 0 does not hide parameters that are not finite)
+          const auto seen_only = [&](float v, int x8) { return !MASK || sees(8 * x + x8) ? v : 0.0f; };
+          l[rb] = __fmaf_rn(static_cast<float>(ph[0]), seen_only(fr[ta], ta), l[rb]);
+          l[rb] = __fmaf_rn(static_cast<float>(ph[1]), seen_only(fr[tb], tb), l[rb]);
+          bsum[rb] = __fmaf_rn(static_cast<float>(ph[0]), seen_only(fv[ta], ta), bsum[rb]);
+          bsum[rb] = __fmaf_rn(static_cast<float>(ph[1]), seen_only(fv[tb], tb), bsum[rb]);
+        }
+      }
+      pf[rb][0] = operand(pw[0], pw[1], pw[2], pw[3]);
+      pf[rb][1] = operand(pw[4], pw[5], pw[6], pw[7]);
+    };
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      if (masked)
+        weights(rb, std::true_type{});
+      else
+        weights(rb, std::false_type{});
+    }
+    typedef __attribute__((address_space(3))) v2i* lds_v2i;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        v8h vo;
+        if constexpr (BITS == 4) {
+          const int row = 16 * g + i;
+          const uint8_t* p = vlds + row * W::ROW + 16 * ((dt >> 1) ^ ((row >> 2) & 3)) + 8 * (dt & 1);
+          const v2i c2 = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i)(uintptr_t)(p));
+          const uint32_t u = static_cast<uint32_t>(c2[x]), u8 = u >> 8;
+          vo = operand(normal(u & 0x000F000Fu, 0), normal(u & 0x00F000F0u, 4), normal(u8 & 0x000F000Fu, 0), normal(u8 & 0x00F000F0u, 4));
+        } else {
+          const int row = 16 * g + 8 * x + (i >> 1);
+          const uint8_t* p = vlds + row * W::ROW + 16 * (dt ^ (row & 7)) + 8 * (i & 1);
+          const v2i c2 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(p));
+          const uint32_t u = static_cast<uint32_t>(c2[0]), v = static_cast<uint32_t>(c2[1]);
+          vo = operand(normal(u & 0x00FF00FFu, 0), normal((u >> 8) & 0x00FF00FFu, 0), normal(v & 0x00FF00FFu, 0),
+                       normal((v >> 8) & 0x00FF00FFu, 0));
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vo, pf[rb][x], acc[rb][dt], 0, 0, 0);
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+
+  // the waves' states of 16 rows at a time meet in LDS
+  const auto add = [](float u, float v) { return __fadd_rn(u, v); };
+  float* const red = reinterpret_cast<float*>(lds);   // [wave][row][kDimRow]
+  float* const red_ml = red + kWaves * 16 * kDimRow;  // [wave][row][2]
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    l[rb] = rows_all(l[rb], add);
+    bsum[rb] = rows_all(bsum[rb], add);
+    const float any = rows_all((seen >> rb) & 1u ? 1.0f : 0.0f, [](float u, float v) { return fmaxf(u, v); });
+    if (any == 0.0f) {  // hidden tokens alone: a query that is not finite has made their sums NaN
+      m[rb] = -INFINITY;
+      l[rb] = bsum[rb] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) acc[rb][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    } else if (m[rb] == -INFINITY) {
+      m[rb] = kNoScore;
+    }
+    const int left = min(16, rows - (r0 + 16 * rb));  // rows of this column
+    if (left <= 0) break;                             // the workgroup leaves together
+    __syncthreads();
+    if (g == 0) {
+      red_ml[(w * 16 + i) * 2] = m[rb];
+      red_ml[(w * 16 + i) * 2 + 1] = l[rb];
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      v4f o;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[r] = __fmaf_rn(acc[rb][dt][r], 512.0f, bsum[rb]);
+      *reinterpret_cast<v4f*>(red + (w * 16 + i) * kDimRow + 16 * dt + 4 * g) = o;
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < left * 32; x += 64 * kWaves) {
+      const int rr = x >> 5, d = 4 * (x & 31);
+      uint32_t tok, gh;
+      div_rem(static_cast<uint32_t>(r0 + 16 * rb + rr), a.group, magic_group, tok, gh);
+      if (a.cu && base + static_cast<int>(tok) < 0) continue;  // a row without a place
+      float M = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) M = fmaxf(M, red_ml[(v * 16 + rr) * 2]);
+      float L = 0.0f;
+      v4f D = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        const float f = rescale(red_ml[(v * 16 + rr) * 2], M);
+        L = __fmaf_rn(red_ml[(v * 16 + rr) * 2 + 1], f, L);
+        const v4f o = *reinterpret_cast<const v4f*>(red + (v * 16 + rr) * kDimRow + d);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) D[r] = __fmaf_rn(o[r], f, D[r]);
+      }
+      const int64_t t = tt.q0 + static_cast<int64_t>(tok), head = static_cast<int64_t>(hk) * a.group + gh;
+      float* pr = a.part + ((t * a.hq + head) * a.plan.chunks + c) * kAttnPart;
+      if (a.plan.chunks > 1 && c == 0 && d == 0) pr[2] = static_cast<float>(own);  // what the join goes by
+      if (own == 1) {
+        uint16_t* o = a.out + t * a.ldo + head * 128 + d;
+        if (M == -INFINITY)  // no token
+          *reinterpret_cast<v2u*>(o) = v2u{0u, 0u};
+        else
+          *reinterpret_cast<v2u*>(o) = v2u{f2h2(__fdiv_rn(D[0], L), __fdiv_rn(D[1], L)), f2h2(__fdiv_rn(D[2], L), __fdiv_rn(D[3], L))};
+      } else {
+        if (d == 0) {
+          pr[0] = M;
+          pr[1] = L;
+        }
+        *reinterpret_cast<v4f*>(pr + 4 + d) = D;
+      }
+    }
+  }
+}
+
+// One workgroup per (row, query head) of the sequences: the states of its chunks, of which the first one has the
+// number.  With one, its workgroup has written the output.
+template <int J>
+__global__ void __launch_bounds__(64 * J)
+attn_tree_combine(const float* part, const int32_t* cu, const int32_t* lens, int64_t B, uint16_t* out, int64_t ldo, int hq, int chunks,
+                  uint32_t magic_hq) {
+  __shared__ float red_m[J], red_l[J];
+  __shared__ float2 red_d[J][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  uint32_t t, h;
+  div_rem(blockIdx.x, hq, magic_hq, t, h);
+  const float* pr = part + static_cast<int64_t>(blockIdx.x) * chunks * kAttnPart;
+  const float number = pr[2];
+  if (cu) {
+    const RowSeq s = find_sequence(cu, lens, B, t);
+    if (s.seq < 0 || row_position(s.len, s.end, t) < 0) return;  // left as it was: nobody wrote its states
+  }
+  const int n = min(static_cast<int>(number), chunks);
+  if (n <= 1) return;
+  float M = -INFINITY, L = 0.0f, D0 = 0.0f, D1 = 0.0f;
+  constexpr int kAhead = 8;  // chunks whose loads are in flight together
+  for (int c0 = w; c0 < n; c0 += J * kAhead) {
+    float2 ml[kAhead], d[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {  // a chunk past the last is the last again, with weight 0
+      const float* p = pr + static_cast<int64_t>(min(c0 + J * x, n - 1)) * kAttnPart;
+      ml[x] = *reinterpret_cast<const float2*>(p);
+      d[x] = reinterpret_cast<const float2*>(p + 4)[lane];
+    }
+    float top = M;
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      if (c0 + J * x >= n) ml[x].x = -INFINITY;
+      top = fmaxf(top, ml[x].x);
+    }
+    const float f0 = rescale(M, top);
+    L *= f0;
+    D0 *= f0;
+    D1 *= f0;
+    M = top;
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const float f = rescale(ml[x].x, M);
+      L = __fmaf_rn(ml[x].y, f, L);
+      D0 = __fmaf_rn(d[x].x, f, D0);
+      D1 = __fmaf_rn(d[x].y, f, D1);
+    }
+  }
+  if constexpr (J > 1) {
+    red_d[w][lane] = make_float2(D0, D1);
+    if (lane == 0) {
+      red_m[w] = M;
+      red_l[w] = L;
+    }
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int v = 0; v < J; ++v) M = fmaxf(M, red_m[v]);
+    L = D0 = D1 = 0.0f;
+#pragma unroll
+    for (int v = 0; v < J; ++v) {
+      const float f = rescale(red_m[v], M);
+      const float2 d = red_d[v][lane];
+      L = __fmaf_rn(red_l[v], f, L);
+      D0 = __fmaf_rn(d.x, f, D0);
+      D1 = __fmaf_rn(d.y, f, D1);
+    }
+  }
+  reinterpret_cast<uint32_t*>(out + t * ldo + static_cast<int64_t>(h) * 128)[lane] =
+      M == -INFINITY ? 0u : f2h2(__fdiv_rn(D0, L), __fdiv_rn(D1, L));
+}
+
+template <int BITS, bool P16, int RB>
+hipError_t launch_part(const TreeArgs& a, hipStream_t stream) {
+  constexpr auto kern = attn_tree_part<BITS, P16, RB>;
+  constexpr int lds = tree_lds<BITS>();
+  const hipError_t init = set_max_lds<kern>(lds);
+  if (init != hipSuccess) return init;
+  const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.plan.tiles) * a.cache.heads * a.plan.chunks);
+  return launch(kern, dim3(blocks), dim3(64 * kWaves), lds, stream, a.q, a.cu, a.lens, div_magic(static_cast<uint32_t>(a.plan.tiles)),
+                div_magic(static_cast<uint32_t>(a.cache.heads)), div_magic(static_cast<uint32_t>(a.group)), a);
+}
+
+template <int RB>
+hipError_t launch_parts(const TreeArgs& a, hipStream_t stream) {
+  if (a.bits == 8) return a.param16 ? launch_part<8, true, RB>(a, stream) : launch_part<8, false, RB>(a, stream);
+  return a.param16 ? launch_part<4, true, RB>(a, stream) : launch_part<4, false, RB>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_attn_tree(const TreeArgs& a, hipStream_t stream) {
+  const hipError_t e = a.plan.rb == 1   ? launch_parts<1>(a, stream)
+                       : a.plan.rb == 2 ? launch_parts<2>(a, stream)
+                                        : launch_parts<4>(a, stream);
+  if (e != hipSuccess || a.plan.chunks == 1) return e;
+  const auto join = [&](auto kern, int waves) {
+    return launch(kern, dim3(static_cast<unsigned>(a.T * a.hq)), dim3(64 * waves), 0, stream, a.part, a.cu, a.lens, a.B, a.out, a.ldo,
+                  a.hq, a.plan.chunks, div_magic(static_cast<uint32_t>(a.hq)));
+  };
+  return a.plan.chunks <= 8 ? join(attn_tree_combine<1>, 1) : join(attn_tree_combine<8>, 8);
+}
+
+}  // namespace sq

@@ -90,21 +90,6 @@ __device__ __forceinline__ void pace() {
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
-// Inclusive sum over the lanes of a wave up to each: rows of 16 by shifts, then the rows' totals.
-__device__ __forceinline__ int wave_scan(int v) {
-  const auto add = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
-    v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
-  };
-  using std::integral_constant;
-  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});  // row_shr:1
-  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
-  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
-  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
-  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15
-  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
-  return v;
-}
-
 // Sequence and tile of the tile number `rem` among ceil(rows / ROWS) tiles a sequence.
 struct PromptTile {
   int seq;          // -1: past the last
@@ -139,7 +124,9 @@ __device__ __forceinline__ PromptTile find_tile(const int32_t* cu_q, const int32
   return {-1, 0, 0, 0, 0, 0, 0};
 }
 
-template <bool SPLIT, int KG>
+// WIN: a row sees the keys up to its own from lim - window + 1 on, and those below sinks; the workgroup's tiles
+// are those of its rows' run of keys (paged.h), the first ones with keys below sinks and then the windows'.
+template <bool SPLIT, int KG, bool WIN>
 __global__ void __launch_bounds__(64 * kWaves, 2)
 attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* cu_q, const int32_t* cu_k,
                  uint32_t magic_heads, uint32_t magic_group, uint32_t magic_splits, PromptArgs a) {
@@ -180,7 +167,11 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   const int lim = limit(row);
   const int wave_lo = limit(tile * P::ROWS + 32 * rw), wave_hi = limit(tile * P::ROWS + 32 * rw + 31);
   const int keys = limit(tile * P::ROWS + P::ROWS - 1) + 1;  // of the workgroup
-  const int tiles_all = keys > 0 ? (keys + kTile - 1) / kTile : 0;
+  // with a window: the first key of this row's, of the wave's last row's, and the workgroup's run of keys
+  const int lo = WIN ? max(lim - a.window + 1, 0) : 0, wave_lo_key = WIN ? max(wave_hi - a.window + 1, 0) : 0;
+  const TokenRun run = WIN ? token_run(limit(tile * P::ROWS), keys, a.window, a.sinks) : TokenRun{0, 0, max(keys, 0)};
+  const int gap = (run.start - run.head) / kTile, head_tiles = run.head / kTile;  // tiles that the run leaves out, and before them
+  const int tiles_all = (run.tokens + kTile - 1) / kTile;
   int kt0 = 0, kt1 = tiles_all;
   if constexpr (SPLIT) {
     const int per = prompt_part(tiles_all, a.splits, a.per);
@@ -283,11 +274,14 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     constexpr bool MASK = decltype(mc)::value;
     if constexpr (MASK) {
       const int left = lim - kt * kTile - 4 * h;
+      const int from = lo - kt * kTile - 4 * h, always = a.sinks - kt * kTile - 4 * h;
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * mt + 8 * (r >> 2) + (r & 3) > left) s[mt][r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) {
+          const int x = 32 * mt + 8 * (r >> 2) + (r & 3);
+          if (x > left || (WIN && x < from && x >= always)) s[mt][r] = -INFINITY;
+        }
     }
     float top = s[0][0];
 #pragma unroll
@@ -342,7 +336,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   auto add_odd = [&](int kt, int buf) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int t = 0; t < kTile; ++t) {
-      if (kt * kTile + t > lim) continue;
+      if (kt * kTile + t > lim || (WIN && kt * kTile + t < lo && kt * kTile + t >= a.sinks)) continue;
 #pragma unroll 1
       for (int c = 0; c < 16; ++c) {
         const v2u u = *reinterpret_cast<const v2u*>(lds + (4 * kg + 2 + buf) * kTileBytes + t * 256 + 16 * (c ^ swizzle(t)) + 8 * h);
@@ -404,12 +398,17 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   // phase 2 i the buffers of keys i + 1 and values i are free, and the copies have until the end of
   // the next phase to land.
   // With two groups of waves (KG 2) a group's tiles are every second one, in buffers of its own.
-  const auto tile_of = [&](int j) { return kt0 + KG * j + kg; };
+  // (the j-th tile of the group among those of the sequence; kt0 and kt1 count those of the run)
+  const auto tile_of = [&](int j) {
+    const int x = kt0 + KG * j + kg;
+    return WIN && x >= head_tiles ? x + gap : x;
+  };
   const auto count = [&](int end) { return max((end - kt0 - kg + KG - 1) / KG, 0); };  // of its tiles before `end`
   const int n = (kt1 - kt0 + KG - 1) / KG;                   // steps of the workgroup
   const int ng = count(kt1);                                 // tiles of the group,
-  const int nw = wave_hi < 0 ? 0 : min(ng, count(wave_hi / kTile + 1));  // that a row of the wave sees a key of,
-  const int nf = wave_lo < 0 ? 0 : min(nw, count((wave_lo + 1) / kTile));  // and that every row sees whole
+  const int nw = wave_hi < 0 ? 0 : min(ng, count(wave_hi / kTile + 1 - gap));  // that a row of the wave sees a key of,
+  const int nf = wave_lo < 0 ? 0 : min(nw, count((wave_lo + 1) / kTile - gap));  // and that every row sees whole,
+  const int na = WIN ? min(nw, count((wave_lo_key + kTile - 1) / kTile - gap)) : 0;  // but for these first ones
   const auto fetch = [&](int i) __attribute__((always_inline)) {  // in phase 2 i
     if (i + 1 < ng) issue(tile_of(i + 1), (i + 1) & 1, true);
     if (i < ng) issue(tile_of(i), i & 1, false);
@@ -457,6 +456,27 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       softmax(tile_of(j), std::false_type{});
       end_softmax();
     };
+    if constexpr (WIN) {  // tiles with keys before some row's window, and the first whole ones up to an odd j
+      if (na > 0) {
+        for (; j < na; ++j) {
+          values(tile_of(j - 1), (j - 1) & 1, std::true_type{});
+          scores(j & 1);
+          end_products(j);
+          softmax(tile_of(j), std::true_type{});
+          end_softmax();
+        }
+        for (bool masked = true; j < nf && (masked || !(j & 1)); ++j, masked = false) {
+          if (masked)
+            values(tile_of(j - 1), (j - 1) & 1, std::true_type{});
+          else
+            values(tile_of(j - 1), (j - 1) & 1, std::false_type{});
+          scores(j & 1);
+          end_products(j);
+          softmax(tile_of(j), std::false_type{});
+          end_softmax();
+        }
+      }
+    }
     for (; j + 1 < nf; j += 2) {
       whole(j, 1);
       whole(j + 1, 0);
@@ -470,7 +490,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     // 2048 tokens of 32 heads 53 -> 49 us, 16 packed prompts 447 -> 431, 37 and 4 tokens over 16000
     // and 6000 keys 39.7 -> 36.4.
     for (; j < nw; ++j) {
-      if (j > nf)
+      if (j > nf || j <= na)
         values(tile_of(j - 1), (j - 1) & 1, std::true_type{});
       else
         values(tile_of(j - 1), (j - 1) & 1, std::false_type{});
@@ -479,7 +499,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       softmax(tile_of(j), std::true_type{});
       end_softmax();
     }
-    if (nw > nf)
+    if (nw > nf || nw <= na)
       values(tile_of(nw - 1), (nw - 1) & 1, std::true_type{});
     else
       values(tile_of(nw - 1), (nw - 1) & 1, std::false_type{});
@@ -520,7 +540,13 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     down |= odds[rw * 128 + 64 + lane];
   }
   if (row >= rows) return;
-  if (mx == -INFINITY && lim >= kt0 * kTile) mx = kNoScore;  // it sees a key of this part, but no score above -inf
+  bool sees = lim >= kt0 * kTile;  // a key of this part
+  if constexpr (WIN) {
+    const int p0 = (kt0 < head_tiles ? kt0 : kt0 + gap) * kTile;  // its first key; from the windows' first tile on, and its end
+    const int w0 = (max(kt0, head_tiles) + gap) * kTile, w1 = (kt1 + gap) * kTile;
+    sees = p0 < min(a.sinks, lim + 1) || (kt1 > head_tiles && max(lo, w0) <= min(lim, w1 - 1));
+  }
+  if (mx == -INFINITY && sees) mx = kNoScore;  // but no score above -inf
   const float inv = SPLIT ? 1.0f : mx == -INFINITY ? 0.0f : __fdiv_rn(1.0f, l);  // a row that sees nothing is zero
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) acc[dt] *= inv;
@@ -591,9 +617,13 @@ attn_prompt_combine(const float* part, const int32_t* cu_q, const int32_t* cu_k,
     uint32_t hk, gh, tok, x;
     div_rem(head, a.group, magic_group, hk, gh);
     const int row = (static_cast<int>(t) - q0) * a.group + static_cast<int>(gh);
-    const int last = min(row / kPromptRows * kPromptRows + kPromptRows - 1, n * a.group - 1);
+    const int first = row / kPromptRows * kPromptRows, last = min(first + kPromptRows - 1, n * a.group - 1);
     div_rem(static_cast<uint32_t>(last), a.group, magic_group, tok, x);
     keys = min(m - n + static_cast<int>(tok) + 1, m);
+    if (a.window > 0) {
+      div_rem(static_cast<uint32_t>(first), a.group, magic_group, tok, x);
+      keys = token_run(m - n + static_cast<int>(tok), keys, a.window, a.sinks).tokens;
+    }
   }
   const int tiles = keys > 0 ? (keys + kTile - 1) / kTile : 0;
   const int per = prompt_part(tiles, a.splits, a.per);
@@ -616,10 +646,10 @@ attn_prompt_combine(const float* part, const int32_t* cu_q, const int32_t* cu_k,
       M == -INFINITY ? 0u : f2h2(__fdiv_rn(D0, L), __fdiv_rn(D1, L));
 }
 
-template <bool SPLIT, int KG>
-hipError_t launch_tiles(const PromptArgs& a, hipStream_t stream) {
+template <bool SPLIT, int KG, bool WIN>
+hipError_t launch_form(const PromptArgs& a, hipStream_t stream) {
   using P = Prompt<KG>;
-  constexpr auto kern = attn_prompt_tile<SPLIT, KG>;
+  constexpr auto kern = attn_prompt_tile<SPLIT, KG, WIN>;
   const hipError_t init = set_max_lds<kern>(P::LDS);
   if (init != hipSuccess) return init;
   // as many tiles as any division of the rows among B sequences can make
@@ -627,6 +657,11 @@ hipError_t launch_tiles(const PromptArgs& a, hipStream_t stream) {
   return launch(kern, dim3(static_cast<unsigned>(tiles * a.hkv * a.splits)), dim3(64 * kWaves), P::LDS, stream, a.q, a.k, a.v, a.cu_q,
                 a.cu_k, div_magic(static_cast<uint32_t>(a.hkv)), div_magic(static_cast<uint32_t>(a.group)),
                 div_magic(static_cast<uint32_t>(a.splits)), a);
+}
+
+template <bool SPLIT, int KG>
+hipError_t launch_tiles(const PromptArgs& a, hipStream_t stream) {
+  return a.window > 0 ? launch_form<SPLIT, KG, true>(a, stream) : launch_form<SPLIT, KG, false>(a, stream);
 }
 
 }  // namespace

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "paged.h"
+#include "paged_plan.h"
 
 namespace sq {
 
@@ -186,6 +187,7 @@ struct RopeWriteArgs {
   const int32_t* cu;     // [B + 1] first row of each sequence; nullptr: row t is sequence t
   const int32_t* lens;   // [B] tokens in the cache, the new ones included
   int64_t B;
+  const int32_t* depth;  // [T] position of a row behind the first new token's, or nullptr: as in the cache
   PagedCache cache;
   const double* freq;    // [rotary / 2] radians per position
   int32_t rotary, interleaved;
@@ -231,6 +233,80 @@ struct PagedAttnArgs {
 };
 hipError_t launch_attn_paged(const PagedAttnArgs& a, hipStream_t stream);
 
+struct TreeArgs {
+  const uint16_t* q;     // fp16 [T, ldq]: hq rotated heads of 128
+  int64_t ldq;
+  const int32_t* cu;     // [B + 1] or nullptr: row t is the last token of sequence t
+  const int32_t* lens;   // [B]
+  int64_t B, T;
+  const int32_t* mask;   // [T, ldm] words of the drafts that a row sees, or nullptr: a chain
+  int64_t ldm;
+  int32_t words;
+  const int32_t* depth;  // [T] or nullptr
+  int32_t window, sinks;
+  int32_t hq, group;
+  PagedCache cache;
+  int32_t bits, param16;
+  int32_t max_len;
+  float scale_log2e;
+  uint16_t* out;         // fp16 [T, ldo]
+  int64_t ldo;
+  TreePlan plan;
+  float* part;           // [T, hq, chunks, kAttnPart]; unused with one chunk
+};
+hipError_t launch_attn_tree(const TreeArgs& a, hipStream_t stream);
+
+struct TreeMaskArgs {
+  const int32_t* parents;  // [T]
+  const int32_t* cu;       // [B + 1]
+  const int32_t* lens;     // [B], read with window and sinks alone
+  int64_t B, T;
+  int32_t window, sinks;
+  int32_t* mask;           // [T, ldm]
+  int64_t ldm;
+  int32_t words;
+  int32_t* depth;          // [T]
+};
+hipError_t launch_tree_mask(const TreeMaskArgs& a, hipStream_t stream);
+
+// The page tables (sq_paged_release, sq_paged_grow).
+struct PoolArgs {
+  int32_t* held;         // [B]
+  int64_t B;
+  int32_t* table;        // [B, ldt]
+  int64_t ldt;
+  int32_t cols, shift;
+  int32_t* pool;         // [pages]
+  int32_t* count;        // [1]
+  int32_t pages;
+};
+hipError_t launch_paged_release(const PoolArgs& p, const int32_t* first, const int32_t* end, hipStream_t stream);
+struct GrowArgs {
+  const int32_t* have;   // [B]
+  const int32_t* add;    // [B]
+  int64_t T;
+  int32_t* lens;         // [B]
+  int32_t* cu;           // [B + 1]
+  int32_t* pos;          // [T]
+  int64_t* slots;        // [T]
+  int32_t* missing;      // [2]
+};
+hipError_t launch_paged_grow(const PoolArgs& p, const GrowArgs& g, hipStream_t stream);
+
+struct KeepArgs {
+  const int32_t* cu;
+  const int32_t* lens;
+  int64_t B;
+  const int32_t* path;   // [B, ldp]
+  int64_t ldp;
+  int32_t most;          // entries of a row that count
+  const int32_t* kept;   // [B]
+  PagedCache cache;
+  int32_t bits, param16;
+  int32_t* lens_out;     // [B]
+};
+hipError_t launch_kv_keep(const KeepArgs& a, hipStream_t stream);
+
 struct PromptArgs {
   const uint16_t* q;     // fp16 [Tq, ldq]: hq heads of 128
   const uint16_t* k;     // fp16 [Tk, ldk]: hkv heads of 128
@@ -242,6 +318,7 @@ struct PromptArgs {
   int32_t hq, hkv, group;
   float scale_log2e;
   int32_t causal;
+  int32_t window, sinks;  // window > 0 (causal alone): the keys a row sees end `window` before it, but for the first sinks
   uint16_t* out;         // fp16 [Tq, ldo]
   int64_t ldo;
   int32_t half, splits, per;  // the PromptPlan

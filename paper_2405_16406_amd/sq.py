@@ -24,7 +24,10 @@ EXPORTS = ("sq_abi_version", "sq_last_error", "sq_time_next_call", "sq_hadamard_
            "sq_w4a4_linear_swiglu", "sq_qk_had_kvquant", "sq_qk_had_kvquant_ex", "sq_attn_decode_kv4",
            "sq_attn_decode_kv4_ex", "sq_attn_decode_workspace", "sq_attn_decode_kv4_split",
            "sq_attn_decode_kv4_split_noalloc", "sq_rope_frequencies", "sq_rope_kv_write", "sq_kv_read",
-           "sq_attn_paged", "sq_attn_paged_workspace", "sq_attn_prompt", "sq_attn_prompt_workspace")
+           "sq_attn_paged", "sq_attn_paged_workspace", "sq_attn_prompt", "sq_attn_prompt_workspace", "sq_tree_mask",
+           "sq_rope_kv_write_ex", "sq_attn_tree", "sq_attn_tree_workspace", "sq_attn_paged_window",
+           "sq_attn_paged_window_workspace", "sq_attn_prompt_window", "sq_attn_prompt_window_workspace",
+           "sq_paged_release", "sq_paged_grow", "sq_kv_keep")
 
 
 class SqError(RuntimeError):
@@ -116,6 +119,34 @@ def load(path: str) -> ctypes.CDLL:
                                  _I32, _P, _I64, _P, _U64, _P]
     L.sq_attn_prompt_workspace.restype = _I32
     L.sq_attn_prompt_workspace.argtypes = [_I64, _I64, _I64, _I64, _I64, _I64, _P]
+    L.sq_tree_mask.restype = _I32
+    L.sq_tree_mask.argtypes = [_P, _P, _P, _I64, _I64, _I32, _I32, _P, _I64, _I64, _P, _P]
+    L.sq_rope_kv_write_ex.restype = _I32
+    L.sq_rope_kv_write_ex.argtypes = [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _I64, _I64,
+                                      _P, _P, _P, _I64, _I64, _I64, _I32, _I32, _P, _I32, _I32, _F32, _F32, _F32,
+                                      _P, _P, _P]
+    L.sq_attn_tree.restype = _I32
+    L.sq_attn_tree.argtypes = [_P, _I64, _P, _P, _I64, _I64, _P, _I64, _I64, _P, _I32, _I32, _P, _I64, _I64, _P, _P, _P,
+                               _I64, _I64, _I64, _I64, _I64, _I32, _I32, _I64, _F32, _P, _I64, _P, _U64, _P]
+    L.sq_attn_tree_workspace.restype = _I32
+    L.sq_attn_tree_workspace.argtypes = [_I64, _I64, _I64, _I32, _I32, _I64, _I64, _I64, _P]
+    L.sq_attn_paged_window.restype = _I32
+    L.sq_attn_paged_window.argtypes = [_P, _I64, _P, _I64, _I32, _I32, _P, _I64, _I64, _P, _P, _P, _I64, _I64, _I64, _I64,
+                                       _I64, _I32, _I32, _I64, _F32, _P, _I64, _P, _U64, _P]
+    L.sq_attn_paged_window_workspace.restype = _I32
+    L.sq_attn_paged_window_workspace.argtypes = [_I64, _I64, _I32, _I32, _I64, _I64, _I64, _P]
+    L.sq_attn_prompt_window.restype = _I32
+    L.sq_attn_prompt_window.argtypes = [_P, _I64, _P, _I64, _P, _I64, _P, _P, _I64, _I64, _I64, _I64, _I64, _I64, _F32,
+                                        _I32, _I32, _P, _I64, _P, _U64, _P]
+    L.sq_attn_prompt_window_workspace.restype = _I32
+    L.sq_attn_prompt_window_workspace.argtypes = [_I64, _I64, _I64, _I32, _I32, _I64, _I64, _I64, _P]
+    L.sq_paged_release.restype = _I32
+    L.sq_paged_release.argtypes = [_P, _P, _P, _I64, _P, _I64, _I64, _I64, _P, _P, _I64, _P]
+    L.sq_paged_grow.restype = _I32
+    L.sq_paged_grow.argtypes = [_P, _P, _P, _I64, _I64, _P, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _P, _P, _P, _P]
+    L.sq_kv_keep.restype = _I32
+    L.sq_kv_keep.argtypes = [_P, _P, _I64, _P, _I64, _I64, _P, _P, _I64, _I64, _P, _P, _P, _I64, _I64, _I64, _I64, _I32,
+                             _I32, _P, _P]
     return L
 
 
@@ -518,12 +549,14 @@ def _same_device(t, *others):
 
 
 def rope_kv_write(q, k, v, cache, block_table, lens, freq=None, cu=None, interleaved: bool = False, magnitude: float = 1.0,
-                  k_clip: float = 1.0, v_clip: float = 1.0, out=None, k_out=None):
+                  k_clip: float = 1.0, v_clip: float = 1.0, out=None, k_out=None, depth=None):
     """Rotary positions and R3 on q, k and the quantized write of k, v into the pages
     (sq_rope_kv_write).  q fp16 [T, Hq, 128], k, v fp16 [T, Hkv, 128] before positions (slices of a
     fused projection are fine); lens int32 [B] with the new tokens; cu int32 [B + 1], or None for one
     token a sequence; freq fp64 [rotary_dim / 2] (rope_frequencies), None for no positions.
-    k_out: optional fp16 [T, Hkv, 128] that takes the rotated keys.  Returns q rotated, fp16 [T, Hq, 128]."""
+    k_out: optional fp16 [T, Hkv, 128] that takes the rotated keys.  depth: int32 [T], each row's position behind
+    its sequence's first new token where that is not its place (drafts of a tree, tree_mask;
+    sq_rope_kv_write_ex).  Returns q rotated, fp16 [T, Hq, 128]."""
     T, Hq, ldq = _heads(q, "q")
     tk, Hkv, ldk = _heads(k, "k")
     tv, hv, ldv = _heads(v, "v")
@@ -546,19 +579,28 @@ def rope_kv_write(q, k, v, cache, block_table, lens, freq=None, cu=None, interle
             _need(t, torch.float16, n)
             if tuple(t.shape) != (T, h, 128) or not t.is_contiguous():
                 raise ValueError(f"{n} must be contiguous [{T}, {h}, 128]")
+    if depth is not None:
+        _index(depth, "depth", T)
     if out is None:
         out = q.new_empty((T, Hq, 128))
-    d = _same_device(q, k, v, *cache, block_table, lens, cu, freq, out, k_out)
+    d = _same_device(q, k, v, *cache, block_table, lens, cu, freq, out, k_out, depth)
     if T == 0 or B == 0:  # an empty tensor has no address
         return out
     if d != _current_device():
         with torch.cuda.device(d):
-            return rope_kv_write(q, k, v, cache, block_table, lens, freq, cu, interleaved, magnitude, k_clip, v_clip, out, k_out)
-    status = lib().sq_rope_kv_write(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, Hq, 128, _ptr(cu),
-                                    lens.data_ptr(), B, *args, *bits, _ptr(freq), rotary, int(interleaved), magnitude,
-                                    k_clip, v_clip, out.data_ptr(), _ptr(k_out), _stream(q))
+            return rope_kv_write(q, k, v, cache, block_table, lens, freq, cu, interleaved, magnitude, k_clip, v_clip, out, k_out,
+                                 depth)
+    if depth is None:
+        status = lib().sq_rope_kv_write(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, Hq, 128, _ptr(cu),
+                                        lens.data_ptr(), B, *args, *bits, _ptr(freq), rotary, int(interleaved), magnitude,
+                                        k_clip, v_clip, out.data_ptr(), _ptr(k_out), _stream(q))
+    else:
+        status = lib().sq_rope_kv_write_ex(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, Hq, 128, _ptr(cu),
+                                           lens.data_ptr(), B, depth.data_ptr(), *args, *bits, _ptr(freq), rotary,
+                                           int(interleaved), magnitude, k_clip, v_clip, out.data_ptr(), _ptr(k_out),
+                                           _stream(q))
     if status:
-        _check(status, "sq_rope_kv_write")
+        _check(status, "sq_rope_kv_write" if depth is None else "sq_rope_kv_write_ex")
     return out
 
 
@@ -592,16 +634,22 @@ def kv_read(cache, block_table, lens, cu, rows: int, plain_basis: bool = False, 
     return k, v
 
 
-def attn_paged_workspace_bytes(B, max_len, Hq, Hkv):
+def attn_paged_workspace_bytes(B, max_len, Hq, Hkv, window: int = 0, sinks: int = 0):
     """Device bytes of attn_paged's workspace on the current device."""
     n = _U64(0)
+    if window:
+        _check(lib().sq_attn_paged_window_workspace(B, max_len, window, sinks, Hq, Hkv, 128, ctypes.byref(n)),
+               "sq_attn_paged_window_workspace")
+        return n.value
     _check(lib().sq_attn_paged_workspace(B, max_len, Hq, Hkv, 128, ctypes.byref(n)), "sq_attn_paged_workspace")
     return n.value
 
 
-def attn_paged(q, cache, block_table, lens, max_len: int, scale=None, out=None, workspace=None):
+def attn_paged(q, cache, block_table, lens, max_len: int, scale=None, out=None, workspace=None, window: int = 0,
+               sinks: int = 0):
     """Attention of one rotated query per sequence over its pages (sq_attn_paged): q fp16
-    [B, Hq, 128]; max_len at least the longest of lens.  workspace: a uint8 device tensor of at least
+    [B, Hq, 128]; max_len at least the longest of lens.  window: over the last `window` tokens and the
+    first `sinks` ones alone (sq_attn_paged_window); 0: over all.  workspace: a uint8 device tensor of at least
     attn_paged_workspace_bytes() bytes, allocated here when None.  Returns out fp16 [B, Hq, 128]."""
     B, Hq, ldq = _heads(q, "q")
     _index(lens, "lens", B)
@@ -617,31 +665,41 @@ def attn_paged(q, cache, block_table, lens, max_len: int, scale=None, out=None, 
         return out
     if d != _current_device():
         with torch.cuda.device(d):
-            return attn_paged(q, cache, block_table, lens, max_len, scale, out, workspace)
+            return attn_paged(q, cache, block_table, lens, max_len, scale, out, workspace, window, sinks)
     if workspace is None:
-        size = attn_paged_workspace_bytes(B, max_len, Hq, args[-1])
+        size = attn_paged_workspace_bytes(B, max_len, Hq, args[-1], window, sinks)
         workspace = q.new_empty(size, dtype=_U8) if size else None
     else:
         size = _workspace_bytes(workspace)
-    status = lib().sq_attn_paged(q.data_ptr(), ldq, lens.data_ptr(), B, *args, Hq, 128, *bits, max_len,
-                                 0.08838834764831845 if scale is None else scale, out.data_ptr(), ldo, _ptr(workspace), size,
-                                 _stream(q))
+    scale = 0.08838834764831845 if scale is None else scale
+    if window:
+        status = lib().sq_attn_paged_window(q.data_ptr(), ldq, lens.data_ptr(), B, window, sinks, *args, Hq, 128, *bits, max_len,
+                                            scale, out.data_ptr(), ldo, _ptr(workspace), size, _stream(q))
+    else:
+        status = lib().sq_attn_paged(q.data_ptr(), ldq, lens.data_ptr(), B, *args, Hq, 128, *bits, max_len, scale, out.data_ptr(),
+                                     ldo, _ptr(workspace), size, _stream(q))
     if status:
-        _check(status, "sq_attn_paged")
+        _check(status, "sq_attn_paged_window" if window else "sq_attn_paged")
     return out
 
 
-def attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv):
+def attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv, window: int = 0, sinks: int = 0):
     """Device bytes of attn_prompt's workspace on the current device."""
     n = _U64(0)
+    if window:
+        _check(lib().sq_attn_prompt_window_workspace(B, Tq, Tk, window, sinks, Hq, Hkv, 128, ctypes.byref(n)),
+               "sq_attn_prompt_window_workspace")
+        return n.value
     _check(lib().sq_attn_prompt_workspace(B, Tq, Tk, Hq, Hkv, 128, ctypes.byref(n)), "sq_attn_prompt_workspace")
     return n.value
 
 
-def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, workspace=None):
+def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, workspace=None, window: int = 0,
+                sinks: int = 0):
     """Attention of packed sequences (sq_attn_prompt): q fp16 [Tq, Hq, 128], k, v fp16 [Tk, Hkv, 128],
     sequence b the rows cu_q[b] .. of q and cu_k[b] .. of k and v (int32 [B + 1] each); causal: its
-    queries are its last tokens.  workspace: a uint8 device tensor of at least
+    queries are its last tokens.  window (causal alone): a query sees the last `window` keys up to its own and
+    the first `sinks` ones (sq_attn_prompt_window); 0: all up to its own.  workspace: a uint8 device tensor of at least
     attn_prompt_workspace_bytes() bytes, allocated here when None.  Returns out fp16 [Tq, Hq, 128]; rows
     of no sequence are left as they are in `out` (allocated unset when None)."""
     Tq, Hq, ldq = _heads(q, "q")
@@ -651,6 +709,8 @@ def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, 
         raise ValueError("k and v disagree on their rows or heads")
     B = _index(cu_q, "cu_q") - 1
     _index(cu_k, "cu_k", B + 1)
+    if window and not causal:
+        raise ValueError("a window needs causal attention")
     if out is None:
         out, ldo = q.new_empty((Tq, Hq, 128)), Hq * 128
     else:
@@ -662,15 +722,195 @@ def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, 
         return out
     if d != _current_device():
         with torch.cuda.device(d):
-            return attn_prompt(q, k, v, cu_q, cu_k, scale, causal, out, workspace)
+            return attn_prompt(q, k, v, cu_q, cu_k, scale, causal, out, workspace, window, sinks)
     if workspace is None:
-        size = attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv)
+        size = attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv, window, sinks)
         workspace = q.new_empty(size, dtype=_U8) if size else None
     else:
         size = _workspace_bytes(workspace)
-    status = lib().sq_attn_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(), cu_k.data_ptr(), B,
-                                  Tq, Tk, Hq, Hkv, 128, 0.08838834764831845 if scale is None else scale, int(causal),
-                                  out.data_ptr(), ldo, _ptr(workspace), size, _stream(q))
+    scale = 0.08838834764831845 if scale is None else scale
+    if window:
+        status = lib().sq_attn_prompt_window(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(),
+                                             cu_k.data_ptr(), B, Tq, Tk, Hq, Hkv, 128, scale, window, sinks, out.data_ptr(), ldo,
+                                             _ptr(workspace), size, _stream(q))
+    else:
+        status = lib().sq_attn_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(), cu_k.data_ptr(),
+                                      B, Tq, Tk, Hq, Hkv, 128, scale, int(causal), out.data_ptr(), ldo, _ptr(workspace), size,
+                                      _stream(q))
     if status:
-        _check(status, "sq_attn_prompt")
+        _check(status, "sq_attn_prompt_window" if window else "sq_attn_prompt")
+    return out
+
+
+# ------------------------------------------------------------------ drafts and page tables
+
+def _rows_of(t, name, rows, dtype=torch.int32):
+    """Row stride and columns of a 2-D tensor of `rows` rows with unit column stride on the GPU."""
+    _need(t, dtype, name)
+    if t.dim() != 2 or t.shape[0] != rows or (t.stride(1) != 1 and t.shape[1] > 1) or t.shape[1] < 1:
+        raise ValueError(f"{name} must be [{rows}, columns] with unit column stride")
+    return (t.stride(0) if rows > 1 else t.shape[1]), t.shape[1]
+
+
+def tree_mask(parents, cu, most: int, lens=None, window: int = 0, sinks: int = 0, out=None):
+    """What each draft of a tree sees of the drafts, from their parents (sq_tree_mask): parents int32 [T],
+    indexes within the sequence (-1: a root), cu int32 [B + 1], most: at least the drafts of any
+    sequence; lens int32 [B], drafts included, needed with window and sinks.  Returns (mask int32
+    [T, ceil(most / 32)], depth int32 [T]); out: that pair.  Rows of no sequence are left as they are."""
+    T = _index(parents, "parents")
+    B = _index(cu, "cu") - 1
+    if lens is not None:
+        _index(lens, "lens", B)
+    if out is None:
+        mask, depth = parents.new_empty((T, max(1, (most + 31) // 32))), torch.empty_like(parents)
+    else:
+        mask, depth = out
+        _index(depth, "depth", T)
+    ld, words = _rows_of(mask, "mask", T)
+    d = _same_device(parents, cu, lens, mask, depth)
+    if T == 0 or B == 0:
+        return mask, depth
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return tree_mask(parents, cu, most, lens, window, sinks, (mask, depth))
+    status = lib().sq_tree_mask(parents.data_ptr(), cu.data_ptr(), _ptr(lens), B, T, window, sinks, mask.data_ptr(), ld, words,
+                                depth.data_ptr(), _stream(parents))
+    if status:
+        _check(status, "sq_tree_mask")
+    return mask, depth
+
+
+def attn_tree_workspace_bytes(B, T, max_len, Hq, Hkv, window: int = 0, sinks: int = 0):
+    """Device bytes of attn_tree's workspace on the current device."""
+    n = _U64(0)
+    _check(lib().sq_attn_tree_workspace(B, T, max_len, window, sinks, Hq, Hkv, 128, ctypes.byref(n)), "sq_attn_tree_workspace")
+    return n.value
+
+
+def attn_tree(q, cache, block_table, lens, cu, max_len: int, mask=None, depth=None, window: int = 0, sinks: int = 0, scale=None,
+              out=None, workspace=None):
+    """Attention of each sequence's last tokens over its pages (sq_attn_tree): q fp16 [T, Hq, 128], rows
+    packed by cu int32 [B + 1]; lens int32 [B] with them, max_len at least the longest.  mask int32
+    [T, words]: the drafts that each row sees (tree_mask), all tokens before them besides; None: a
+    chain, each sees those before it.  window, sinks: the last `window` tokens and the first `sinks` ones alone, by
+    the rows' depth (int32 [T]) with a mask.  workspace: a uint8 device tensor of at least
+    attn_tree_workspace_bytes() bytes, allocated here when None.  Returns out fp16 [T, Hq, 128]; rows of
+    no sequence are left as they are in `out` (allocated unset when None)."""
+    T, Hq, ldq = _heads(q, "q")
+    B = _index(lens, "lens")
+    _index(cu, "cu", B + 1)
+    args, bits = _cache_args(cache, block_table, B)
+    ldm = words = 0
+    if mask is not None:
+        ldm, words = _rows_of(mask, "mask", T)
+    if depth is not None:
+        _index(depth, "depth", T)
+    if out is None:
+        out, ldo = q.new_empty((T, Hq, 128)), Hq * 128
+    else:
+        to, ho, ldo = _heads(out, "out")
+        if (to, ho) != (T, Hq):
+            raise ValueError(f"out must be [{T}, {Hq}, 128]")
+    d = _same_device(q, *cache, block_table, lens, cu, mask, depth, out, workspace)
+    if T == 0 or B == 0:
+        return out
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return attn_tree(q, cache, block_table, lens, cu, max_len, mask, depth, window, sinks, scale, out, workspace)
+    if workspace is None:
+        size = attn_tree_workspace_bytes(B, T, max_len, Hq, args[-1], window, sinks)
+        workspace = q.new_empty(size, dtype=_U8) if size else None
+    else:
+        size = _workspace_bytes(workspace)
+    status = lib().sq_attn_tree(q.data_ptr(), ldq, cu.data_ptr(), lens.data_ptr(), B, T, _ptr(mask), ldm, words, _ptr(depth), window,
+                                sinks, *args, Hq, 128, *bits, max_len, 0.08838834764831845 if scale is None else scale,
+                                out.data_ptr(), ldo, _ptr(workspace), size, _stream(q))
+    if status:
+        _check(status, "sq_attn_tree")
+    return out
+
+
+def _pool_args(block_table, held, pool, count):
+    """B and the arguments of the calls on page tables from the table on."""
+    B = _index(held, "held")
+    ld, cols = _rows_of(block_table, "block_table", B)
+    _index(pool, "pool")
+    _index(count, "count", 1)
+    return B, (block_table.data_ptr(), ld, cols), (pool.data_ptr(), count.data_ptr(), pool.shape[0])
+
+
+def paged_release(block_table, page: int, first, end, held, pool, count) -> None:
+    """Pages whose positions all lie in first .. end - 1 (int32 [B] each) go back to the pool
+    (sq_paged_release).  In place: block_table int32 [B, blocks], held int32 [B] (blocks of each sequence
+    that have a page), pool int32 [pages] with its first count[0] entries free, count int32 [1]."""
+    B, table, store = _pool_args(block_table, held, pool, count)
+    _index(first, "first", B)
+    _index(end, "end", B)
+    d = _same_device(held, block_table, first, end, pool, count)
+    if B == 0:
+        return
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return paged_release(block_table, page, first, end, held, pool, count)
+    status = lib().sq_paged_release(first.data_ptr(), end.data_ptr(), held.data_ptr(), B, *table, page, *store, _stream(held))
+    if status:
+        _check(status, "sq_paged_release")
+
+
+def paged_grow(have, add, held, block_table, page: int, pool, count, rows: int, out=None):
+    """Pages, lengths and rows of a step's new tokens (sq_paged_grow): have int32 [B] tokens in the cache, add
+    int32 [B] new ones, `rows` at least their sum.  In place: block_table, held, count as in
+    paged_release.  Returns (lens int32 [B], cu int32 [B + 1], pos int32 [rows], slots int64 [rows],
+    missing int32 [2]); out: those five tensors.  missing is (pages, rows) that lack; where it is not
+    (0, 0), nothing was handed out and the step has no rows."""
+    B, table, store = _pool_args(block_table, held, pool, count)
+    _index(have, "have", B)
+    _index(add, "add", B)
+    if out is None:
+        lens, cu, pos, missing = (have.new_empty(n) for n in (B, B + 1, rows, 2))
+        slots = have.new_empty(rows, dtype=torch.int64)
+    else:
+        lens, cu, pos, slots, missing = out
+        for t, n, size in ((lens, "lens", B), (cu, "cu", B + 1), (pos, "pos", rows), (missing, "missing", 2)):
+            _index(t, n, size)
+        _need(slots, torch.int64, "slots")
+        if slots.dim() != 1 or not slots.is_contiguous() or slots.shape[0] != rows:
+            raise ValueError(f"slots must be a contiguous vector of {rows} entries")
+    d = _same_device(held, block_table, have, add, pool, count, lens, cu, pos, slots, missing)
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return paged_grow(have, add, held, block_table, page, pool, count, rows, (lens, cu, pos, slots, missing))
+    if B == 0:  # no sequence has a row
+        cu.zero_(), pos.fill_(-1), slots.fill_(-1), missing.zero_()
+        return lens, cu, pos, slots, missing
+    status = lib().sq_paged_grow(have.data_ptr(), add.data_ptr(), held.data_ptr(), B, rows, *table, page, *store, lens.data_ptr(),
+                                 cu.data_ptr(), pos.data_ptr(), slots.data_ptr(), missing.data_ptr(), _stream(held))
+    if status:
+        _check(status, "sq_paged_grow")
+    return lens, cu, pos, slots, missing
+
+
+def kv_keep(cache, block_table, lens, cu, path, kept, out=None):
+    """The accepted drafts' slots become the sequence's next tokens (sq_kv_keep): path int32 [B, most], kept
+    int32 [B]: draft path[b, i] moves to the place of draft i, i < kept[b].  Returns the lengths then,
+    int32 [B]; out: a tensor for them (not lens)."""
+    B = _index(lens, "lens")
+    _index(cu, "cu", B + 1)
+    _index(kept, "kept", B)
+    ldp, most = _rows_of(path, "path", B)
+    args, bits = _cache_args(cache, block_table, B)
+    if out is None:
+        out = torch.empty_like(lens)
+    else:
+        _index(out, "out", B)
+    d = _same_device(lens, cu, kept, path, *cache, block_table, out)
+    if B == 0:
+        return out
+    if d != _current_device():
+        with torch.cuda.device(d):
+            return kv_keep(cache, block_table, lens, cu, path, kept, out)
+    status = lib().sq_kv_keep(cu.data_ptr(), lens.data_ptr(), B, path.data_ptr(), ldp, most, kept.data_ptr(), *args, 128, *bits,
+                              out.data_ptr(), _stream(lens))
+    if status:
+        _check(status, "sq_kv_keep")
     return out
