@@ -15,9 +15,20 @@ namespace {
 
 constexpr int kWaves = kPagedWaves;
 
-template <int BITS>
+// LDS of a wave: value codes of a block, a token's 16 bytes apart from the next one's (so that a read's place is one
+// register and a constant; paged_attn.hip's exchanged units would take one for each); its coefficients as in
+// paged_attn.hip, and two rows more (1 / va and vb / va of tokens where one is not finite); three numbers of each row.
+template <int BITS, int RB>
+struct TreeLds {
+  static constexpr int ROW = BITS * 16;  // bytes of a token's value codes
+  static constexpr int PITCH = ROW + 16;
+  static constexpr int CODES = kBlock * PITCH;
+  static constexpr int SIGHT = CODES + 7 * kBlock * 4, QUERIES = SIGHT + 3 * 16 * RB * 4;
+  static constexpr int BYTES = QUERIES + (RB > 1 ? RB * 4096 : 0);
+};
+template <int BITS, int RB>
 constexpr int tree_lds() {
-  const int merge = kWaves * 16 * (kDimRow + 2) * 4, codes = kWaves * WaveLds<BITS>::BYTES;
+  const int merge = kWaves * 16 * (kDimRow + 2) * 4, codes = kWaves * TreeLds<BITS, RB>::BYTES;
   return merge > codes ? merge : codes;
 }
 
@@ -60,11 +71,11 @@ __device__ __forceinline__ TreeTile find_tree_tile(const int32_t* cu, const int3
 __device__ __forceinline__ uint32_t below(int end, int t) { return (1u << min(max(end - t, 0), 16)) - 1u; }
 
 template <int BITS, bool P16, int RB>
-__global__ void __launch_bounds__(64 * kWaves, RB == 1 ? (BITS == 4 ? 3 : 2) : RB == 2 ? 2 : 1)
+__global__ void __launch_bounds__(64 * kWaves, 2)
 attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32_t magic_tiles, uint32_t magic_heads,
                uint32_t magic_group, TreeArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  using W = WaveLds<BITS>;
+  using W = TreeLds<BITS, RB>;
   constexpr int ROWS = 16 * RB;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -95,13 +106,15 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
   const int last = min(run.tokens, first + a.plan.chunk_tokens);  // places of the run
   const int32_t* const table = a.cache.table + tt.seq * a.cache.ldt;
 
+  uint8_t* const vlds = lds + w * W::BYTES;
+  float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
+  int* const sight = reinterpret_cast<int*>(vlds + W::SIGHT);
+  v8h* const qlds = reinterpret_cast<v8h*>(vlds + W::QUERIES);
   // The lane's rows: r0 + 16 rb + i (past the last: that one again, not stored), dims 32 g .. 32 g + 31 of the
   // queries in the codes' pair order, and their sums over all dims; what they see: t < hi where t >= lo or
-  // t < sinks, and the bits of mask row `bits`.
+  // t < sinks, and the bits of their rows of the mask: [hi, lo, row][16] of each column in LDS.
   v8h qf[RB][4];
   float qsum[RB];
-  int lo[RB], hi[RB];
-  const int32_t* bits[RB];
   int lo_most = 0, hi_least = len;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -114,11 +127,14 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     for (int x = 0; x < 4; ++x) raw[x] = qv[x];
     int at = static_cast<int>(tok);
     if (a.mask && a.depth && a.window > 0) at = min(max(a.depth[t], 0), 1 << 30);
-    hi[rb] = min(a.mask ? base : base + static_cast<int>(tok) + 1, len);
-    lo[rb] = a.window > 0 ? max(base + at - a.window + 1, 0) : 0;
-    bits[rb] = a.mask ? a.mask + t * a.ldm : nullptr;
-    hi_least = min(hi_least, hi[rb]);
-    lo_most = max(lo_most, lo[rb]);
+    const int hi = min(a.mask ? base : base + static_cast<int>(tok) + 1, len), lo = a.window > 0 ? max(base + at - a.window + 1, 0) : 0;
+    hi_least = min(hi_least, hi);
+    lo_most = max(lo_most, lo);
+    if (g == 0) {  // (for the few blocks that need them, and out of the registers)
+      sight[(3 * rb + 0) * 16 + i] = hi;
+      sight[(3 * rb + 1) * 16 + i] = lo;
+      sight[(3 * rb + 2) * 16 + i] = static_cast<int>(t);  // (rows below 2^24)
+    }
     float sum = 0.0f;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
@@ -141,12 +157,16 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
                             __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x05040100u), __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x07060302u));
     }
   }
+  if constexpr (RB > 1) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) qlds[(4 * rb + x) * 64 + lane] = qf[rb][x];
+  }
   // of the whole tile (lo and hi are not negative there but for hi of a base below 0, which counts as 0)
   lo_most = static_cast<int>(wave_all(static_cast<uint32_t>(lo_most), [](uint32_t u, uint32_t v) { return max(u, v); }));
   hi_least = static_cast<int>(wave_all(static_cast<uint32_t>(max(hi_least, 0)), [](uint32_t u, uint32_t v) { return min(u, v); }));
 
-  uint8_t* const vlds = lds + w * W::BYTES;
-  float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
   constexpr int KW = BITS == 4 ? 1 : 2;
   const float cs = a.scale_log2e, cs24 = a.scale_log2e * 16777216.0f;
 
@@ -158,24 +178,28 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     const int32_t col = table_column(a.cache, run.position(v0) + 16 * g);
     return col < 0 ? -1 : table[col];
   };
-  auto load = [&](int v0, int32_t entry) __attribute__((always_inline)) {
-    const int t0 = run.position(v0);
-    const int32_t mine = valid_page(a.cache, entry);
-    par_ok = mine >= 0 && v0 + lane < last;
-    const int32_t safe = max(mine, 0);
+  auto load_keys = [&](int v0, int32_t entry) __attribute__((always_inline)) {
+    const int t0 = run.position(v0), n = i >> 2;
+    const int32_t safe = max(valid_page(a.cache, entry), 0);
     int32_t pg[4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) pg[n] = __builtin_amdgcn_readlane(safe, 16 * n);
-    const int n = i >> 2;
+    for (int x = 0; x < 4; ++x) pg[x] = __builtin_amdgcn_readlane(safe, 16 * x);
     const int32_t pk = n == 0 ? pg[0] : n == 1 ? pg[1] : n == 2 ? pg[2] : pg[3];
     const uint8_t* kp = a.cache.kq + token_slot(a.cache, pk, hk, t0 + 16 * n + (i & 3)) * W::ROW + (BITS == 4 ? 16 : 32) * g;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int x = 0; x < KW; ++x) kc[j][x] = *reinterpret_cast<const v4u*>(kp + 4 * j * W::ROW + 16 * x);
+  };
+  // values, and the parameters of the lane's token t0 + lane; tokens without a page, or past the chunk, read page 0
+  auto load_values = [&](int v0, int32_t entry) __attribute__((always_inline)) {
+    const int t0 = run.position(v0);
+    const int32_t mine = valid_page(a.cache, entry), safe = max(mine, 0);
+    par_ok = mine >= 0 && v0 + lane < last;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      const uint8_t* vp = a.cache.vq + token_slot(a.cache, pg[m], hk, t0 + 16 * m) * W::ROW + 16 * lane;
+      const int32_t pg = __builtin_amdgcn_readlane(safe, 16 * m);
+      const uint8_t* vp = a.cache.vq + token_slot(a.cache, pg, hk, t0 + 16 * m) * W::ROW + 16 * lane;
 #pragma unroll
       for (int x = 0; x < KW; ++x) vc[m][x] = *reinterpret_cast<const v4u*>(vp + 1024 * x);
     }
@@ -190,10 +214,12 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
   };
   // The lane's tokens t .. t + 15 that its row of column rb sees.
   auto visible = [&](int rb, int t) -> uint32_t {
-    uint32_t vis = below(hi[rb], t) & (~below(lo[rb], t) | below(a.sinks, t));
+    const int hi = sight[(3 * rb + 0) * 16 + i], lo = sight[(3 * rb + 1) * 16 + i];
+    uint32_t vis = below(hi, t) & (~below(lo, t) | below(a.sinks, t));
     if (a.mask && t + 15 >= base) {
       const int j = t - base, word = j >> 5;  // (rounded down: -1 for the words before the first)
-      const auto at = [&](int x) { return x >= 0 && x < a.words ? static_cast<uint32_t>(bits[rb][x]) : 0u; };
+      const int32_t* const bits = a.mask + sight[(3 * rb + 2) * 16 + i] * a.ldm;
+      const auto at = [&](int x) { return x >= 0 && x < a.words ? static_cast<uint32_t>(bits[x]) : 0u; };
       const uint64_t two = at(word) | static_cast<uint64_t>(at(word + 1)) << 32;
       vis |= static_cast<uint32_t>(two >> (j & 31)) & below(min(base + tt.n, len), t);
     }
@@ -215,7 +241,9 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
   int v0 = first + w * kBlock;
   int32_t entry = -1;
   if (v0 < last) {
-    load(v0, entry_of(v0));
+    entry = entry_of(v0);
+    load_values(v0, entry);
+    load_keys(v0, entry);
     entry = entry_of(v0 + step);
   }
   for (; v0 < last; v0 += step) {
@@ -225,39 +253,35 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
 #pragma unroll
       for (int x = 0; x < KW; ++x) {
         const int row = 16 * mm + (BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3));
-        const int unit = BITS == 4 ? (lane & 3) ^ ((row >> 2) & 3) : (lane & 7) ^ (row & 7);
-        *reinterpret_cast<v4u*>(vlds + row * W::ROW + 16 * unit) = vc[mm][x];
+        *reinterpret_cast<v4u*>(vlds + row * W::PITCH + 16 * (lane & (BITS == 4 ? 3 : 7))) = vc[mm][x];
       }
     const uint64_t there = __ballot(par_ok);
     par.z = par.z == 0.0f ? 1.0f : par.z;  // a slot of a zeroed cache that was never written
-    const float rva = par_ok ? __fdiv_rn(1.0f, par.z) : 0.0f;
+    float rva = par_ok ? __fdiv_rn(1.0f, par.z) : 0.0f, rvb = par_ok ? par.w * rva : 0.0f;
+    const bool masked = t0 + kBlock > hi_least || (t0 < lo_most && t0 + kBlock > a.sinks);
+    uint64_t odd = 0;
+    if (masked) {  // (a weight of 0 does not hide parameters that are not finite)
+      odd = __ballot(!(fabsf(rva) < INFINITY) || !(fabsf(rvb) < INFINITY));
+      if (__builtin_expect(odd != 0, 0)) {
+        coef[5 * kBlock + lane] = rva;
+        coef[6 * kBlock + lane] = rvb;
+        if ((odd >> lane) & 1) rva = rvb = 0.0f;
+      }
+    }
     coef[0 * kBlock + lane] = par_ok ? par.x * cs24 : 0.0f;
     coef[1 * kBlock + lane] = par_ok ? par.y * cs : 0.0f;
     coef[2 * kBlock + lane] = par_ok ? __builtin_amdgcn_logf(par.z) : -INFINITY;
     coef[3 * kBlock + lane] = rva;
-    coef[4 * kBlock + lane] = par_ok ? par.w * rva : 0.0f;
-    v4u kn[4][KW];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int x = 0; x < KW; ++x) kn[j][x] = kc[j][x];
-    if (v0 + step < last) {
-      load(v0 + step, entry);
-      entry = entry_of(v0 + 2 * step);
-    }
+    coef[4 * kBlock + lane] = rvb;
+    const bool more = v0 + step < last;
     asm volatile("" ::: "memory");
 
-    const uint32_t here = static_cast<uint32_t>(there >> (16 * g)) & 0xFFFFu;  // of the lane's tokens
-    const bool masked = t0 + kBlock > hi_least || (t0 < lo_most && t0 + kBlock > a.sinks);
-    uint32_t vis[RB];
+    if constexpr (RB > 1) {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) vis[rb] = 0xFFFFu;
-    if (masked)
+      for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) vis[rb] = visible(rb, t0 + 16 * g);
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) seen |= static_cast<uint32_t>((vis[rb] & here) != 0) << rb;
-
+        for (int x = 0; x < 4; ++x) qf[rb][x] = qlds[(4 * rb + x) * 64 + lane];
+    }
     float s[RB][16];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -271,53 +295,89 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
       if constexpr (BITS == 4) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t u = kn[j][0][2 * e], v = kn[j][0][2 * e + 1], u8 = u >> 8, v8 = v >> 8;
-          ko[2 * e] = operand(u & 0x000F000Fu, u8 & 0x000F000Fu, v & 0x000F000Fu, v8 & 0x000F000Fu);
-          ko[2 * e + 1] = operand(u & 0x00F000F0u, u8 & 0x00F000F0u, v & 0x00F000F0u, v8 & 0x00F000F0u);
+          const uint32_t u = kc[j][0][2 * e], v = kc[j][0][2 * e + 1];
+          ko[2 * e] = operand(u & 0x000F000Fu, (u >> 8) & 0x000F000Fu, v & 0x000F000Fu, (v >> 8) & 0x000F000Fu);
+          ko[2 * e + 1] = operand((u >> 4) & 0x000F000Fu, (u >> 12) & 0x000F000Fu, (v >> 4) & 0x000F000Fu, (v >> 12) & 0x000F000Fu);
         }
       } else {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const uint32_t u = kn[j][x / 2][2 * (x & 1)], v = kn[j][x / 2][2 * (x & 1) + 1];
+          const uint32_t u = kc[j][x / 2][2 * (x & 1)], v = kc[j][x / 2][2 * (x & 1) + 1];
           ko[x] = operand(u & 0x00FF00FFu, (u >> 8) & 0x00FF00FFu, v & 0x00FF00FFu, (v >> 8) & 0x00FF00FFu);
         }
       }
+      v4f dot[RB];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) dot[rb] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) dot[rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ko[x], qf[rb][x], dot[rb], 0, 0, 0);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[rb][4 * j + r] = __fmaf_rn(fa[r], dot[rb][r], __fmaf_rn(fb[r], qsum[rb], fl[r]));
+      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) {
+      load_keys(v0 + step, entry);
+      load_values(v0 + step, entry);
+      entry = entry_of(v0 + 2 * step);
+    }
+    const uint32_t here = static_cast<uint32_t>(there >> (16 * g)) & 0xFFFFu;  // of the lane's tokens
+    if (__builtin_expect(masked, 0)) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        v4f se = {0.0f, 0.0f, 0.0f, 0.0f}, so = {0.0f, 0.0f, 0.0f, 0.0f};
+        const uint32_t vis = visible(rb, t0 + 16 * g);
+        seen |= static_cast<uint32_t>((vis & here) != 0) << rb;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          se = __builtin_amdgcn_mfma_f32_16x16x32_f16(ko[2 * e], qf[rb][2 * e], se, 0, 0, 0);
-          so = __builtin_amdgcn_mfma_f32_16x16x32_f16(ko[2 * e + 1], qf[rb][2 * e + 1], so, 0, 0, 0);
+        for (int x = 0; x < 16; ++x) {  // bitwise: a compare each would take the scalar registers' room
+          const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(vis << (31 - x)) >> 31);
+          s[rb][x] = __uint_as_float((__float_as_uint(s[rb][x]) & keep) | (~keep & 0xFF800000u));  // -inf
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float dot = BITS == 4 ? __fmaf_rn(so[r], 0.0625f, se[r]) : __fadd_rn(se[r], so[r]);
-          s[rb][4 * j + r] = __fmaf_rn(fa[r], dot, __fmaf_rn(fb[r], qsum[rb], fl[r]));
+        // what a row sees of such parameters, whatever its weight
+        if (__builtin_expect(odd != 0, 0)) {
+          for (uint32_t left = vis & static_cast<uint32_t>(odd >> (16 * g)) & 0xFFFFu; left; left &= left - 1) {
+            const int x = 16 * g + __builtin_ctz(left);
+            const float r = coef[5 * kBlock + x], v = coef[6 * kBlock + x];
+            if (!(fabsf(r) < INFINITY)) l[rb] += r;
+            if (!(fabsf(v) < INFINITY)) bsum[rb] += v;
+          }
         }
       }
+    } else if (here) {
+      seen |= (1u << RB) - 1u;
     }
-    v8h pf[RB][2];
-    const auto weights = [&](int rb, auto mc) __attribute__((always_inline)) {
-      constexpr bool MASK = decltype(mc)::value;
-      const auto sees = [&](int x) { return (vis[rb] >> x) & 1u; };
-      if constexpr (MASK)
+
+    // the columns' maxima; m moves, and what it scales, where one would grow too far (m = -inf: with any token)
+    float top[RB];
+    uint64_t moves = 0;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) s[rb][x] = sees(x) ? s[rb][x] : -INFINITY;
-      float top = s[rb][0];
+    for (int rb = 0; rb < RB; ++rb) {
+      top[rb] = s[rb][0];
 #pragma unroll
-      for (int x = 1; x < 16; ++x) top = fmaxf(top, s[rb][x]);
-      top = rows_all(top, [](float u, float v) { return fmaxf(u, v); });
-      if (__ballot(top - m[rb] > kWeightBits + kSlack)) {  // (m = -inf: any token)
-        const float mn = fmaxf(m[rb], fabsf(top) < kLargeScore ? top - kWeightBits : top);
-        const float f = rescale(m[rb], mn);
+      for (int x = 1; x < 16; ++x) top[rb] = fmaxf(top[rb], s[rb][x]);
+      top[rb] = rows_all(top[rb], [](float u, float v) { return fmaxf(u, v); });
+      moves |= __ballot(top[rb] - m[rb] > kWeightBits + kSlack);
+    }
+    if (__builtin_expect(moves != 0, 0)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const bool mine = top[rb] - m[rb] > kWeightBits + kSlack;
+        const float mn = mine ? fmaxf(m[rb], fabsf(top[rb]) < kLargeScore ? top[rb] - kWeightBits : top[rb]) : m[rb];
+        const float f = mine ? rescale(m[rb], mn) : 1.0f;
         l[rb] *= f;
         bsum[rb] *= f;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) acc[rb][dt] *= f;
         m[rb] = mn;
       }
-      // weights rounded to fp16 in the value codes' pair order; l and b sum the rounded ones
+    }
+
+    v8h pf[RB][2];
+    // weights of column rb rounded to fp16 in the value codes' pair order; l and b sum the rounded ones
+    const auto weights = [&](int rb) __attribute__((always_inline)) {
       const float from = m[rb] == -INFINITY ? 0.0f : m[rb];
       uint32_t pw[8];
 #pragma unroll
@@ -334,47 +394,51 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
           const uint32_t p2 = f2h2(exp2_fast(s[rb][8 * x + ta] - from), exp2_fast(s[rb][8 * x + tb] - from));
           pw[4 * x + y] = p2;
           const v2h ph = __builtin_bit_cast(v2h, p2);
-          // (a weight of 0 does not hide parameters that are not finite)
-          const auto seen_only = [&](float v, int x8) { return !MASK || sees(8 * x + x8) ? v : 0.0f; };
-          l[rb] = __fmaf_rn(static_cast<float>(ph[0]), seen_only(fr[ta], ta), l[rb]);
-          l[rb] = __fmaf_rn(static_cast<float>(ph[1]), seen_only(fr[tb], tb), l[rb]);
-          bsum[rb] = __fmaf_rn(static_cast<float>(ph[0]), seen_only(fv[ta], ta), bsum[rb]);
-          bsum[rb] = __fmaf_rn(static_cast<float>(ph[1]), seen_only(fv[tb], tb), bsum[rb]);
+          l[rb] = __fmaf_rn(static_cast<float>(ph[0]), fr[ta], l[rb]);
+          l[rb] = __fmaf_rn(static_cast<float>(ph[1]), fr[tb], l[rb]);
+          bsum[rb] = __fmaf_rn(static_cast<float>(ph[0]), fv[ta], bsum[rb]);
+          bsum[rb] = __fmaf_rn(static_cast<float>(ph[1]), fv[tb], bsum[rb]);
         }
       }
       pf[rb][0] = operand(pw[0], pw[1], pw[2], pw[3]);
       pf[rb][1] = operand(pw[4], pw[5], pw[6], pw[7]);
     };
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      if (masked)
-        weights(rb, std::true_type{});
-      else
-        weights(rb, std::false_type{});
-    }
     typedef __attribute__((address_space(3))) v2i* lds_v2i;
+    const auto value = [&](int dt, v8h (&vo)[2]) __attribute__((always_inline)) {
+      if constexpr (BITS == 4) {
+        const int row = 16 * g + i;
+        const uint8_t* p = vlds + row * W::PITCH + 8 * dt;
+        const v2i c2 = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i)(uintptr_t)(p));
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        v8h vo;
-        if constexpr (BITS == 4) {
-          const int row = 16 * g + i;
-          const uint8_t* p = vlds + row * W::ROW + 16 * ((dt >> 1) ^ ((row >> 2) & 3)) + 8 * (dt & 1);
-          const v2i c2 = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i)(uintptr_t)(p));
+        for (int x = 0; x < 2; ++x) {
           const uint32_t u = static_cast<uint32_t>(c2[x]), u8 = u >> 8;
-          vo = operand(normal(u & 0x000F000Fu, 0), normal(u & 0x00F000F0u, 4), normal(u8 & 0x000F000Fu, 0), normal(u8 & 0x00F000F0u, 4));
-        } else {
+          vo[x] = operand(normal(u & 0x000F000Fu, 0), normal(u & 0x00F000F0u, 4), normal(u8 & 0x000F000Fu, 0), normal(u8 & 0x00F000F0u, 4));
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
           const int row = 16 * g + 8 * x + (i >> 1);
-          const uint8_t* p = vlds + row * W::ROW + 16 * (dt ^ (row & 7)) + 8 * (i & 1);
+          const uint8_t* p = vlds + row * W::PITCH + 16 * dt + 8 * (i & 1);
           const v2i c2 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(p));
           const uint32_t u = static_cast<uint32_t>(c2[0]), v = static_cast<uint32_t>(c2[1]);
-          vo = operand(normal(u & 0x00FF00FFu, 0), normal((u >> 8) & 0x00FF00FFu, 0), normal(v & 0x00FF00FFu, 0),
-                       normal((v >> 8) & 0x00FF00FFu, 0));
+          vo[x] = operand(normal(u & 0x00FF00FFu, 0), normal((u >> 8) & 0x00FF00FFu, 0), normal(v & 0x00FF00FFu, 0),
+                          normal((v >> 8) & 0x00FF00FFu, 0));
         }
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vo, pf[rb][x], acc[rb][dt], 0, 0, 0);
       }
+    };
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      weights(rb);
+      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      v8h vo[2];
+      value(dt, vo);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vo[x], pf[rb][x], acc[rb][dt], 0, 0, 0);
     }
     asm volatile("" ::: "memory");
   }
@@ -524,7 +588,7 @@ attn_tree_combine(const float* part, const int32_t* cu, const int32_t* lens, int
 template <int BITS, bool P16, int RB>
 hipError_t launch_part(const TreeArgs& a, hipStream_t stream) {
   constexpr auto kern = attn_tree_part<BITS, P16, RB>;
-  constexpr int lds = tree_lds<BITS>();
+  constexpr int lds = tree_lds<BITS, RB>();
   const hipError_t init = set_max_lds<kern>(lds);
   if (init != hipSuccess) return init;
   const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.plan.tiles) * a.cache.heads * a.plan.chunks);
@@ -541,9 +605,7 @@ hipError_t launch_parts(const TreeArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attn_tree(const TreeArgs& a, hipStream_t stream) {
-  const hipError_t e = a.plan.rb == 1   ? launch_parts<1>(a, stream)
-                       : a.plan.rb == 2 ? launch_parts<2>(a, stream)
-                                        : launch_parts<4>(a, stream);
+  const hipError_t e = a.plan.rb == 2 ? launch_parts<2>(a, stream) : launch_parts<1>(a, stream);
   if (e != hipSuccess || a.plan.chunks == 1) return e;
   const auto join = [&](auto kern, int waves) {
     return launch(kern, dim3(static_cast<unsigned>(a.T * a.hq)), dim3(64 * waves), 0, stream, a.part, a.cu, a.lens, a.B, a.out, a.ldo,
