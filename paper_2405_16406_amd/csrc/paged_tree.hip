@@ -15,23 +15,6 @@ namespace {
 
 constexpr int kWaves = kPagedWaves;
 
-// LDS of a wave: value codes of a block, a token's 16 bytes apart from the next one's (so that a read's place is one
-// register and a constant; paged_attn.hip's exchanged units would take one for each); its coefficients as in
-// paged_attn.hip, and two rows more (1 / va and vb / va of tokens where one is not finite); three numbers of each row.
-template <int BITS, int RB>
-struct TreeLds {
-  static constexpr int ROW = BITS * 16;  // bytes of a token's value codes
-  static constexpr int PITCH = ROW + 16;
-  static constexpr int CODES = kBlock * PITCH;
-  static constexpr int SIGHT = CODES + 7 * kBlock * 4, QUERIES = SIGHT + 3 * 16 * RB * 4;
-  static constexpr int BYTES = QUERIES + (RB > 1 ? RB * 4096 : 0);
-};
-template <int BITS, int RB>
-constexpr int tree_lds() {
-  const int merge = kWaves * 16 * (kDimRow + 2) * 4, codes = kWaves * TreeLds<BITS, RB>::BYTES;
-  return merge > codes ? merge : codes;
-}
-
 // Sequence and tile of rows of the tile number `rem` among ceil(n * group / ROWS) a sequence; seq -1: past the last.
 struct TreeTile {
   int seq, tile;
@@ -67,290 +50,329 @@ __device__ __forceinline__ TreeTile find_tree_tile(const int32_t* cu, const int3
   return {-1, 0, 0, 0, 0};
 }
 
-// Bits x of the 16 tokens t .. t + 15 with t + x < end.
-__device__ __forceinline__ uint32_t below(int end, int t) { return (1u << min(max(end - t, 0), 16)) - 1u; }
+// Bits x of a block's tokens t .. t + 63 with t + x < end.
+__device__ __forceinline__ uint64_t below(int end, int t) {
+  const int n = min(max(end - t, 0), kBlock);
+  return n == kBlock ? ~uint64_t{0} : (uint64_t{1} << n) - 1;
+}
+// Of a block's 64 bits those of a lane's 16 tokens 16 j + 4 g + r, in the order of its scores, 4 j + r.
+__device__ __forceinline__ uint32_t lane_bits(uint64_t block) {
+  const uint64_t mine = block >> (4 * ((threadIdx.x & 63) >> 4));
+  const auto four = [&](int j) { return static_cast<uint32_t>(mine >> (16 * j)) & 0xFu; };
+  return four(0) | four(1) << 4 | four(2) << 8 | four(3) << 12;
+}
 
-template <int BITS, bool P16, int RB>
-__global__ void __launch_bounds__(64 * kWaves, 2)
-attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32_t magic_tiles, uint32_t magic_heads,
-               uint32_t magic_group, TreeArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  using W = TreeLds<BITS, RB>;
-  constexpr int ROWS = 16 * RB;
-  const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int i = lane & 15, g = lane >> 4;
-  // As in attn_paged_part: chunks from a tile's last one back slowest, then tile, then key/value head (so that
-  // the tiles which share keys follow each other on one of the chip's caches).
+// What a workgroup has to do: its tile of rows, and of the run of tokens that these see the places first .. last - 1.
+struct TreePlace {
+  int seq, q0, n;    // the sequence, its first row of the call and its rows
+  int base, len;     // tokens before the rows; tokens that count
+  int r0, rows;      // first row of the tile (16 RB .. of them), rows of the sequence
+  TokenRun run;
+  int first, last;
+  int c, own;        // the chunk, and how many the tile has
+  int hk;
+  const int32_t* table;
+};
+
+// false: nothing (the workgroup leaves together).  Workgroups in the order of dispatch as in attn_paged_part: the
+// chunks from a tile's last one back slowest, then tile, then key/value head (so that the tiles which share keys
+// follow each other on one of the chip's caches).
+template <int ROWS>
+__device__ __forceinline__ bool find_place(const int32_t* cu, const int32_t* lens, uint32_t magic_tiles, uint32_t magic_heads,
+                                           uint32_t magic_group, const TreeArgs& a, TreePlace& p) {
   uint32_t rest, hk, back, number;
   div_rem(blockIdx.x, a.cache.heads, magic_heads, rest, hk);
   div_rem(rest, a.plan.tiles, magic_tiles, back, number);
   back = a.plan.chunks - 1 - back;
   const TreeTile tt = find_tree_tile<ROWS>(cu, lens, a.B, a.T, a.group, static_cast<int>(number));
-  if (tt.seq < 0) return;  // the workgroup leaves together
-  const int all = min(max(tt.len, 0), (1 << 30) - 1), base = all - tt.n;  // (a position plus a depth stays below 2^31)
-  const int len = min(all, a.max_len);
-  const int rows = tt.n * a.group;
-  const int r0 = tt.tile * ROWS;
+  if (tt.seq < 0) return false;
+  const int all = min(max(tt.len, 0), (1 << 30) - 1);  // (a position plus a depth stays below 2^31)
+  p.seq = tt.seq;
+  p.q0 = tt.q0;
+  p.n = tt.n;
+  p.base = all - tt.n;
+  p.len = min(all, a.max_len);
+  p.rows = tt.n * a.group;
+  p.r0 = tt.tile * ROWS;
+  p.hk = static_cast<int>(hk);
   const auto token_of = [&](int r) {
     uint32_t t, h;
     div_rem(static_cast<uint32_t>(r), a.group, magic_group, t, h);
     return static_cast<int>(t);
   };
-  const int i0 = token_of(r0), i1 = token_of(min(r0 + ROWS, rows) - 1);  // first and last token of the tile
-  const TokenRun run = token_run(a.mask ? base : base + i0, a.mask ? len : min(base + i1 + 1, len), a.window, a.sinks);
-  const int own = max(1, (run.tokens + a.plan.chunk_tokens - 1) / a.plan.chunk_tokens);  // chunks of the tile
-  if (static_cast<int>(back) >= own) return;  // the workgroup leaves together
-  const int c = own - 1 - static_cast<int>(back);
-  const int first = c * a.plan.chunk_tokens;
-  const int last = min(run.tokens, first + a.plan.chunk_tokens);  // places of the run
-  const int32_t* const table = a.cache.table + tt.seq * a.cache.ldt;
+  const int i0 = token_of(p.r0), i1 = token_of(min(p.r0 + ROWS, p.rows) - 1);  // first and last token of the tile
+  p.run = token_run(a.mask ? p.base : p.base + i0, a.mask ? p.len : min(p.base + i1 + 1, p.len), a.window, a.sinks);
+  p.own = max(1, (p.run.tokens + a.plan.chunk_tokens - 1) / a.plan.chunk_tokens);
+  if (static_cast<int>(back) >= p.own) return false;
+  p.c = p.own - 1 - static_cast<int>(back);
+  p.first = p.c * a.plan.chunk_tokens;
+  p.last = min(p.run.tokens, p.first + a.plan.chunk_tokens);
+  p.table = a.cache.table + tt.seq * a.cache.ldt;
+  return true;
+}
 
-  uint8_t* const vlds = lds + w * W::BYTES;
-  float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
-  int* const sight = reinterpret_cast<int*>(vlds + W::SIGHT);
-  v8h* const qlds = reinterpret_cast<v8h*>(vlds + W::QUERIES);
-  // The lane's rows: r0 + 16 rb + i (past the last: that one again, not stored), dims 32 g .. 32 g + 31 of the
-  // queries in the codes' pair order, and their sums over all dims; what they see: t < hi where t >= lo or
-  // t < sinks, and the bits of their rows of the mask: [hi, lo, row][16] of each column in LDS.
-  v8h qf[RB][4];
-  float qsum[RB];
-  int lo_most = 0, hi_least = len;
+// The table's entry of the 16 tokens of a block (at place v0 of the run) that lane / 16 stands for.
+__device__ __forceinline__ int32_t entry_of(const TreeArgs& a, const TreePlace& p, int v0) {
+  if (v0 >= p.last) return -1;
+  const int32_t col = table_column(a.cache, p.run.position(v0) + 16 * ((threadIdx.x & 63) >> 4));
+  return col < 0 ? -1 : p.table[col];
+}
+
+// Parameters of the token in slot `slot` of the pool.
+template <bool P16>
+__device__ __forceinline__ float4 token_params(const PagedCache& c, int64_t slot) {
+  if constexpr (P16) {
+    const uint2 p = static_cast<const uint2*>(c.params)[slot];
+    return make_float4(h2f(static_cast<uint16_t>(p.x)), h2f(static_cast<uint16_t>(p.x >> 16)), h2f(static_cast<uint16_t>(p.y)),
+                       h2f(static_cast<uint16_t>(p.y >> 16)));
+  } else {
+    return static_cast<const float4*>(c.params)[slot];
+  }
+}
+
+// Coefficients of a block's 64 tokens, one a lane, in seven rows of 64: a, b, lv, 1 / va and vb / va with the score
+// s_t + log2 va_t = a_t (q . c_t) + b_t sum(q) + lv_t, as in paged_attn.hip.  A weight of 0 does not hide a
+// 1 / va or vb / va that is not finite: such tokens (the result) have zeros there, and what they are in the
+// last two rows.
+__device__ __forceinline__ uint64_t token_coefs(float4 par, bool there, float cs, float down, float* coef) {
+  const int lane = threadIdx.x & 63;
+  par.z = par.z == 0.0f ? 1.0f : par.z;  // a slot of a zeroed cache that was never written
+  float rva = there ? __fdiv_rn(1.0f, par.z) : 0.0f, rvb = there ? par.w * rva : 0.0f;
+  const bool bad = !(fabsf(rva) < INFINITY) || !(fabsf(rvb) < INFINITY);
+  const uint64_t odd = __ballot(bad);
+  if (__builtin_expect(odd != 0, 0)) {
+    coef[5 * kBlock + lane] = rva;
+    coef[6 * kBlock + lane] = rvb;
+    if (bad) rva = rvb = 0.0f;
+  }
+  coef[0 * kBlock + lane] = there ? par.x * (cs * 16777216.0f * down) : 0.0f;  // 2^24 undoes the codes' subnormal scale
+  coef[1 * kBlock + lane] = there ? par.y * cs : 0.0f;
+  coef[2 * kBlock + lane] = there ? __builtin_amdgcn_logf(par.z) : -INFINITY;
+  coef[3 * kBlock + lane] = rva;
+  coef[4 * kBlock + lane] = rvb;
+  return odd;
+}
+
+// A token's key codes of dims 32 g .. 32 g + 31 as the four operands of a lane (4 bits: odd dims in place, 16 n, for
+// queries that have 1 / 16 there).
+template <int BITS, int KW>
+__device__ __forceinline__ void key_operands(const v4u (&k)[KW], v8h (&ko)[4]) {
+  if constexpr (BITS == 4) {
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    uint32_t tok, gh;
-    div_rem(static_cast<uint32_t>(min(r0 + 16 * rb + i, rows - 1)), a.group, magic_group, tok, gh);
-    const int64_t t = tt.q0 + static_cast<int64_t>(tok);
-    const v4u* qv = reinterpret_cast<const v4u*>(q + t * a.ldq + (static_cast<int64_t>(hk) * a.group + gh) * 128 + 32 * g);
-    v4u raw[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) raw[x] = qv[x];
-    int at = static_cast<int>(tok);
-    if (a.mask && a.depth && a.window > 0) at = min(max(a.depth[t], 0), 1 << 30);
-    const int hi = min(a.mask ? base : base + static_cast<int>(tok) + 1, len), lo = a.window > 0 ? max(base + at - a.window + 1, 0) : 0;
-    hi_least = min(hi_least, hi);
-    lo_most = max(lo_most, lo);
-    if (g == 0) {  // (for the few blocks that need them, and out of the registers)
-      sight[(3 * rb + 0) * 16 + i] = hi;
-      sight[(3 * rb + 1) * 16 + i] = lo;
-      sight[(3 * rb + 2) * 16 + i] = static_cast<int>(t);  // (rows below 2^24)
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t u = k[0][2 * e], v = k[0][2 * e + 1];
+      ko[2 * e] = operand(u & 0x000F000Fu, (u >> 8) & 0x000F000Fu, v & 0x000F000Fu, (v >> 8) & 0x000F000Fu);
+      ko[2 * e + 1] = operand(u & 0x00F000F0u, (u >> 8) & 0x00F000F0u, v & 0x00F000F0u, (v >> 8) & 0x00F000F0u);
     }
-    float sum = 0.0f;
+  } else {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+    for (int x = 0; x < 4; ++x) {
+      const uint32_t u = k[x / 2][2 * (x & 1)], v = k[x / 2][2 * (x & 1) + 1];
+      ko[x] = operand(u & 0x00FF00FFu, (u >> 8) & 0x00FF00FFu, v & 0x00FF00FFu, (v >> 8) & 0x00FF00FFu);
+    }
+  }
+}
+
+// Value codes of a block in LDS, a token's 16 bytes apart from the next one's (so that a read's place is one register
+// and a constant; paged_attn.hip's exchanged units would take a register for each): dims 16 dt + i of the lane's 16
+// tokens as two operands.
+template <int BITS>
+constexpr int kPitch = BITS * 16 + 16;
+template <int BITS>
+__device__ __forceinline__ void value_operands(const uint8_t* codes, int dt, v8h (&vo)[2]) {
+  typedef __attribute__((address_space(3))) v2i* lds_v2i;
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  if constexpr (BITS == 4) {
+    const int row = 16 * (i >> 2) + 4 * g + (i & 3);  // the lane's i-th token
+    const v2i c2 = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i)(uintptr_t)(codes + row * kPitch<BITS> + 8 * dt));
 #pragma unroll
-      for (int y = 0; y < 4; ++y) sum += h2f(static_cast<uint16_t>(raw[x][y])) + h2f(static_cast<uint16_t>(raw[x][y] >> 16));
-    qsum[rb] = rows_all(sum, [](float u, float v) { return __fadd_rn(u, v); });
-    if constexpr (BITS == 4) {
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t u = static_cast<uint32_t>(c2[x]), u8 = u >> 8;
+      vo[x] = operand(normal(u & 0x000F000Fu, 0), normal(u & 0x00F000F0u, 4), normal(u8 & 0x000F000Fu, 0), normal(u8 & 0x00F000F0u, 4));
+    }
+  } else {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const v4u u = raw[2 * e], v = raw[2 * e + 1];
-        qf[rb][2 * e] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x05040100u), __builtin_amdgcn_perm(u[3], u[1], 0x05040100u),
-                                __builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x05040100u));
-        qf[rb][2 * e + 1] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[1], 0x07060302u),
-                                    __builtin_amdgcn_perm(v[2], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u));
+    for (int x = 0; x < 2; ++x) {
+      const int n = 8 * x + (i >> 1), row = 16 * (n >> 2) + 4 * g + (n & 3);  // its n-th
+      const v2i c2 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(codes + row * kPitch<BITS> + 16 * dt + 8 * (i & 1)));
+      const uint32_t u = static_cast<uint32_t>(c2[0]), v = static_cast<uint32_t>(c2[1]);
+      vo[x] = operand(normal(u & 0x00FF00FFu, 0), normal((u >> 8) & 0x00FF00FFu, 0), normal(v & 0x00FF00FFu, 0),
+                      normal((v >> 8) & 0x00FF00FFu, 0));
+    }
+  }
+}
+
+// 16 RB rows of a wave, one a lane and column: queries, what they see, and their softmax states.
+template <int BITS, int RB>
+struct TreeRows {
+  v8h qf[RB][4];    // dims 32 g .. 32 g + 31 in the codes' pair order, times 2^-down (4 bits: odd dims 1 / 16 of that)
+  float down;
+  float qsum[RB];   // sums over all dims
+  int lo_most, hi_least;  // every row sees t where lo_most <= t < hi_least (or t < sinks)
+  int* sight;       // in LDS, out of the registers: [hi, lo, row][16] of each column
+  float m[RB], l[RB], bsum[RB];
+  uint32_t seen;    // bit rb: the row sees a token with a page
+  v4f acc[RB][8];
+
+  static constexpr int SIGHT = 3 * 16 * RB;  // numbers in LDS
+
+  // Rows p.r0 + first + 16 rb + i; past the last: that one again, not stored.
+  __device__ __forceinline__ void init(const uint16_t* q, int first, uint32_t magic_group, const TreeArgs& a, const TreePlace& p, int* in_lds) {
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    sight = in_lds;
+    seen = 0;
+    lo_most = 0;
+    hi_least = p.len;
+    float largest = 0.0f;
+    v4u all[RB][4];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      m[rb] = -INFINITY;
+      l[rb] = bsum[rb] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) acc[rb][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      uint32_t tok, gh;
+      div_rem(static_cast<uint32_t>(min(p.r0 + first + 16 * rb + i, p.rows - 1)), a.group, magic_group, tok, gh);
+      const int64_t t = p.q0 + static_cast<int64_t>(tok);
+      const v4u* qv = reinterpret_cast<const v4u*>(q + t * a.ldq + (static_cast<int64_t>(p.hk) * a.group + gh) * 128 + 32 * g);
+      v4u raw[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) raw[x] = qv[x];
+      int at = static_cast<int>(tok);
+      if (a.mask && a.depth && a.window > 0) at = min(max(a.depth[t], 0), 1 << 30);
+      const int hi = min(a.mask ? p.base : p.base + static_cast<int>(tok) + 1, p.len);
+      const int lo = a.window > 0 ? max(p.base + at - a.window + 1, 0) : 0;
+      hi_least = min(hi_least, hi);
+      lo_most = max(lo_most, lo);
+      if (g == 0) {
+        sight[(3 * rb + 0) * 16 + i] = hi;
+        sight[(3 * rb + 1) * 16 + i] = lo;
+        sight[(3 * rb + 2) * 16 + i] = static_cast<int>(t);  // (rows below 2^24)
       }
-    } else {
+      float sum = 0.0f;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        qf[rb][x] = operand(__builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x05040100u), __builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x07060302u),
-                            __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x05040100u), __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x07060302u));
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float u = h2f(static_cast<uint16_t>(raw[x][y])), v = h2f(static_cast<uint16_t>(raw[x][y] >> 16));
+          sum += u + v;
+          largest = fmaxf(largest, fmaxf(fabsf(u), fabsf(v)));
+        }
+      qsum[rb] = rows_all(sum, [](float u, float v) { return __fadd_rn(u, v); });
+#pragma unroll
+      for (int x = 0; x < 4; ++x) all[rb][x] = raw[x];
     }
-  }
-  if constexpr (RB > 1) {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) qlds[(4 * rb + x) * 64 + lane] = qf[rb][x];
-  }
-  // of the whole tile (lo and hi are not negative there but for hi of a base below 0, which counts as 0)
-  lo_most = static_cast<int>(wave_all(static_cast<uint32_t>(lo_most), [](uint32_t u, uint32_t v) { return max(u, v); }));
-  hi_least = static_cast<int>(wave_all(static_cast<uint32_t>(max(hi_least, 0)), [](uint32_t u, uint32_t v) { return min(u, v); }));
-
-  constexpr int KW = BITS == 4 ? 1 : 2;
-  const float cs = a.scale_log2e, cs24 = a.scale_log2e * 16777216.0f;
-
-  v4u kc[4][KW], vc[4][KW];
-  float4 par;
-  bool par_ok;
-  auto entry_of = [&](int v0) -> int32_t {
-    if (v0 >= last) return -1;
-    const int32_t col = table_column(a.cache, run.position(v0) + 16 * g);
-    return col < 0 ? -1 : table[col];
-  };
-  auto load_keys = [&](int v0, int32_t entry) __attribute__((always_inline)) {
-    const int t0 = run.position(v0), n = i >> 2;
-    const int32_t safe = max(valid_page(a.cache, entry), 0);
-    int32_t pg[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) pg[x] = __builtin_amdgcn_readlane(safe, 16 * x);
-    const int32_t pk = n == 0 ? pg[0] : n == 1 ? pg[1] : n == 2 ? pg[2] : pg[3];
-    const uint8_t* kp = a.cache.kq + token_slot(a.cache, pk, hk, t0 + 16 * n + (i & 3)) * W::ROW + (BITS == 4 ? 16 : 32) * g;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int x = 0; x < KW; ++x) kc[j][x] = *reinterpret_cast<const v4u*>(kp + 4 * j * W::ROW + 16 * x);
-  };
-  // values, and the parameters of the lane's token t0 + lane; tokens without a page, or past the chunk, read page 0
-  auto load_values = [&](int v0, int32_t entry) __attribute__((always_inline)) {
-    const int t0 = run.position(v0);
-    const int32_t mine = valid_page(a.cache, entry), safe = max(mine, 0);
-    par_ok = mine >= 0 && v0 + lane < last;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int32_t pg = __builtin_amdgcn_readlane(safe, 16 * m);
-      const uint8_t* vp = a.cache.vq + token_slot(a.cache, pg, hk, t0 + 16 * m) * W::ROW + 16 * lane;
-#pragma unroll
-      for (int x = 0; x < KW; ++x) vc[m][x] = *reinterpret_cast<const v4u*>(vp + 1024 * x);
-    }
-    const int64_t pslot = token_slot(a.cache, safe, hk, t0 + lane);
-    if constexpr (P16) {
-      const uint2 p = static_cast<const uint2*>(a.cache.params)[pslot];
-      par = make_float4(h2f(static_cast<uint16_t>(p.x)), h2f(static_cast<uint16_t>(p.x >> 16)),
-                        h2f(static_cast<uint16_t>(p.y)), h2f(static_cast<uint16_t>(p.y >> 16)));
-    } else {
-      par = static_cast<const float4*>(a.cache.params)[pslot];
-    }
-  };
-  // The lane's tokens t .. t + 15 that its row of column rb sees.
-  auto visible = [&](int rb, int t) -> uint32_t {
-    const int hi = sight[(3 * rb + 0) * 16 + i], lo = sight[(3 * rb + 1) * 16 + i];
-    uint32_t vis = below(hi, t) & (~below(lo, t) | below(a.sinks, t));
-    if (a.mask && t + 15 >= base) {
-      const int j = t - base, word = j >> 5;  // (rounded down: -1 for the words before the first)
-      const int32_t* const bits = a.mask + sight[(3 * rb + 2) * 16 + i] * a.ldm;
-      const auto at = [&](int x) { return x >= 0 && x < a.words ? static_cast<uint32_t>(bits[x]) : 0u; };
-      const uint64_t two = at(word) | static_cast<uint64_t>(at(word + 1)) << 32;
-      vis |= static_cast<uint32_t>(two >> (j & 31)) & below(min(base + tt.n, len), t);
-    }
-    return vis & 0xFFFFu;
-  };
-
-  float m[RB], l[RB], bsum[RB];
-  uint32_t seen = 0;  // bit rb: the row sees a token with a page
-  v4f acc[RB][8];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    m[rb] = -INFINITY;
-    l[rb] = bsum[rb] = 0.0f;
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) acc[rb][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-
-  const int step = kWaves * kBlock;
-  int v0 = first + w * kBlock;
-  int32_t entry = -1;
-  if (v0 < last) {
-    entry = entry_of(v0);
-    load_values(v0, entry);
-    load_keys(v0, entry);
-    entry = entry_of(v0 + step);
-  }
-  for (; v0 < last; v0 += step) {
-    const int t0 = run.position(v0);
-#pragma unroll
-    for (int mm = 0; mm < 4; ++mm)
-#pragma unroll
-      for (int x = 0; x < KW; ++x) {
-        const int row = 16 * mm + (BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3));
-        *reinterpret_cast<v4u*>(vlds + row * W::PITCH + 16 * (lane & (BITS == 4 ? 3 : 7))) = vc[mm][x];
-      }
-    const uint64_t there = __ballot(par_ok);
-    par.z = par.z == 0.0f ? 1.0f : par.z;  // a slot of a zeroed cache that was never written
-    float rva = par_ok ? __fdiv_rn(1.0f, par.z) : 0.0f, rvb = par_ok ? par.w * rva : 0.0f;
-    const bool masked = t0 + kBlock > hi_least || (t0 < lo_most && t0 + kBlock > a.sinks);
-    uint64_t odd = 0;
-    if (masked) {  // (a weight of 0 does not hide parameters that are not finite)
-      odd = __ballot(!(fabsf(rva) < INFINITY) || !(fabsf(rvb) < INFINITY));
-      if (__builtin_expect(odd != 0, 0)) {
-        coef[5 * kBlock + lane] = rva;
-        coef[6 * kBlock + lane] = rvb;
-        if ((odd >> lane) & 1) rva = rvb = 0.0f;
+    // 4 bits: the odd dims' sixteenth would lose bits of small numbers, so the wave's queries are first brought up to where
+    // the largest lies in 2^13 .. 2^14 (by a power of two, exact but for what is 2^-27 of the largest)
+    down = 1.0f;
+    float up = 1.0f;
+    if constexpr (BITS == 4) {
+      largest = wave_max(largest);
+      if (largest > 0.0f && largest < INFINITY) {
+        const int e = 13 - (static_cast<int>(__float_as_uint(largest) >> 23) - 127);
+        up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+        down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
       }
     }
-    coef[0 * kBlock + lane] = par_ok ? par.x * cs24 : 0.0f;
-    coef[1 * kBlock + lane] = par_ok ? par.y * cs : 0.0f;
-    coef[2 * kBlock + lane] = par_ok ? __builtin_amdgcn_logf(par.z) : -INFINITY;
-    coef[3 * kBlock + lane] = rva;
-    coef[4 * kBlock + lane] = rvb;
-    const bool more = v0 + step < last;
-    asm volatile("" ::: "memory");
-
-    if constexpr (RB > 1) {
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+    for (int rb = 0; rb < RB; ++rb) {
+      v4u raw[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) qf[rb][x] = qlds[(4 * rb + x) * 64 + lane];
-    }
-    float s[RB][16];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 ca = *reinterpret_cast<const float4*>(coef + 0 * kBlock + 16 * g + 4 * j);
-      const float4 cb = *reinterpret_cast<const float4*>(coef + 1 * kBlock + 16 * g + 4 * j);
-      const float4 cl = *reinterpret_cast<const float4*>(coef + 2 * kBlock + 16 * g + 4 * j);
-      const float* fa = &ca.x;
-      const float* fb = &cb.x;
-      const float* fl = &cl.x;
-      v8h ko[4];
+      for (int x = 0; x < 4; ++x) raw[x] = all[rb][x];
       if constexpr (BITS == 4) {
+        // (even dims in the low halves)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            raw[x][y] = f2h2(h2f(static_cast<uint16_t>(raw[x][y])) * up, h2f(static_cast<uint16_t>(raw[x][y] >> 16)) * (0.0625f * up));
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t u = kc[j][0][2 * e], v = kc[j][0][2 * e + 1];
-          ko[2 * e] = operand(u & 0x000F000Fu, (u >> 8) & 0x000F000Fu, v & 0x000F000Fu, (v >> 8) & 0x000F000Fu);
-          ko[2 * e + 1] = operand((u >> 4) & 0x000F000Fu, (u >> 12) & 0x000F000Fu, (v >> 4) & 0x000F000Fu, (v >> 12) & 0x000F000Fu);
+          const v4u u = raw[2 * e], v = raw[2 * e + 1];
+          qf[rb][2 * e] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x05040100u), __builtin_amdgcn_perm(u[3], u[1], 0x05040100u),
+                                  __builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x05040100u));
+          qf[rb][2 * e + 1] = operand(__builtin_amdgcn_perm(u[2], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[1], 0x07060302u),
+                                      __builtin_amdgcn_perm(v[2], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u));
         }
       } else {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint32_t u = kc[j][x / 2][2 * (x & 1)], v = kc[j][x / 2][2 * (x & 1) + 1];
-          ko[x] = operand(u & 0x00FF00FFu, (u >> 8) & 0x00FF00FFu, v & 0x00FF00FFu, (v >> 8) & 0x00FF00FFu);
-        }
+        for (int x = 0; x < 4; ++x)
+          qf[rb][x] = operand(__builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x05040100u), __builtin_amdgcn_perm(raw[x][1], raw[x][0], 0x07060302u),
+                              __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x05040100u), __builtin_amdgcn_perm(raw[x][3], raw[x][2], 0x07060302u));
       }
-      v4f dot[RB];
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) dot[rb] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) dot[rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ko[x], qf[rb][x], dot[rb], 0, 0, 0);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[rb][4 * j + r] = __fmaf_rn(fa[r], dot[rb][r], __fmaf_rn(fb[r], qsum[rb], fl[r]));
-      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (more) {
-      load_keys(v0 + step, entry);
-      load_values(v0 + step, entry);
-      entry = entry_of(v0 + 2 * step);
+    // of all rows (lo and hi are not negative there but for hi of a base below 0, which counts as 0)
+    lo_most = static_cast<int>(wave_all(static_cast<uint32_t>(lo_most), [](uint32_t u, uint32_t v) { return max(u, v); }));
+    hi_least = static_cast<int>(wave_all(static_cast<uint32_t>(max(hi_least, 0)), [](uint32_t u, uint32_t v) { return min(u, v); }));
+  }
+
+  // Scores of the block's tokens 16 j + 4 g .. + 3 with their key operands.
+  __device__ __forceinline__ void scores(int j, const v8h (&ko)[4], const float* coef, float (&s)[RB][16]) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const float4 ca = *reinterpret_cast<const float4*>(coef + 0 * kBlock + 16 * j + 4 * g);
+    const float4 cb = *reinterpret_cast<const float4*>(coef + 1 * kBlock + 16 * j + 4 * g);
+    const float4 cl = *reinterpret_cast<const float4*>(coef + 2 * kBlock + 16 * j + 4 * g);
+    const float fa[4] = {ca.x, ca.y, ca.z, ca.w}, fb[4] = {cb.x, cb.y, cb.z, cb.w}, fl[4] = {cl.x, cl.y, cl.z, cl.w};
+    v4f dot[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) dot[rb] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) dot[rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ko[x], qf[rb][x], dot[rb], 0, 0, 0);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[rb][4 * j + r] = __fmaf_rn(fa[r], dot[rb][r], __fmaf_rn(fb[r], qsum[rb], fl[r]));
+  }
+
+  // Of the block's tokens t .. t + 63 those that the lane's row of column rb sees.
+  __device__ __forceinline__ uint64_t visible(int rb, int t, const TreeArgs& a, const TreePlace& p) const {
+    const int i = threadIdx.x & 15;
+    const int hi = sight[(3 * rb + 0) * 16 + i], lo = sight[(3 * rb + 1) * 16 + i];
+    uint64_t vis = below(hi, t) & (~below(lo, t) | below(a.sinks, t));
+    if (a.mask && t + kBlock > p.base) {
+      const int j = t - p.base, word = j >> 5, shift = j & 31;  // (rounded down: negative for the words before the first)
+      const int32_t* const bits = a.mask + sight[(3 * rb + 2) * 16 + i] * a.ldm;
+      const auto at = [&](int x) { return x >= 0 && x < a.words ? static_cast<uint64_t>(static_cast<uint32_t>(bits[x])) : uint64_t{0}; };
+      uint64_t sees = (at(word) | at(word + 1) << 32) >> shift;
+      if (shift) sees |= at(word + 2) << (64 - shift);
+      vis |= sees & below(min(p.base + p.n, p.len), t);
     }
-    const uint32_t here = static_cast<uint32_t>(there >> (16 * g)) & 0xFFFFu;  // of the lane's tokens
-    if (__builtin_expect(masked, 0)) {
+    return vis;
+  }
+
+  // Takes what a row does not see out of the scores of the block at token t0.  there, odd: bits of its tokens that have
+  // a page, and of those whose coefficients are not finite.
+  __device__ __forceinline__ void hide(int t0, uint64_t there, uint64_t odd, const float* coef, const TreeArgs& a, const TreePlace& p,
+                                       float (&s)[RB][16]) {
+    const uint32_t here = lane_bits(there);  // of the lane's tokens
+    const bool masked = t0 + kBlock > hi_least || (t0 < lo_most && t0 + kBlock > a.sinks);
+    if (__builtin_expect(masked || odd != 0, 0)) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const uint32_t vis = visible(rb, t0 + 16 * g);
+        const uint32_t vis = masked ? lane_bits(visible(rb, t0, a, p)) : 0xFFFFu;
         seen |= static_cast<uint32_t>((vis & here) != 0) << rb;
 #pragma unroll
         for (int x = 0; x < 16; ++x) {  // bitwise: a compare each would take the scalar registers' room
           const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(vis << (31 - x)) >> 31);
           s[rb][x] = __uint_as_float((__float_as_uint(s[rb][x]) & keep) | (~keep & 0xFF800000u));  // -inf
         }
-        // what a row sees of such parameters, whatever its weight
-        if (__builtin_expect(odd != 0, 0)) {
-          for (uint32_t left = vis & static_cast<uint32_t>(odd >> (16 * g)) & 0xFFFFu; left; left &= left - 1) {
-            const int x = 16 * g + __builtin_ctz(left);
-            const float r = coef[5 * kBlock + x], v = coef[6 * kBlock + x];
-            if (!(fabsf(r) < INFINITY)) l[rb] += r;
-            if (!(fabsf(v) < INFINITY)) bsum[rb] += v;
-          }
+        // what the row sees of parameters that are not finite, whatever its weight
+        for (uint32_t left = vis & lane_bits(odd); left; left &= left - 1) {
+          const int k = __builtin_ctz(left), x = 16 * (k >> 2) + 4 * ((threadIdx.x & 63) >> 4) + (k & 3);
+          const float r = coef[5 * kBlock + x], v = coef[6 * kBlock + x];
+          if (!(fabsf(r) < INFINITY)) l[rb] += r;
+          if (!(fabsf(v) < INFINITY)) bsum[rb] += v;
         }
       }
     } else if (here) {
       seen |= (1u << RB) - 1u;
     }
+  }
 
-    // the columns' maxima; m moves, and what it scales, where one would grow too far (m = -inf: with any token)
+  // Moves m, and what it scales, where the largest weight would grow too far (m = -inf: with any token).
+  __device__ __forceinline__ void move(const float (&s)[RB][16]) {
     float top[RB];
     uint64_t moves = 0;
 #pragma unroll
@@ -374,81 +396,48 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
         m[rb] = mn;
       }
     }
-
-    v8h pf[RB][2];
-    // weights of column rb rounded to fp16 in the value codes' pair order; l and b sum the rounded ones
-    const auto weights = [&](int rb) __attribute__((always_inline)) {
-      const float from = m[rb] == -INFINITY ? 0.0f : m[rb];
-      uint32_t pw[8];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float4 cr0 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 8 * x);
-        const float4 cr1 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 16 * g + 8 * x + 4);
-        const float4 cv0 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 8 * x);
-        const float4 cv1 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 16 * g + 8 * x + 4);
-        const float fr[8] = {cr0.x, cr0.y, cr0.z, cr0.w, cr1.x, cr1.y, cr1.z, cr1.w};
-        const float fv[8] = {cv0.x, cv0.y, cv0.z, cv0.w, cv1.x, cv1.y, cv1.z, cv1.w};
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const int ta = BITS == 4 ? y : 4 * (y >> 1) + (y & 1), tb = ta + (BITS == 4 ? 4 : 2);
-          const uint32_t p2 = f2h2(exp2_fast(s[rb][8 * x + ta] - from), exp2_fast(s[rb][8 * x + tb] - from));
-          pw[4 * x + y] = p2;
-          const v2h ph = __builtin_bit_cast(v2h, p2);
-          l[rb] = __fmaf_rn(static_cast<float>(ph[0]), fr[ta], l[rb]);
-          l[rb] = __fmaf_rn(static_cast<float>(ph[1]), fr[tb], l[rb]);
-          bsum[rb] = __fmaf_rn(static_cast<float>(ph[0]), fv[ta], bsum[rb]);
-          bsum[rb] = __fmaf_rn(static_cast<float>(ph[1]), fv[tb], bsum[rb]);
-        }
-      }
-      pf[rb][0] = operand(pw[0], pw[1], pw[2], pw[3]);
-      pf[rb][1] = operand(pw[4], pw[5], pw[6], pw[7]);
-    };
-    typedef __attribute__((address_space(3))) v2i* lds_v2i;
-    const auto value = [&](int dt, v8h (&vo)[2]) __attribute__((always_inline)) {
-      if constexpr (BITS == 4) {
-        const int row = 16 * g + i;
-        const uint8_t* p = vlds + row * W::PITCH + 8 * dt;
-        const v2i c2 = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i)(uintptr_t)(p));
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint32_t u = static_cast<uint32_t>(c2[x]), u8 = u >> 8;
-          vo[x] = operand(normal(u & 0x000F000Fu, 0), normal(u & 0x00F000F0u, 4), normal(u8 & 0x000F000Fu, 0), normal(u8 & 0x00F000F0u, 4));
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int row = 16 * g + 8 * x + (i >> 1);
-          const uint8_t* p = vlds + row * W::PITCH + 16 * dt + 8 * (i & 1);
-          const v2i c2 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(p));
-          const uint32_t u = static_cast<uint32_t>(c2[0]), v = static_cast<uint32_t>(c2[1]);
-          vo[x] = operand(normal(u & 0x00FF00FFu, 0), normal((u >> 8) & 0x00FF00FFu, 0), normal(v & 0x00FF00FFu, 0),
-                          normal((v >> 8) & 0x00FF00FFu, 0));
-        }
-      }
-    };
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      weights(rb);
-      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) {
-      v8h vo[2];
-      value(dt, vo);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vo[x], pf[rb][x], acc[rb][dt], 0, 0, 0);
-    }
-    asm volatile("" ::: "memory");
   }
 
-  // the waves' states of 16 rows at a time meet in LDS
-  const auto add = [](float u, float v) { return __fadd_rn(u, v); };
-  float* const red = reinterpret_cast<float*>(lds);   // [wave][row][kDimRow]
-  float* const red_ml = red + kWaves * 16 * kDimRow;  // [wave][row][2]
+  // Weights of column rb rounded to fp16 in the value codes' pair order; l and b sum the rounded ones.
+  __device__ __forceinline__ void weights(int rb, const float (&s)[16], const float* coef, v8h (&pf)[2]) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const float from = m[rb] == -INFINITY ? 0.0f : m[rb];
+    uint32_t pw[8];
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
+    for (int x = 0; x < 2; ++x) {
+      const float4 cr0 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 32 * x + 4 * g);
+      const float4 cr1 = *reinterpret_cast<const float4*>(coef + 3 * kBlock + 32 * x + 16 + 4 * g);
+      const float4 cv0 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 32 * x + 4 * g);
+      const float4 cv1 = *reinterpret_cast<const float4*>(coef + 4 * kBlock + 32 * x + 16 + 4 * g);
+      const float fr[8] = {cr0.x, cr0.y, cr0.z, cr0.w, cr1.x, cr1.y, cr1.z, cr1.w};
+      const float fv[8] = {cv0.x, cv0.y, cv0.z, cv0.w, cv1.x, cv1.y, cv1.z, cv1.w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        // pairs of tokens: 4 bits (0, 4), (1, 5), (2, 6), (3, 7); 8 bits (0, 2), (1, 3), ..
+        const int ta = BITS == 4 ? y : 4 * (y >> 1) + (y & 1), tb = ta + (BITS == 4 ? 4 : 2);
+        const uint32_t p2 = f2h2(exp2_fast(s[8 * x + ta] - from), exp2_fast(s[8 * x + tb] - from));
+        pw[4 * x + y] = p2;
+        const v2h ph = __builtin_bit_cast(v2h, p2);
+        l[rb] = __fmaf_rn(static_cast<float>(ph[0]), fr[ta], l[rb]);
+        l[rb] = __fmaf_rn(static_cast<float>(ph[1]), fr[tb], l[rb]);
+        bsum[rb] = __fmaf_rn(static_cast<float>(ph[0]), fv[ta], bsum[rb]);
+        bsum[rb] = __fmaf_rn(static_cast<float>(ph[1]), fv[tb], bsum[rb]);
+      }
+    }
+    pf[0] = operand(pw[0], pw[1], pw[2], pw[3]);
+    pf[1] = operand(pw[4], pw[5], pw[6], pw[7]);
+  }
+
+  __device__ __forceinline__ void values(int dt, const v8h (&vo)[2], const v8h (&pf)[RB][2]) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vo[x], pf[rb][x], acc[rb][dt], 0, 0, 0);
+  }
+
+  // The state of column rb when all blocks are through: l and b over all tokens, m as the join takes it.
+  __device__ __forceinline__ void finish(int rb) {
+    const auto add = [](float u, float v) { return __fadd_rn(u, v); };
     l[rb] = rows_all(l[rb], add);
     bsum[rb] = rows_all(bsum[rb], add);
     const float any = rows_all((seen >> rb) & 1u ? 1.0f : 0.0f, [](float u, float v) { return fmaxf(u, v); });
@@ -460,26 +449,177 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     } else if (m[rb] == -INFINITY) {
       m[rb] = kNoScore;
     }
-    const int left = min(16, rows - (r0 + 16 * rb));  // rows of this column
-    if (left <= 0) break;                             // the workgroup leaves together
+  }
+};
+
+// Puts down dims d .. d + 3 (not yet divided by L) of row `row` of the sequence: the output where the tile has one chunk,
+// else the chunk's state.
+__device__ __forceinline__ void store_row(const TreeArgs& a, const TreePlace& p, uint32_t magic_group, int row, int d, float M, float L, v4f D) {
+  uint32_t tok, gh;
+  div_rem(static_cast<uint32_t>(row), a.group, magic_group, tok, gh);
+  if (a.cu && p.base + static_cast<int>(tok) < 0) return;  // a row without a place
+  const int64_t t = p.q0 + static_cast<int64_t>(tok), head = static_cast<int64_t>(p.hk) * a.group + gh;
+  float* pr = a.part + ((t * a.hq + head) * a.plan.chunks + p.c) * kAttnPart;
+  if (a.plan.chunks > 1 && p.c == 0 && d == 0) pr[2] = static_cast<float>(p.own);  // what the join goes by
+  if (p.own == 1) {
+    uint16_t* o = a.out + t * a.ldo + head * 128 + d;
+    if (M == -INFINITY)  // no token
+      *reinterpret_cast<v2u*>(o) = v2u{0u, 0u};
+    else
+      *reinterpret_cast<v2u*>(o) = v2u{f2h2(__fdiv_rn(D[0], L), __fdiv_rn(D[1], L)), f2h2(__fdiv_rn(D[2], L), __fdiv_rn(D[3], L))};
+  } else {
+    if (d == 0) {
+      pr[0] = M;
+      pr[1] = L;
+    }
+    *reinterpret_cast<v4f*>(pr + 4 + d) = D;
+  }
+}
+
+// LDS of a wave of attn_tree_part: value codes of a block, its coefficients, the rows' sight, their queries (with two
+// columns, whose registers they would take).
+template <int BITS, int RB>
+struct TreeLds {
+  static constexpr int CODES = kBlock * kPitch<BITS>;
+  static constexpr int SIGHT = CODES + 7 * kBlock * 4, QUERIES = SIGHT + TreeRows<BITS, RB>::SIGHT * 4;
+  static constexpr int BYTES = QUERIES + (RB > 1 ? RB * 4096 : 0);
+};
+template <int BITS, int RB>
+constexpr int tree_lds() {
+  const int merge = kWaves * 16 * (kDimRow + 2) * 4, codes = kWaves * TreeLds<BITS, RB>::BYTES;
+  return merge > codes ? merge : codes;
+}
+
+template <int BITS, bool P16, int RB>
+__global__ void __launch_bounds__(64 * kWaves, 2)
+attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32_t magic_tiles, uint32_t magic_heads,
+               uint32_t magic_group, TreeArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  using W = TreeLds<BITS, RB>;
+  constexpr int ROWS = 16 * RB, ROW = BITS * 16;  // of the workgroup; bytes of a token's codes
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  TreePlace p;
+  if (!find_place<ROWS>(cu, lens, magic_tiles, magic_heads, magic_group, a, p)) return;
+
+  uint8_t* const vlds = lds + w * W::BYTES;
+  float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
+  v8h* const qlds = reinterpret_cast<v8h*>(vlds + W::QUERIES);
+  TreeRows<BITS, RB> r;
+  r.init(q, 0, magic_group, a, p, reinterpret_cast<int*>(vlds + W::SIGHT));
+  if constexpr (RB > 1) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) qlds[(4 * rb + x) * 64 + lane] = r.qf[rb][x];
+  }
+
+  constexpr int KW = BITS == 4 ? 1 : 2;  // 16-byte loads of a lane's key codes
+  v4u kc[4][KW], vc[4][KW];
+  float4 par;
+  bool par_ok;
+  // tokens without a page, or past the chunk, read page 0 and have no weight
+  auto load = [&](int v0, int32_t entry) __attribute__((always_inline)) {
+    const int t0 = p.run.position(v0);
+    const int32_t mine = valid_page(a.cache, entry), safe = max(mine, 0);
+    par_ok = mine >= 0 && v0 + lane < p.last;
+    // load j brings the 16 tokens of group j, which lie in one page: keys of token i from its byte 16 g (32 g) on, values
+    // in order, four (eight) lanes a token
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t at = token_slot(a.cache, __builtin_amdgcn_readlane(safe, 16 * j), p.hk, t0 + 16 * j) * ROW;
+      const uint8_t* const kp = a.cache.kq + at;
+      const uint8_t* const vp = a.cache.vq + at;
+#pragma unroll
+      for (int x = 0; x < KW; ++x) {
+        kc[j][x] = *reinterpret_cast<const v4u*>(kp + static_cast<uint32_t>(i * ROW + (BITS == 4 ? 16 : 32) * g + 16 * x));
+        vc[j][x] = *reinterpret_cast<const v4u*>(vp + static_cast<uint32_t>(16 * lane + 1024 * x));
+      }
+    }
+    par = token_params<P16>(a.cache, token_slot(a.cache, safe, p.hk, t0 + lane));
+  };
+
+  const int step = kWaves * kBlock;
+  int v0 = p.first + w * kBlock;
+  int32_t entry = -1;
+  if (v0 < p.last) {
+    load(v0, entry_of(a, p, v0));
+    entry = entry_of(a, p, v0 + step);
+  }
+  for (; v0 < p.last; v0 += step) {
+    // codes and coefficients to LDS (this wave's own: no barrier, its LDS operations are in order)
+#pragma unroll
+    for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+      for (int x = 0; x < KW; ++x) {
+        const int row = 16 * mm + (BITS == 4 ? lane >> 2 : 8 * x + (lane >> 3));
+        *reinterpret_cast<v4u*>(vlds + row * kPitch<BITS> + 16 * (lane & (BITS == 4 ? 3 : 7))) = vc[mm][x];
+      }
+    const uint64_t there = __ballot(par_ok);
+    const uint64_t odd = token_coefs(par, par_ok, a.scale_log2e, r.down, coef);
+    asm volatile("" ::: "memory");
+    if constexpr (RB > 1) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) r.qf[rb][x] = qlds[(4 * rb + x) * 64 + lane];
+    }
+    float s[RB][16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v8h ko[4];
+      key_operands<BITS>(kc[j], ko);
+      r.scores(j, ko, coef, s);
+      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    // the next block's codes, when the registers of this one's are free (asked for before the scores they cost
+    // a spill, and its way through memory, with two columns)
+    __builtin_amdgcn_sched_barrier(0);
+    if (v0 + step < p.last) {
+      load(v0 + step, entry);
+      entry = entry_of(a, p, v0 + 2 * step);
+    }
+    r.hide(p.run.position(v0), there, odd, coef, a, p, s);
+    r.move(s);
+    v8h pf[RB][2];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      r.weights(rb, s[rb], coef, pf[rb]);
+      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      v8h vo[2];
+      value_operands<BITS>(vlds, dt, vo);
+      r.values(dt, vo, pf);
+    }
+    asm volatile("" ::: "memory");
+  }
+
+  // the waves' states of 16 rows at a time meet in LDS
+  float* const red = reinterpret_cast<float*>(lds);   // [wave][row][kDimRow]
+  float* const red_ml = red + kWaves * 16 * kDimRow;  // [wave][row][2]
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    r.finish(rb);
+    const int left = min(16, p.rows - (p.r0 + 16 * rb));  // rows of this column
+    if (left <= 0) break;                                 // the workgroup leaves together
     __syncthreads();
     if (g == 0) {
-      red_ml[(w * 16 + i) * 2] = m[rb];
-      red_ml[(w * 16 + i) * 2 + 1] = l[rb];
+      red_ml[(w * 16 + i) * 2] = r.m[rb];
+      red_ml[(w * 16 + i) * 2 + 1] = r.l[rb];
     }
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
       v4f o;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) o[r] = __fmaf_rn(acc[rb][dt][r], 512.0f, bsum[rb]);
+      for (int x = 0; x < 4; ++x) o[x] = __fmaf_rn(r.acc[rb][dt][x], 512.0f, r.bsum[rb]);
       *reinterpret_cast<v4f*>(red + (w * 16 + i) * kDimRow + 16 * dt + 4 * g) = o;
     }
     __syncthreads();
     for (int x = threadIdx.x; x < left * 32; x += 64 * kWaves) {
       const int rr = x >> 5, d = 4 * (x & 31);
-      uint32_t tok, gh;
-      div_rem(static_cast<uint32_t>(r0 + 16 * rb + rr), a.group, magic_group, tok, gh);
-      if (a.cu && base + static_cast<int>(tok) < 0) continue;  // a row without a place
       float M = -INFINITY;
 #pragma unroll
       for (int v = 0; v < kWaves; ++v) M = fmaxf(M, red_ml[(v * 16 + rr) * 2]);
@@ -491,24 +631,9 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
         L = __fmaf_rn(red_ml[(v * 16 + rr) * 2 + 1], f, L);
         const v4f o = *reinterpret_cast<const v4f*>(red + (v * 16 + rr) * kDimRow + d);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) D[r] = __fmaf_rn(o[r], f, D[r]);
+        for (int y = 0; y < 4; ++y) D[y] = __fmaf_rn(o[y], f, D[y]);
       }
-      const int64_t t = tt.q0 + static_cast<int64_t>(tok), head = static_cast<int64_t>(hk) * a.group + gh;
-      float* pr = a.part + ((t * a.hq + head) * a.plan.chunks + c) * kAttnPart;
-      if (a.plan.chunks > 1 && c == 0 && d == 0) pr[2] = static_cast<float>(own);  // what the join goes by
-      if (own == 1) {
-        uint16_t* o = a.out + t * a.ldo + head * 128 + d;
-        if (M == -INFINITY)  // no token
-          *reinterpret_cast<v2u*>(o) = v2u{0u, 0u};
-        else
-          *reinterpret_cast<v2u*>(o) = v2u{f2h2(__fdiv_rn(D[0], L), __fdiv_rn(D[1], L)), f2h2(__fdiv_rn(D[2], L), __fdiv_rn(D[3], L))};
-      } else {
-        if (d == 0) {
-          pr[0] = M;
-          pr[1] = L;
-        }
-        *reinterpret_cast<v4f*>(pr + 4 + d) = D;
-      }
+      store_row(a, p, magic_group, p.r0 + 16 * rb + rr, d, M, L, D);
     }
   }
 }
