@@ -64,19 +64,16 @@ inline void paged_split(int64_t B, int64_t max_len, int32_t hq, int32_t hkv, int
 
 // Several rows of a sequence over its pages: workgroups of 16 * rb (row, query head) pairs, `tiles` of them
 // at most, and the tokens that they see in `chunks` pieces of chunk_tokens.
-//   rb: a column of 16 rows, or two that share the expanded codes.  Two need whole columns, and work
-//   enough that half the workgroups still fill the compute units (64 drafts behind 131008 tokens, 32 heads on
-//   8, us: one column 325, two 227; 16 behind 2048 12.6 and 13.5).  With 8 bits, whose codes take fewer
-//   instructions and more registers, they gain from 128 rows on (256 rows over 131072 tokens 385 and 345; 32
-//   rows 72 and 81; rows of 2 .. 256 over 16 sequences 97 and 105).
+//   rb: a column of 16 rows, or two that share the expanded codes.  Two need whole columns, and work enough that half
+//   the workgroups still fill the compute units (64 drafts behind 131008 tokens, 32 heads on 8, us: one column 315, two
+//   219; 8 behind 131008 with 8 bits 73 and 65; 16 behind 2048 12.8 and 13.5).
 //   chunks: as in decode above for up to 16 rows; more work longer on a token, and of several sequences half as
 //   many pieces do (16 sequences of 4096 tokens, 64 rows, 8 heads: 1024 tokens 26.6, 512 33.6, 2048 30.4).
-//   They do not go by rb, so that the workspace is the same for 4 and 8 bits.
 struct TreePlan {
   int32_t rb, tiles, chunks, chunk_tokens;
 };
 inline TreePlan tree_plan(int64_t B, int64_t T, bool single, int64_t max_len, int32_t window, int32_t sinks, int32_t hq, int32_t hkv,
-                          int32_t bits, int cus) {
+                          int cus) {
   constexpr int64_t unit = kPagedWaves * kPagedBlock;
   const int64_t group = hq / hkv, rows = T * group, some = B > 0 ? B : 1;
   TreePlan p{};
@@ -87,7 +84,7 @@ inline TreePlan tree_plan(int64_t B, int64_t T, bool single, int64_t max_len, in
     if (run > most) run = most;
   }
   const int64_t each = (rows + some - 1) / some;  // rows of an average sequence
-  const bool two = each > (bits == 8 ? 127 : 16) && some * ((each + 31) / 32) * hkv * ((run + unit - 1) / unit) >= cus;
+  const bool two = each > 16 && some * ((each + 31) / 32) * hkv * ((run + unit - 1) / unit) >= cus;
   p.rb = two ? 2 : 1;
   const int64_t tile = 16 * p.rb;
   p.tiles = static_cast<int32_t>(single ? B * ((group + tile - 1) / tile) : (rows + B * (tile - 1)) / tile);

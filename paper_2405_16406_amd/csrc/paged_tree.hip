@@ -571,7 +571,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
       v8h ko[4];
       key_operands<BITS>(kc[j], ko);
       r.scores(j, ko, coef, s);
-      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
+      if constexpr (RB > 1 && BITS == 4) __builtin_amdgcn_sched_barrier(0);
     }
     // the next block's codes, when the registers of this one's are free (asked for before the scores they cost
     // a spill, and its way through memory, with two columns)
@@ -584,10 +584,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     r.move(s);
     v8h pf[RB][2];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      r.weights(rb, s[rb], coef, pf[rb]);
-      if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int rb = 0; rb < RB; ++rb) r.weights(rb, s[rb], coef, pf[rb]);
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
       v8h vo[2];

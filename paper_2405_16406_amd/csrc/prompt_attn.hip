@@ -78,6 +78,9 @@ __device__ __forceinline__ float halves(float v, Op op) {
   return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
+// The lowest n of 64 bits, none for n <= 0 and all from 64 on.
+__device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~uint64_t{0} : (uint64_t{1} << max(n, 0)) - 1; }
+
 // Schedule of a run of N products whose first operand takes R LDS reads: reads stay AHEAD operands
 // in front (the compiler would read all of them first and run out of registers).
 template <int N, int R, int AHEAD>
@@ -272,16 +275,24 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   // MASK: the tile holds keys that a row of the wave does not see
   auto softmax = [&](int kt, auto mc) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mc)::value;
-    if constexpr (MASK) {
-      const int left = lim - kt * kTile - 4 * h;
-      const int from = lo - kt * kTile - 4 * h, always = a.sinks - kt * kTile - 4 * h;
+    if constexpr (MASK && WIN) {  // a bit for each key, and two operations a score, whatever hides it
+      const int k0 = kt * kTile + 4 * h;
+      const uint64_t vis = below(lim + 1 - k0) & (~below(lo - k0) | below(a.sinks - k0));
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int x = 32 * mt + 8 * (r >> 2) + (r & 3);
-          if (x > left || (WIN && x < from && x >= always)) s[mt][r] = -INFINITY;
+          const int x = 8 * (r >> 2) + (r & 3);
+          const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(static_cast<uint32_t>(vis >> (32 * mt)) << (31 - x)) >> 31);
+          s[mt][r] = __uint_as_float((__float_as_uint(s[mt][r]) & keep) | (~keep & 0xFF800000u));  // -inf
         }
+    } else if constexpr (MASK) {
+      const int left = lim - kt * kTile - 4 * h;
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * mt + 8 * (r >> 2) + (r & 3) > left) s[mt][r] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll

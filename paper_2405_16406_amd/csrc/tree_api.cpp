@@ -24,13 +24,13 @@ sq_status check_tree_sizes(int64_t B, int64_t T, int64_t max_len, int32_t window
   return SQ_OK;
 }
 
-// The plan on the current device, and the workspace bytes it needs (which do not go by the bits).
+// The plan on the current device, and the workspace bytes it needs.
 sq_status tree_plan_here(int64_t B, int64_t T, bool single, int64_t max_len, int32_t window, int32_t sinks, int64_t Hq, int64_t Hkv,
-                         int32_t bits, sq::TreePlan& plan, uint64_t& bytes) {
+                         sq::TreePlan& plan, uint64_t& bytes) {
   int cus = 0;
   const hipError_t e = sq::device_cus(&cus);
   if (e != hipSuccess) return hip_status(e, "compute-unit count of the current device");
-  plan = sq::tree_plan(B, T, single, max_len, window, sinks, static_cast<int32_t>(Hq), static_cast<int32_t>(Hkv), bits, cus);
+  plan = sq::tree_plan(B, T, single, max_len, window, sinks, static_cast<int32_t>(Hq), static_cast<int32_t>(Hkv), cus);
   bytes = plan.chunks > 1 ? static_cast<uint64_t>(T) * Hq * plan.chunks * (sq::kAttnPart * 4) : 0;
   return SQ_OK;
 }
@@ -61,7 +61,7 @@ sq_status attn_tree(const void* q, int64_t ldq, const int32_t* cu, bool single, 
   if (s != SQ_OK) return s;
   if (T == 0 || B == 0) return ok();
   uint64_t need = 0;
-  if ((s = tree_plan_here(B, T, single, max_len, window, sinks, Hq, Hkv, bits, a.plan, need)) != SQ_OK) return s;
+  if ((s = tree_plan_here(B, T, single, max_len, window, sinks, Hq, Hkv, a.plan, need)) != SQ_OK) return s;
   if ((s = check_workspace(workspace, workspace_bytes, need)) != SQ_OK) return s;
   a.q = static_cast<const uint16_t*>(q);
   a.ldq = ldq;
@@ -155,7 +155,7 @@ sq_status sq_attn_tree_workspace(int64_t B, int64_t T, int64_t max_len, int32_t 
   if (s != SQ_OK) return s;
   sq::TreePlan plan{};
   uint64_t need = 0;
-  if ((s = tree_plan_here(B, T, false, max_len, window, sinks, Hq, Hkv, 4, plan, need)) != SQ_OK) return s;
+  if ((s = tree_plan_here(B, T, false, max_len, window, sinks, Hq, Hkv, plan, need)) != SQ_OK) return s;
   *bytes = need;
   return ok();
 }
@@ -177,7 +177,7 @@ sq_status sq_attn_paged_window_workspace(int64_t B, int64_t max_len, int32_t win
   if (s != SQ_OK) return s;
   sq::TreePlan plan{};
   uint64_t need = 0;
-  if ((s = tree_plan_here(B, B, true, max_len, window, sinks, Hq, Hkv, 4, plan, need)) != SQ_OK) return s;
+  if ((s = tree_plan_here(B, B, true, max_len, window, sinks, Hq, Hkv, plan, need)) != SQ_OK) return s;
   *bytes = need;
   return ok();
 }
