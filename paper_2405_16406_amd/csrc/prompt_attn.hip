@@ -129,27 +129,29 @@ __device__ __forceinline__ PromptTile find_tile(const int32_t* cu_q, const int32
 
 // WIN: a row sees the keys up to its own from lim - window + 1 on, and those below sinks; the workgroup's tiles
 // are those of its rows' run of keys (paged.h), the first ones with keys below sinks and then the windows'.
-template <bool SPLIT, int KG, bool WIN>
-__global__ void __launch_bounds__(64 * kWaves, 2)
-attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* cu_q, const int32_t* cu_k,
-                 uint32_t magic_heads, uint32_t magic_group, uint32_t magic_splits, PromptArgs a) {
+// CAREFUL: values that are not finite are looked for where some row does not see them; without, the caller is told
+// (true: nothing written) when the result holds something that is not finite, and starts over with it.
+template <bool SPLIT, int KG, bool WIN, bool CAREFUL>
+__device__ __forceinline__ bool prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* cu_q,
+                                            const int32_t* cu_k, uint32_t magic_heads, uint32_t magic_group, uint32_t magic_splits,
+                                            uint32_t block, uint32_t thread, const PromptArgs& a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   using P = Prompt<KG>;
-  const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = thread & 63;
+  const int w = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int late = w >> 2;              // the second of a SIMD's two waves
   const int rw = KG == 1 ? w : w & 3;   // which rows,
   const int kg = KG == 1 ? 0 : late;    // and which group of waves
   const int col = lane & 31, h = lane >> 5;
   uint32_t rest, hk, split = 0;
-  div_rem(blockIdx.x, a.hkv, magic_heads, rest, hk);
+  div_rem(block, a.hkv, magic_heads, rest, hk);
   if constexpr (SPLIT) {
     uint32_t r2;
     div_rem(rest, a.splits, magic_splits, r2, split);
     rest = r2;
   }
   const PromptTile pt = find_tile<P::ROWS>(cu_q, cu_k, a.B, a.Tq, a.Tk, a.group, static_cast<int>(rest));
-  if (pt.seq < 0) return;  // the workgroup leaves together
+  if (pt.seq < 0) return false;  // the workgroup leaves together
   const int tile = a.causal ? pt.tiles - 1 - pt.tile : pt.tile;  // the longest first
   const int k0 = pt.k0, m = pt.m;
   const int rows = pt.n * a.group;
@@ -180,7 +182,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     const int per = prompt_part(tiles_all, a.splits, a.per);
     kt0 = min(static_cast<int>(split) * per, tiles_all);
     kt1 = min(kt0 + per, tiles_all);
-    if (split > 0 && kt0 == kt1) return;  // the workgroup leaves together; part 0 is always there
+    if (split > 0 && kt0 == kt1) return false;  // the workgroup leaves together; part 0 is always there
   }
 
   // Q^T operands: lane (row, h) holds dims 16 s + 8 h .. + 7
@@ -365,7 +367,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   };
   auto values = [&](int kt, int buf, auto mc) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mc)::value;
-    if constexpr (MASK) {
+    if constexpr (MASK && CAREFUL) {
       uint32_t any = 0;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
@@ -521,6 +523,22 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
   }
   if (!late) meet();
 
+  if constexpr (!CAREFUL) {
+    float sum = 0.0f;  // NaN where one is not finite
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum = __fmaf_rn(acc[dt][r], 0.0f, sum);
+    uint32_t* const found = reinterpret_cast<uint32_t*>(lds + P::LDS);  // of each wave
+    const bool mine = __ballot(sum != 0.0f) != 0;
+    if (lane == 0) found[w] = mine;
+    __syncthreads();
+    uint32_t any = 0;
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) any |= found[x];
+    if (__builtin_amdgcn_readfirstlane(any) != 0) return true;  // the workgroup together, done with the tiles
+  }
+
   l = halves(l, [](float x, float y) { return __fadd_rn(x, y); });
   if constexpr (KG == 2) {  // the second group's states go to the first through LDS
     float* const states = reinterpret_cast<float*>(lds);                       // [wave][64 dims][lane]
@@ -537,7 +555,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       odds[rw * 128 + 64 + lane] = down;
     }
     __syncthreads();
-    if (kg == 1) return;
+    if (kg == 1) return false;
     const float2 o = stats[rw * 64 + lane];
     const float M = fmaxf(mx, o.x);
     const float f0 = rescale(mx, M), f1 = rescale(o.x, M);
@@ -550,7 +568,7 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
     up |= odds[rw * 128 + lane];
     down |= odds[rw * 128 + 64 + lane];
   }
-  if (row >= rows) return;
+  if (row >= rows) return false;
   bool sees = lim >= kt0 * kTile;  // a key of this part
   if constexpr (WIN) {
     const int p0 = (kt0 < head_tiles ? kt0 : kt0 + gap) * kTile;  // its first key; from the windows' first tile on, and its end
@@ -590,6 +608,19 @@ attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const 
       for (int y = 0; y < 4; ++y)
         *reinterpret_cast<v2u*>(o + 32 * dt + 8 * y) =
             v2u{f2h2(acc[dt][4 * y], acc[dt][4 * y + 1]), f2h2(acc[dt][4 * y + 2], acc[dt][4 * y + 3])};
+  }
+  return false;
+}
+
+template <bool SPLIT, int KG, bool WIN>
+__global__ void __launch_bounds__(64 * kWaves, 2)
+attn_prompt_tile(const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* cu_q, const int32_t* cu_k,
+                 uint32_t magic_heads, uint32_t magic_group, uint32_t magic_splits, PromptArgs a) {
+  uint32_t block = blockIdx.x, thread = threadIdx.x;
+  if (!prompt_tile<SPLIT, KG, WIN, !WIN>(q, k, v, cu_q, cu_k, magic_heads, magic_group, magic_splits, block, thread, a)) return;
+  if constexpr (WIN) {
+    asm volatile("" : "+s"(block), "+v"(thread));  // (so that nothing is kept for this from before)
+    prompt_tile<SPLIT, KG, WIN, true>(q, k, v, cu_q, cu_k, magic_heads, magic_group, magic_splits, block, thread, a);
   }
 }
 
@@ -661,11 +692,12 @@ template <bool SPLIT, int KG, bool WIN>
 hipError_t launch_form(const PromptArgs& a, hipStream_t stream) {
   using P = Prompt<KG>;
   constexpr auto kern = attn_prompt_tile<SPLIT, KG, WIN>;
-  const hipError_t init = set_max_lds<kern>(P::LDS);
+  constexpr int lds = P::LDS + (WIN ? kWaves * 4 : 0);
+  const hipError_t init = set_max_lds<kern>(lds);
   if (init != hipSuccess) return init;
   // as many tiles as any division of the rows among B sequences can make
   const int64_t tiles = a.Tq * a.group / P::ROWS + a.B;
-  return launch(kern, dim3(static_cast<unsigned>(tiles * a.hkv * a.splits)), dim3(64 * kWaves), P::LDS, stream, a.q, a.k, a.v, a.cu_q,
+  return launch(kern, dim3(static_cast<unsigned>(tiles * a.hkv * a.splits)), dim3(64 * kWaves), lds, stream, a.q, a.k, a.v, a.cu_q,
                 a.cu_k, div_magic(static_cast<uint32_t>(a.hkv)), div_magic(static_cast<uint32_t>(a.group)),
                 div_magic(static_cast<uint32_t>(a.splits)), a);
 }

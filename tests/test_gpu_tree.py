@@ -308,7 +308,7 @@ def test_attn_prompt_window(case):
     assert torch.all(out[up(~rows)] == 7.0)
 
 
-@pytest.mark.parametrize("Hq,nq,nk", [(2, 300, 300), (2, 4, 3000)], ids=["whole", "parts"])
+@pytest.mark.parametrize("Hq,nq,nk", [(2, 300, 300), (2, 4, 3000), (130, 300, 300)], ids=["halves", "parts", "whole"])
 def test_prompt_keys_behind_the_window(Hq, nq, nk):
     """What is not finite in keys and values that a row does not see leaves it alone; the rows that see it are not finite."""
     g = rng(21)
