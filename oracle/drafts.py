@@ -71,34 +71,36 @@ def attn_tree(q, cache, cu, lens, table, max_len, sees=None, depth=None, window=
     """(out fp64 [T, Hq, 128], weight: sum p (|va c| + |vb|) of each, rows: which are written)."""
     T, Hq = q.shape[:2]
     pages, H, page, _ = cache["k_q"].shape
+    group = Hq // H
     scale = 1 / math.sqrt(D) if scale is None else scale
     out, weight, rows = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.zeros(T, dtype=bool)
     for b in range(len(lens)):
         n, length = int(cu[b + 1]) - int(cu[b]), max(int(lens[b]), 0)
-        where = [page_of(table, b, t, page, pages) for t in range(min(length, max_len))]
-        values = {}
+        there, parts = [], []
+        for t in range(min(length, max_len)):
+            where = page_of(table, b, t, page, pages)
+            there.append(where >= 0)
+            parts.append([np.stack(np.broadcast_arrays(*_values(cache, s, max(where, 0), t % page))) for s in (0, 1)])
+        if parts:
+            parts = np.array(parts)  # [token, key or value, alpha c or beta, head, 128]
         for i in range(n):
             t = int(cu[b]) + i
             if length - n + i < 0:
                 continue
             rows[t] = True
             keys = [x for x in seen_keys(i, n, length, max_len, None if sees is None else sees[t], i if depth is None else int(depth[t]),
-                                         window, sinks) if where[x] >= 0]
+                                         window, sinks) if there[x]]
             if not keys:
                 continue
-            for x in keys:
-                if x not in values:
-                    values[x] = [_values(cache, s, where[x], x % page) for s in (0, 1)]
+            seen = parts[keys]
             for g in range(H):
-                K = np.stack([values[x][0][0][g] + values[x][0][1][g] for x in keys])
-                va, vb = (np.stack([values[x][1][s][g] for x in keys]) for s in (0, 1))
-                heads = slice(g * (Hq // H), (g + 1) * (Hq // H))
-                s = q[t, heads].astype(np.float64) @ K.T * scale
+                heads = slice(g * group, (g + 1) * group)
                 with np.errstate(invalid="ignore"):
+                    s = q[t, heads].astype(np.float64) @ seen[:, 0, :, g].sum(1).T * scale
                     p = np.exp(s - s.max(-1, keepdims=True))
                     p /= p.sum(-1, keepdims=True)
-                    out[t, heads] = p @ (va + vb)
-                    weight[t, heads] = p @ (np.abs(va) + np.abs(vb))
+                    out[t, heads] = p @ seen[:, 1, :, g].sum(1)
+                    weight[t, heads] = p @ np.abs(seen[:, 1, :, g]).sum(1)
     return out, weight, rows
 
 

@@ -640,7 +640,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
 template <int J>
 __global__ void __launch_bounds__(64 * J)
 attn_tree_combine(const float* part, const int32_t* cu, const int32_t* lens, int64_t B, uint16_t* out, int64_t ldo, int hq, int chunks,
-                  uint32_t magic_hq) {
+                  uint32_t magic_hq, int32_t rows) {
   __shared__ float red_m[J], red_l[J];
   __shared__ float2 red_d[J][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -650,7 +650,7 @@ attn_tree_combine(const float* part, const int32_t* cu, const int32_t* lens, int
   const float number = pr[2];
   if (cu) {
     const RowSeq s = find_sequence(cu, lens, B, t);
-    if (s.seq < 0 || row_position(s.len, s.end, t) < 0) return;  // left as it was: nobody wrote its states
+    if (s.seq < 0 || row_position(s.len, min(s.end, rows), t) < 0) return;  // left as it was: nobody wrote its states
   }
   const int n = min(static_cast<int>(number), chunks);
   if (n <= 1) return;
@@ -731,7 +731,7 @@ hipError_t launch_attn_tree(const TreeArgs& a, hipStream_t stream) {
   if (e != hipSuccess || a.plan.chunks == 1) return e;
   const auto join = [&](auto kern, int waves) {
     return launch(kern, dim3(static_cast<unsigned>(a.T * a.hq)), dim3(64 * waves), 0, stream, a.part, a.cu, a.lens, a.B, a.out, a.ldo,
-                  a.hq, a.plan.chunks, div_magic(static_cast<uint32_t>(a.hq)));
+                  a.hq, a.plan.chunks, div_magic(static_cast<uint32_t>(a.hq)), static_cast<int32_t>(a.T));
   };
   return a.plan.chunks <= 8 ? join(attn_tree_combine<1>, 1) : join(attn_tree_combine<8>, 8);
 }

@@ -142,6 +142,11 @@ ATTN = [  # Hq, Hkv, page, bits, params, drafts, tokens before, window, sinks
     (4, 4, 16, 8, np.float16, [40, 1], [700, 800], 100, 70),               # first tokens beyond a block
     (8, 1, 128, 4, np.float16, [9], [1000], 1, 0),
     (16, 2, 16, 4, np.float32, [70, 5], [90, 2000], 64, 16),
+    (64, 8, 32, 4, np.float16, [32, 5, 17], [1500, 700, 64], 0, 0),        # two columns
+    (32, 32, 16, 8, np.float32, [20, 33], [300, 1100], 0, 0),
+    (64, 8, 16, 8, np.float16, [16, 7], [900, 600], 500, 20),
+    (36, 12, 16, 4, np.float32, [11, 6, 23], [1200, 800, 5], 700, 3),      # rows across columns
+    (8, 2, 16, 4, np.float32, [9], [7000], 0, 0),                          # many chunks
 ]
 
 
@@ -366,3 +371,354 @@ def test_keep_nothing():
     dc = device_cache(cache)
     got = sq.kv_keep(dc, ints(table), ints([20, 30]), ints([0, 4, 9]), ints([[0], [0]]), ints([0, -3]))
     assert got.tolist() == [16, 25] and all(np.array_equal(t.cpu().numpy(), cache[n]) for t, n in zip(dc, ("k_q", "v_q", "params")))
+
+
+def test_many_sequences():
+    """More sequences than one step of the searches, some without drafts, in several chunks."""
+    g = rng(31)
+    B, Hq, H, page = 150, 8, 2, 16
+    new = [int(x) for x in g.integers(0, 5, B)]
+    new[7], new[140] = 30, 17
+    lens = [n + int(x) for n, x in zip(new, g.integers(0, 90, B))]
+    lens[3], lens[149] = new[3] + 1500, new[149] + 900
+    cu, T = packed(new, 3), sum(new) + 5
+    table, pages = spread_table(g, lens, page)
+    cache = filled(g, pages, H, page, 4, np.float16)
+    q = heads_of(g, T, Hq)
+    parents = np.concatenate([[0] * 3] + [np.array(tree(g, n), dtype=np.int64) for n in new] + [[0] * 2]).astype(np.int64)
+    mask, depth = sq.tree_mask(ints(parents), ints(cu), 30)
+    sees, want_depth, rows = od.tree_mask(parents, cu)
+    assert np.array_equal(mask.cpu().numpy()[rows], od.words_of(sees, 1)[rows]) and np.array_equal(depth.cpu().numpy()[rows], want_depth[rows])
+    n = sq.attn_tree_workspace_bytes(B, T, max(lens), Hq, H)
+    assert n > 0
+    ws = torch.full((n + 16,), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full((T, Hq, 128), 7.0, dtype=torch.float16, device=DEV)
+    sq.attn_tree(up(q), device_cache(cache), ints(table), ints(lens), ints(cu), max(lens), mask=mask, out=out, workspace=ws)
+    want, weight, rows = od.attn_tree(q, cache, cu, lens, table, max(lens), sees)
+    attention_close(out[up(rows)], want[rows], weight[rows], 2e-5)
+    assert torch.all(out[up(~rows)] == 7.0) and torch.all(ws[n:] == 255)
+
+
+def test_a_chain_is_what_the_chunk_of_a_prompt_is():
+    """A chunk's rows over the pages against the same keys read back and attended in fp16 (rounded there: 2^-11 of keys,
+    16 of them in a score of this size, and of values)."""
+    g = rng(32)
+    Hq, H, page, n, length = 16, 4, 32, 300, 1300
+    table, pages = spread_table(g, [length], page)
+    dc = device_cache(filled(g, pages, H, page, 8, np.float32))
+    q = up(heads_of(g, n, Hq))
+    for window, sinks in ((0, 0), (200, 5)):
+        got = sq.attn_tree(q, dc, ints(table), ints([length]), ints([0, n]), length, window=window, sinks=sinks)
+        k, v = sq.kv_read(dc, ints(table), ints([length]), ints([0, length]), length)
+        want = sq.attn_prompt(q, k, v, ints([0, n]), ints([0, length]), window=window, sinks=sinks)
+        size = f64(v).max()
+        assert np.abs(f64(got) - f64(want)).max() <= (2.0 ** -11 * 16 + 3 * 2.0 ** -11) * size
+
+
+def test_a_window_of_everything_is_no_window():
+    g = rng(33)
+    lens, page = [300, 20], 16
+    table, pages = spread_table(g, lens, page)
+    dc = device_cache(filled(g, pages, 2, page, 4, np.float32))
+    q = up(heads_of(g, 2, 8))
+    a = sq.attn_paged(q, dc, ints(table), ints(lens), 300)
+    for window, sinks in ((300, 0), (2 ** 30 - 1, 0), (1, 2 ** 30 - 1), (5, 295)):
+        b = sq.attn_paged(q, dc, ints(table), ints(lens), 300, window=window, sinks=sinks)
+        assert np.abs(f64(a) - f64(b)).max() <= 2 * (2.0 ** -11 + 2e-5) * 8
+    p = up(heads_of(g, 90, 8)), up(heads_of(g, 90, 2)), up(heads_of(g, 90, 2))
+    cu = ints([0, 90])
+    a = sq.attn_prompt(*p, cu, cu)
+    for window, sinks in ((90, 0), (2 ** 30 - 1, 0), (3, 87)):
+        assert torch.equal(a, sq.attn_prompt(*p, cu, cu, window=window, sinks=sinks)), (window, sinks)
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 2.0])
+def test_scales(scale):
+    g = rng(34)
+    lens, cu = [150, 70], [0, 9, 15]
+    table, pages = spread_table(g, lens, 16)
+    cache = filled(g, pages, 2, 16, 4, np.float32, 0.5)
+    q = heads_of(g, 15, 8, 0.5)
+    sees, depth, _ = od.tree_mask(tree(g, 9) + tree(g, 6), cu)
+    got = sq.attn_tree(up(q), device_cache(cache), ints(table), ints(lens), ints(cu), 150, mask=up(od.words_of(sees, 1)), scale=scale)
+    want, weight, _ = od.attn_tree(q, cache, cu, lens, table, 150, sees, scale=scale)
+    # fp32 scores: 130 roundings of scale sum |q k|
+    attention_close(got, want, weight, 2e-5 + 130 * 2.0 ** -24 * abs(scale) * 128 * 0.5)
+
+
+@pytest.mark.parametrize("std", [2.0 ** -23, 2.0 ** -14, 2.0 ** 9])
+def test_queries_of_any_size(std):
+    """Queries of subnormal and of large numbers, with a scale that makes the scores the same; one row far below the others."""
+    g = rng(35)
+    lens, cu = [200], [0, 8]
+    table, pages = spread_table(g, lens, 16)
+    cache = filled(g, pages, 2, 16, 4, np.float32)
+    q = heads_of(g, 8, 8, std)
+    q[3] = heads_of(g, 1, 8, std * 2.0 ** -6)[0]
+    scale = 128 ** -0.5 / std
+    got = sq.attn_tree(up(q), device_cache(cache), ints(table), ints(lens), ints(cu), 200, scale=scale)
+    want, weight, _ = od.attn_tree(q, cache, cu, lens, table, 200, scale=scale)
+    attention_close(got, want, weight, 2e-5)
+
+
+def test_slots_that_were_never_written():
+    """A zeroed cache, and drafts that see such slots."""
+    g = rng(36)
+    got = sq.attn_tree(up(heads_of(g, 5, 8)), sq.kv_cache(5, 16, 2), ints([[4, 2, 0]]), ints([41]), ints([0, 5]), 41)
+    assert not got.any()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_pages_beyond_32_bits(bits):
+    """A pool of more than 4 GiB of codes: attention over its last pages, and a draft moved among them."""
+    H, page, row = 64, 128, 16 * bits
+    pages = (2 ** 32 + 2 ** 28) // (H * page * row)
+    k_q = torch.zeros((pages, H, page, row), dtype=torch.uint8, device=DEV)
+    cache = k_q, torch.zeros_like(k_q), torch.zeros((pages, H, page, 4), dtype=torch.float16, device=DEV)
+    g = rng(37)
+    small = filled(g, 2, H, page, bits, np.float16)
+    for t, n in zip(cache, ("k_q", "v_q", "params")):
+        t[pages - 2:] = up(small[n])
+    table, near = [[pages - 1, pages - 2]], [[1, 0]]
+    q = up(heads_of(g, 12, H))
+    args = ints([230]), ints([0, 12]), 230
+    want = sq.attn_tree(q, device_cache(small), ints(near), *args)
+    assert torch.equal(sq.attn_tree(q, cache, ints(table), *args), want)
+    want = sq.attn_paged(q[:1], device_cache(small), ints(near), ints([230]), 230, window=60, sinks=4)
+    assert torch.equal(sq.attn_paged(q[:1], cache, ints(table), ints([230]), 230, window=60, sinks=4), want)
+    dc = device_cache(small)
+    path, kept = ints([[0, 3, 7, 11]]), ints([4])
+    assert sq.kv_keep(dc, ints(near), ints([260 - 9]), ints([0, 12]), path, kept).tolist() == [243]
+    sq.kv_keep(cache, ints(table), ints([251]), ints([0, 12]), path, kept)
+    assert all(torch.equal(a[pages - 2:], b) for a, b in zip(cache, dc))
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Captured trees of different sizes over one workspace, replayed in turn with eager work between: each as eager."""
+    g = rng(41)
+    Hq, H, page = 32, 8, 16
+    calls, buffers = [], []
+    size = 0
+    for new, past, window in (([16], [2000], 0), ([3, 9, 1], [900, 70, 400], 0), ([8], [1500], 300)):
+        lens, cu = [n + p for n, p in zip(new, past)], packed(new)
+        table, pages = spread_table(g, lens, page)
+        sees, depth, _ = od.tree_mask(sum((tree(g, n) for n in new), []), cu, lens, window, 2)
+        args = dict(mask=up(od.words_of(sees, 1)), depth=ints(depth), window=window, sinks=2 if window else 0)
+        cache = device_cache(filled(g, pages, H, page, 4, np.float32))
+        q = up(heads_of(g, sum(new), Hq))
+        place = cache, ints(table), ints(lens), ints(cu), max(lens)
+        size = max(size, sq.attn_tree_workspace_bytes(len(new), sum(new), max(lens), Hq, H, window, args["sinks"]))
+        buffers.append((q, torch.empty_like(q)))
+        calls.append((place, args))
+    ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+
+    def call(k):
+        (q, out), (place, args) = buffers[k], calls[k]
+        sq.attn_tree(q, *place, out=out, workspace=ws, **args)
+
+    for k in range(3):
+        call(k)
+    torch.cuda.synchronize()
+    graphs = []
+    for k in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(k)
+        graphs.append(graph)
+    for turn in range(4):
+        for k in range(2):
+            buffers[k][0].copy_(up(heads_of(g, buffers[k][0].shape[0], Hq)))
+        wants = [sq.attn_tree(buffers[k][0], *calls[k][0], **calls[k][1]) for k in range(3)]
+        for k in (0, 1) if turn % 2 else (1, 0):
+            graphs[k].replay()
+            call(2)
+        torch.cuda.synchronize()
+        for k in range(3):
+            assert torch.equal(buffers[k][1], wants[k]), (turn, k)
+
+
+def test_another_stream():
+    g = rng(42)
+    lens, cu = [700], [0, 20]
+    table, pages = spread_table(g, lens, 16)
+    dc = device_cache(filled(g, pages, 2, 16, 4, np.float32))
+    q = up(heads_of(g, 20, 8))
+    args = dc, ints(table), ints(lens), ints(cu), 700
+    want = sq.attn_tree(q, *args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        late = q * 1.0
+        got = sq.attn_tree(late, *args)
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_empty_calls():
+    cache = sq.kv_cache(2, 16, 2)
+    none, one = ints([]), ints([0])
+    q = torch.empty((0, 8, 128), dtype=torch.float16, device=DEV)
+    assert sq.attn_tree(q, cache, ints([[0]]), ints([5]), ints([0, 0]), 5).shape == (0, 8, 128)
+    assert sq.attn_tree(q, cache, none.view(0, 1), none, one, 5).shape == (0, 8, 128)
+    assert sq.attn_paged(q, cache, none.view(0, 1), none, 5, window=4).shape == (0, 8, 128)
+    assert sq.attn_prompt(q, q[:, :2], q[:, :2], one, one, window=4).shape == (0, 8, 128)
+    mask, depth = sq.tree_mask(none, ints([0, 0]), 4)
+    assert mask.shape == (0, 1) and depth.shape == (0,)
+    assert sq.kv_keep(cache, none.view(0, 1), none, one, none.view(0, 1), none).shape == (0,)
+    sq.paged_release(none.view(0, 1), 16, none, none, none, ints([0, 0]), one)
+    # drafts without any sequence that has some
+    out = torch.full((3, 8, 128), 7.0, dtype=torch.float16, device=DEV)
+    sq.attn_tree(out.clone(), cache, ints([[0], [1]]), ints([5, 3]), ints([2, 2, 2]), 5, out=out)
+    assert torch.all(out == 7.0)
+
+
+def test_binding_refusals():
+    cache = sq.kv_cache(2, 16, 2)
+    q = torch.zeros((4, 8, 128), dtype=torch.float16, device=DEV)
+    t, lens, cu = ints([[0, 1]]), ints([20]), ints([0, 4])
+    mask = ints([[1], [3], [5], [9]])
+    ok = lambda **k: sq.attn_tree(q, cache, t, lens, cu, 20, **k)  # noqa: E731
+    ok(mask=mask)
+    for bad in (dict(mask=mask[:3]), dict(mask=mask.t()), dict(mask=mask.long()), dict(mask=mask, depth=ints([0, 1])), dict(out=q[:3]),
+                dict(workspace=torch.empty((64, 2), dtype=torch.uint8, device=DEV)[:, 0])):
+        with pytest.raises((TypeError, ValueError)):
+            ok(**bad)
+    for bad in (dict(depth=ints([0, 1, 2, 3])), dict(window=-1), dict(window=1 << 30), dict(scale=float("nan"))):
+        with pytest.raises(sq.SqError):
+            ok(**bad)
+    with pytest.raises(sq.SqError):  # in place
+        ok(out=q)
+    with pytest.raises(ValueError):
+        sq.attn_prompt(q, q[:, :2], q[:, :2], cu, cu, causal=False, window=3)
+    with pytest.raises(ValueError):
+        sq.tree_mask(ints([0, 1]), cu, 4, out=(mask, ints([0, 0])))
+    with pytest.raises(sq.SqError):
+        sq.tree_mask(ints([0, 1, 1, 2]), cu, 4, window=3, sinks=1)
+    with pytest.raises(sq.SqError):
+        sq.kv_keep(cache, t, lens, cu, ints([[0, 1]]), ints([1]), out=lens)
+    with pytest.raises(ValueError):
+        sq.kv_keep(cache, t, lens, cu, ints([[0, 1], [0, 1]]), ints([1]))
+    with pytest.raises(ValueError):
+        sq.paged_grow(lens, lens, ints([1, 1]), t, 16, ints([0, 0]), ints([2]), 4)
+    with pytest.raises(sq.SqError):
+        sq.paged_grow(lens, lens, ints([1]), t, 24, ints([0, 0]), ints([2]), 4)
+
+
+@pytest.mark.parametrize("window,sinks,bits", [(0, 0, 4), (60, 4, 8)])
+def test_a_server_that_drafts(window, sinks, bits):
+    """Prompts, then steps of drafts: pages handed out, masks, the write by depth, attention, a check that keeps some
+    path, its move, and pages given back; each call's input is the one before's output, and each is the oracle's on
+    it.  A token's keys in the cache are, in the end, those of the text written at once."""
+    g = rng(51 + bits)
+    B, Hq, H, page, cols, pages = 3, 8, 2, 16, 14, 60
+    freq = opg.rope_frequencies(128, 10000.0)
+    dfreq = up(freq)
+    cache = sq.kv_cache(pages, page, H, bits)
+    held, pool, count = ints([0] * B), ints(g.permutation(pages)), ints([pages])
+    table = ints(np.full((B, cols), -1))
+    have = ints([0] * B)
+    texts = [np.zeros((0, 2 * H, 128), dtype=np.float16) for _ in range(B)]  # keys and values before positions
+    for step in range(6):
+        new = [int(x) for x in g.integers(20, 90, B)] if step == 0 else [int(x) for x in g.integers(1, 12, B)]
+        T = sum(new)
+        lens, cu, pos, slots, missing = sq.paged_grow(have, ints(new), held, table, page, pool, count, T)
+        assert missing.tolist() == [0, 0]
+        base, bounds = have.tolist(), cu.tolist()
+        parents = sum(([i - 1 for i in range(n)] if step == 0 else tree(g, n, 4) for n in new), [])
+        mask, depth = sq.tree_mask(ints(parents), cu, max(new), lens=lens, window=window, sinks=sinks)
+        sees, want_depth, _ = od.tree_mask(parents, bounds, lens.tolist(), window, sinks, mask.shape[1])
+        assert np.array_equal(mask.cpu().numpy(), od.words_of(sees, mask.shape[1])) and depth.tolist() == list(want_depth)
+        q, kv = heads_of(g, T, Hq), heads_of(g, T, 2 * H)
+        qr = sq.rope_kv_write(up(q), up(kv)[:, :H], up(kv)[:, H:], cache, table, lens, dfreq, cu=cu, depth=depth)
+        # each row's slot holds its value's codes
+        host = {n: t.cpu().numpy() for n, t in zip(("k_q", "v_q", "params"), cache)}
+        codes, a, b = opg.quant_asym(kv[:, H:].astype(np.float32), bits=bits, group=128, clip=1.0, param_fp16=False)
+        for t, s in enumerate(slots.tolist()):
+            assert np.array_equal(host["v_q"][s // page, :, s % page], opg.store_codes(codes[t], bits))
+        out = sq.attn_tree(qr, cache, table, lens, cu, cols * page, mask=mask, depth=depth, window=window, sinks=sinks)
+        want, weight, _ = od.attn_tree(qr.cpu().numpy(), host, bounds, lens.tolist(), table.cpu().numpy(), cols * page, sees, want_depth,
+                                       window, sinks)
+        attention_close(out, want, weight, 2e-5)
+        # the check: a way down from a root, or nothing; prompts are kept whole
+        paths = []
+        for b in range(B):
+            mine = parents[bounds[b]:bounds[b + 1]]
+            end = new[b] - 1 if step == 0 else int(g.integers(-1, new[b]))
+            way = []
+            while end >= 0:
+                way.append(end)
+                end = mine[end]
+            paths.append(way[::-1])
+            texts[b] = np.concatenate([texts[b], kv[[bounds[b] + i for i in paths[b]]]])
+        longest = max(1, max(len(p) for p in paths))
+        have = sq.kv_keep(cache, table, lens, cu, ints([p + [0] * (longest - len(p)) for p in paths]), ints([len(p) for p in paths]))
+        assert have.tolist() == [n + len(p) for n, p in zip(base, paths)]
+        sq.paged_release(table, page, have, ints([2 ** 31 - 1] * B), held, pool, count)
+        assert count.item() == pages - sum(held.tolist()) and held.tolist() == [-(-n // page) for n in have.tolist()]
+    # the same text written in one call
+    total = have.tolist()
+    cu, rows = packed(total), sum(total)
+    kv = up(np.concatenate(texts))
+    again = sq.kv_cache(pages, page, H, bits)
+    sq.rope_kv_write(up(heads_of(g, rows, Hq)), kv[:, :H], kv[:, H:], again, table, have, dfreq, cu=ints(cu))
+    a, b = (sq.kv_read(c, table, have, ints(cu), rows) for c in (cache, again))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_a_captured_step_of_drafts():
+    """A whole step in one graph, replayed while the sequences grow, with eager work between: each replay as eager."""
+    g = rng(61)
+    B, Hq, H, page, cols, pages, n = 2, 8, 2, 16, 20, 60, 6
+    dfreq = up(opg.rope_frequencies(128, 10000.0))
+    T = B * n
+
+    def state():
+        return dict(cache=sq.kv_cache(pages, page, H), held=ints([0] * B), pool=ints(range(pages)), count=ints([pages]),
+                    table=ints(np.full((B, cols), -1)), have=ints([0] * B))
+
+    parents, path, kept, add = ints(np.zeros(T)), ints(np.zeros((B, n))), ints([0] * B), ints([n] * B)
+    qkv = torch.zeros((T, Hq + 2 * H, 128), dtype=torch.float16, device=DEV)
+    ws = torch.empty(sq.attn_tree_workspace_bytes(B, T, cols * page, Hq, H), dtype=torch.uint8, device=DEV)
+    outs = [ints([0] * B), ints([0] * (B + 1)), ints([0] * T), torch.zeros(T, dtype=torch.int64, device=DEV), ints([0, 0])]
+    mask, depth, out = ints(np.zeros((T, 1))), ints([0] * T), torch.empty((T, Hq, 128), dtype=torch.float16, device=DEV)
+    qr, after, far = torch.empty_like(out), ints([0] * B), ints([2 ** 31 - 1] * B)
+
+    def step(s):
+        lens, cu, *_ = sq.paged_grow(s["have"], add, s["held"], s["table"], page, s["pool"], s["count"], T, out=outs)
+        sq.tree_mask(parents, cu, n, out=(mask, depth))
+        sq.rope_kv_write(qkv[:, :Hq], qkv[:, Hq:Hq + H], qkv[:, Hq + H:], s["cache"], s["table"], lens, dfreq, cu=cu, out=qr, depth=depth)
+        sq.attn_tree(qr, s["cache"], s["table"], lens, cu, cols * page, mask=mask, depth=depth, out=out, workspace=ws)
+        sq.kv_keep(s["cache"], s["table"], lens, cu, path, kept, out=after)
+        s["have"].copy_(after)
+        sq.paged_release(s["table"], page, s["have"], far, s["held"], s["pool"], s["count"])
+
+    eager, captured = state(), state()
+    step(state())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured)
+    for turn in range(12):
+        ways = []
+        trees = [tree(g, n, 3) for _ in range(B)]
+        for t in trees:
+            end, way = int(g.integers(0, n)), []
+            while end >= 0:
+                way.append(end)
+                end = t[end]
+            ways.append(way[::-1])
+        parents.copy_(ints(sum(trees, [])))
+        path.copy_(ints([w + [0] * (n - len(w)) for w in ways]))
+        kept.copy_(ints([len(w) for w in ways]))
+        qkv.copy_(up(heads_of(g, T, Hq + 2 * H)))
+        step(eager)
+        want = out.clone()
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), turn
+        for x, y in zip(eager["cache"], captured["cache"]):
+            assert torch.equal(x, y), turn
+        assert all(torch.equal(eager[k], captured[k]) for k in ("held", "pool", "count", "table", "have")), turn
+    assert min(eager["have"].tolist()) > 12
