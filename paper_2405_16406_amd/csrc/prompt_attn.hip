@@ -167,7 +167,8 @@ __device__ __forceinline__ bool prompt_tile(const uint16_t* q, const uint16_t* k
     if (!a.causal) return m - 1;
     uint32_t t, x;
     div_rem(static_cast<uint32_t>(min(r, rows - 1)), a.group, magic_group, t, x);
-    return min(m - pt.n + static_cast<int>(t), m - 1);
+    const int last = min(m - pt.n + static_cast<int>(t), m - 1);
+    return WIN ? max(last, -1) : last;  // (-1 less a window stays in 32 bits)
   };
   const int lim = limit(row);
   const int wave_lo = limit(tile * P::ROWS + 32 * rw), wave_hi = limit(tile * P::ROWS + 32 * rw + 31);
@@ -664,7 +665,7 @@ attn_prompt_combine(const float* part, const int32_t* cu_q, const int32_t* cu_k,
     keys = min(m - n + static_cast<int>(tok) + 1, m);
     if (a.window > 0) {
       div_rem(static_cast<uint32_t>(first), a.group, magic_group, tok, x);
-      keys = token_run(m - n + static_cast<int>(tok), keys, a.window, a.sinks).tokens;
+      keys = token_run(max(m - n + static_cast<int>(tok), -1), keys, a.window, a.sinks).tokens;
     }
   }
   const int tiles = keys > 0 ? (keys + kTile - 1) / kTile : 0;

@@ -489,6 +489,7 @@ def kv_cache(pages: int, page: int, heads: int, bits: int = 4, param_dtype=torch
 # use each property once, and the device is switched only where another one is current.
 _F16, _U8, _I32T, _F64T = torch.float16, torch.uint8, torch.int32, torch.float64
 _current_device = torch._C._cuda_getDevice
+_Tensor = torch.Tensor
 
 
 def _heads(t, name):
@@ -507,11 +508,12 @@ def _heads(t, name):
 
 def _index(t, name, n=None):
     """A contiguous int32 vector (of n entries) on the GPU."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not _I32T or not t.is_cuda:
+    if not isinstance(t, _Tensor) or t.dtype is not _I32T or not t.is_cuda:
         raise TypeError(f"{name} must be a torch.int32 tensor on the GPU")
-    if t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n):
+    shape = t.shape
+    if len(shape) != 1 or not t.is_contiguous() or (n is not None and shape[0] != n):
         raise ValueError(f"{name} must be a contiguous vector" + ("" if n is None else f" of {n} entries"))
-    return t.shape[0]
+    return shape[0]
 
 
 def _cache_args(cache, table, B):
@@ -744,12 +746,14 @@ def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, 
 
 # ------------------------------------------------------------------ drafts and page tables
 
-def _rows_of(t, name, rows, dtype=torch.int32):
-    """Row stride and columns of a 2-D tensor of `rows` rows with unit column stride on the GPU."""
-    _need(t, dtype, name)
-    if t.dim() != 2 or t.shape[0] != rows or (t.stride(1) != 1 and t.shape[1] > 1) or t.shape[1] < 1:
+def _rows_of(t, name, rows):
+    """Row stride and columns of a 2-D int32 tensor of `rows` rows with unit column stride on the GPU."""
+    if not isinstance(t, _Tensor) or t.dtype is not _I32T or not t.is_cuda:
+        raise TypeError(f"{name} must be a torch.int32 tensor on the GPU")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] < 1 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{name} must be [{rows}, columns] with unit column stride")
-    return (t.stride(0) if rows > 1 else t.shape[1]), t.shape[1]
+    return (stride[0] if rows > 1 else shape[1]), shape[1]
 
 
 def tree_mask(parents, cu, most: int, lens=None, window: int = 0, sinks: int = 0, out=None):
@@ -867,7 +871,7 @@ def paged_grow(have, add, held, block_table, page: int, pool, count, rows: int, 
     _index(have, "have", B)
     _index(add, "add", B)
     if out is None:
-        lens, cu, pos, missing = (have.new_empty(n) for n in (B, B + 1, rows, 2))
+        lens, cu, pos, missing = have.new_empty(B), have.new_empty(B + 1), have.new_empty(rows), have.new_empty(2)
         slots = have.new_empty(rows, dtype=torch.int64)
     else:
         lens, cu, pos, slots, missing = out
