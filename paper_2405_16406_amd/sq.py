@@ -520,25 +520,27 @@ def _cache_args(cache, table, B):
     """The cache's arguments: table, its stride and columns, the three tensors, pages, page, heads; and
     (bits, param_bits)."""
     k_q, v_q, params = cache
-    if not (isinstance(k_q, torch.Tensor) and isinstance(v_q, torch.Tensor) and k_q.dtype is v_q.dtype is _U8):
+    if not (isinstance(k_q, _Tensor) and isinstance(v_q, _Tensor) and k_q.dtype is v_q.dtype is _U8):
         raise TypeError("k_q and v_q must be torch.uint8 tensors on the GPU")
-    if not isinstance(params, torch.Tensor) or params.dtype not in _PARAM_BITS:
+    param_bits = _PARAM_BITS.get(params.dtype) if isinstance(params, _Tensor) else None
+    if param_bits is None:
         raise TypeError("params must be a torch.float32 or torch.float16 tensor on the GPU")
-    if not isinstance(table, torch.Tensor) or table.dtype is not _I32T:
+    if not isinstance(table, _Tensor) or table.dtype is not _I32T:
         raise TypeError("block_table must be a torch.int32 tensor on the GPU")
     shape = k_q.shape
-    if len(shape) != 4 or v_q.shape != shape or params.shape != (shape[0], shape[1], shape[2], 4):
+    pages, heads, page, row = shape if len(shape) == 4 else (0, 0, 0, 0)
+    if len(shape) != 4 or v_q.shape != shape or params.shape != (pages, heads, page, 4):
         raise ValueError("the cache is codes [pages, heads, page, bytes] twice and parameters [pages, heads, page, 4]")
     if not (k_q.is_contiguous() and v_q.is_contiguous() and params.is_contiguous()):
         raise ValueError("the cache's tensors must be contiguous")
-    pages, heads, page, row = shape
     if row != 64 and row != 128:
         raise ValueError("a token's codes are 64 (4 bits) or 128 (8 bits) bytes")
-    if table.dim() != 2 or table.shape[0] != B or (table.stride(1) != 1 and table.shape[1] > 1):
+    table_shape, table_stride = table.shape, table.stride()
+    if len(table_shape) != 2 or table_shape[0] != B or (table_stride[1] != 1 and table_shape[1] > 1):
         raise ValueError(f"block_table must be [{B}, blocks] with unit column stride")
-    cols = table.shape[1]
-    return ((table.data_ptr(), table.stride(0) if B > 1 else cols, cols, k_q.data_ptr(), v_q.data_ptr(), params.data_ptr(),
-             pages, page, heads), (row // 16, _PARAM_BITS[params.dtype]))
+    cols = table_shape[1]
+    return ((table.data_ptr(), table_stride[0] if B > 1 else cols, cols, k_q.data_ptr(), v_q.data_ptr(), params.data_ptr(),
+             pages, page, heads), (row // 16, param_bits))
 
 
 def _same_device(t, *others):
@@ -871,7 +873,7 @@ def paged_grow(have, add, held, block_table, page: int, pool, count, rows: int, 
     _index(have, "have", B)
     _index(add, "add", B)
     if out is None:
-        lens, cu, pos, missing = have.new_empty(B), have.new_empty(B + 1), have.new_empty(rows), have.new_empty(2)
+        lens, cu, pos, missing = have.new_empty(2 * B + rows + 3).split((B, B + 1, rows, 2))  # (an allocation each: 1 us)
         slots = have.new_empty(rows, dtype=torch.int64)
     else:
         lens, cu, pos, slots, missing = out
