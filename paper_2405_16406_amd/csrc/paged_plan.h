@@ -62,8 +62,8 @@ inline void paged_split(int64_t B, int64_t max_len, int32_t hq, int32_t hkv, int
   if (chunks < 1) chunks = 1;
 }
 
-// Several rows of a sequence over its pages: workgroups of 16 * rb (row, query head) pairs, `tiles` of them
-// at most, and the tokens that they see in `chunks` pieces of chunk_tokens.
+// Several rows of a sequence over its pages: workgroups of `waves` waves for 16 * rb (row, query head) pairs,
+// `tiles` of them at most, and the tokens that they see in `chunks` pieces of chunk_tokens.
 //   rb: a column of 16 rows, or two that share the expanded codes.  Two need whole columns, and work enough that half
 //   the workgroups still fill the compute units (64 drafts behind 131008 tokens, 32 heads on 8, us: one column 315, two
 //   219; 8 behind 131008 with 8 bits 73 and 65; 16 behind 2048 12.8 and 13.5).
@@ -71,8 +71,12 @@ inline void paged_split(int64_t B, int64_t max_len, int32_t hq, int32_t hkv, int
 //   many pieces do (16 sequences of 4096 tokens, 64 rows, 8 heads: 1024 tokens 26.6, 512 33.6, 2048 30.4).
 //   Windows shorter than the sequences make their runs as good as equal: one round, as of one sequence (64
 //   of 512 .. 8192 tokens in windows of 2048, 8 heads: uncut 33.9, 768 tokens 44.4).
+//   waves: short runs of few workgroups stay uncut, with eight waves each, which spares the join's launch (16
+//   drafts behind L tokens, 4 bits, eager calls and on the device alone, us: L = 512 12.9 and 8.8, cut 16.8 and
+//   10.9; 1024 12.9 and 11.0, cut 17.0 and 11.0; 2048 15.4 and 15.3, cut 17.0 and 13.1; 4096 with 8 bits 28, cut 16).
+constexpr int kWideRun = 5 * kPagedWaves * kPagedBlock;
 struct TreePlan {
-  int32_t rb, tiles, chunks, chunk_tokens;
+  int32_t rb, waves, tiles, chunks, chunk_tokens;
 };
 inline TreePlan tree_plan(int64_t B, int64_t T, bool single, int64_t max_len, int32_t window, int32_t sinks, int32_t hq, int32_t hkv,
                           int cus) {
@@ -98,7 +102,12 @@ inline TreePlan tree_plan(int64_t B, int64_t T, bool single, int64_t max_len, in
   if (chunk < least) chunk = least;
   chunk = (chunk + unit - 1) / unit * unit;
   if (chunk > run) chunk = (run + unit - 1) / unit * unit;
+  p.waves = kPagedWaves;
   p.chunk_tokens = static_cast<int32_t>(chunk < unit ? unit : chunk);
+  if (!two && run > p.chunk_tokens && run <= kWideRun && static_cast<int64_t>(p.tiles) * hkv <= cus) {
+    p.waves = 2 * kPagedWaves;
+    p.chunk_tokens = static_cast<int32_t>((run + 2 * unit - 1) / (2 * unit) * (2 * unit));
+  }
   p.chunks = static_cast<int32_t>((run + p.chunk_tokens - 1) / p.chunk_tokens);
   if (p.chunks < 1) p.chunks = 1;
   return p;

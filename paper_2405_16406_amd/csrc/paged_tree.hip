@@ -4,7 +4,7 @@
 //     mask:   t < base where t > base + depth_i - window or t < sinks, and the drafts base + j of its bits
 //     chain:  t <= base + i with the same window at base + i.
 //
-// A workgroup of kWaves waves serves one (sequence, key/value head, 16 RB of its rows, chunk of the tokens that
+// A workgroup of four or eight waves serves one (sequence, key/value head, 16 RB of its rows, chunk of the tokens that
 // these rows see); its waves take the chunk's blocks of 64 tokens in turn, each on its own.  A block's codes
 // become operands once for all RB columns of 16 rows.  What a row does not see is cut out of the scores by
 // 16 bits a lane, one for each of its tokens, in the blocks alone that some row does not see whole.
@@ -12,8 +12,6 @@
 
 namespace sq {
 namespace {
-
-constexpr int kWaves = kPagedWaves;
 
 // Sequence and tile of rows of the tile number `rem` among ceil(n * group / ROWS) a sequence; seq -1: past the last.
 struct TreeTile {
@@ -484,14 +482,14 @@ struct TreeLds {
   static constexpr int SIGHT = CODES + 7 * kBlock * 4, QUERIES = SIGHT + TreeRows<BITS, RB>::SIGHT * 4;
   static constexpr int BYTES = QUERIES + (RB > 1 ? RB * 4096 : 0);
 };
-template <int BITS, int RB>
+template <int BITS, int RB, int WAVES>
 constexpr int tree_lds() {
-  const int merge = kWaves * 16 * (kDimRow + 2) * 4, codes = kWaves * TreeLds<BITS, RB>::BYTES;
+  const int merge = WAVES * 16 * (kDimRow + 2) * 4, codes = WAVES * TreeLds<BITS, RB>::BYTES;
   return merge > codes ? merge : codes;
 }
 
-template <int BITS, bool P16, int RB>
-__global__ void __launch_bounds__(64 * kWaves, 2)
+template <int BITS, bool P16, int RB, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2)
 attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32_t magic_tiles, uint32_t magic_heads,
                uint32_t magic_group, TreeArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -540,7 +538,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     par = token_params<P16>(a.cache, token_slot(a.cache, safe, p.hk, t0 + lane));
   };
 
-  const int step = kWaves * kBlock;
+  const int step = WAVES * kBlock;
   int v0 = p.first + w * kBlock;
   int32_t entry = -1;
   if (v0 < p.last) {
@@ -596,7 +594,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
 
   // the waves' states of 16 rows at a time meet in LDS
   float* const red = reinterpret_cast<float*>(lds);   // [wave][row][kDimRow]
-  float* const red_ml = red + kWaves * 16 * kDimRow;  // [wave][row][2]
+  float* const red_ml = red + WAVES * 16 * kDimRow;  // [wave][row][2]
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     r.finish(rb);
@@ -615,15 +613,15 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
       *reinterpret_cast<v4f*>(red + (w * 16 + i) * kDimRow + 16 * dt + 4 * g) = o;
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < left * 32; x += 64 * kWaves) {
+    for (int x = threadIdx.x; x < left * 32; x += 64 * WAVES) {
       const int rr = x >> 5, d = 4 * (x & 31);
       float M = -INFINITY;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) M = fmaxf(M, red_ml[(v * 16 + rr) * 2]);
+      for (int v = 0; v < WAVES; ++v) M = fmaxf(M, red_ml[(v * 16 + rr) * 2]);
       float L = 0.0f;
       v4f D = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
+      for (int v = 0; v < WAVES; ++v) {
         const float f = rescale(red_ml[(v * 16 + rr) * 2], M);
         L = __fmaf_rn(red_ml[(v * 16 + rr) * 2 + 1], f, L);
         const v4f o = *reinterpret_cast<const v4f*>(red + (v * 16 + rr) * kDimRow + d);
@@ -707,27 +705,29 @@ attn_tree_combine(const float* part, const int32_t* cu, const int32_t* lens, int
       M == -INFINITY ? 0u : f2h2(__fdiv_rn(D0, L), __fdiv_rn(D1, L));
 }
 
-template <int BITS, bool P16, int RB>
+template <int BITS, bool P16, int RB, int WAVES>
 hipError_t launch_part(const TreeArgs& a, hipStream_t stream) {
-  constexpr auto kern = attn_tree_part<BITS, P16, RB>;
-  constexpr int lds = tree_lds<BITS, RB>();
+  constexpr auto kern = attn_tree_part<BITS, P16, RB, WAVES>;
+  constexpr int lds = tree_lds<BITS, RB, WAVES>();
   const hipError_t init = set_max_lds<kern>(lds);
   if (init != hipSuccess) return init;
   const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.plan.tiles) * a.cache.heads * a.plan.chunks);
-  return launch(kern, dim3(blocks), dim3(64 * kWaves), lds, stream, a.q, a.cu, a.lens, div_magic(static_cast<uint32_t>(a.plan.tiles)),
+  return launch(kern, dim3(blocks), dim3(64 * WAVES), lds, stream, a.q, a.cu, a.lens, div_magic(static_cast<uint32_t>(a.plan.tiles)),
                 div_magic(static_cast<uint32_t>(a.cache.heads)), div_magic(static_cast<uint32_t>(a.group)), a);
 }
 
-template <int RB>
+template <int RB, int WAVES>
 hipError_t launch_parts(const TreeArgs& a, hipStream_t stream) {
-  if (a.bits == 8) return a.param16 ? launch_part<8, true, RB>(a, stream) : launch_part<8, false, RB>(a, stream);
-  return a.param16 ? launch_part<4, true, RB>(a, stream) : launch_part<4, false, RB>(a, stream);
+  if (a.bits == 8) return a.param16 ? launch_part<8, true, RB, WAVES>(a, stream) : launch_part<8, false, RB, WAVES>(a, stream);
+  return a.param16 ? launch_part<4, true, RB, WAVES>(a, stream) : launch_part<4, false, RB, WAVES>(a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_attn_tree(const TreeArgs& a, hipStream_t stream) {
-  const hipError_t e = a.plan.rb == 2 ? launch_parts<2>(a, stream) : launch_parts<1>(a, stream);
+  const hipError_t e = a.plan.rb == 2                  ? launch_parts<2, kPagedWaves>(a, stream)
+                       : a.plan.waves > kPagedWaves ? launch_parts<1, 2 * kPagedWaves>(a, stream)
+                                                    : launch_parts<1, kPagedWaves>(a, stream);
   if (e != hipSuccess || a.plan.chunks == 1) return e;
   const auto join = [&](auto kern, int waves) {
     return launch(kern, dim3(static_cast<unsigned>(a.T * a.hq)), dim3(64 * waves), 0, stream, a.part, a.cu, a.lens, a.B, a.out, a.ldo,

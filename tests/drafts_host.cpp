@@ -21,4 +21,8 @@ void tree_plan(int64_t B, int64_t T, int32_t single, int64_t max_len, int32_t wi
   out[2] = p.chunks;
   out[3] = p.chunk_tokens;
 }
+
+int32_t tree_waves(int64_t B, int64_t T, int32_t single, int64_t max_len, int32_t window, int32_t sinks, int32_t hq, int32_t hkv, int cus) {
+  return sq::tree_plan(B, T, single != 0, max_len, window, sinks, hq, hkv, cus).waves;
+}
 }

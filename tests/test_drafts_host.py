@@ -124,6 +124,31 @@ def test_every_form_is_tested(host):
     assert {c for _, r, c in forms if r == 2} >= {"few"}
 
 
+def test_every_kernel_is_tested(host):
+    """Codes, parameters, columns and waves of the kernels that those sizes reach, and whether their runs are cut."""
+    t = pytest.importorskip("test_gpu_tree")
+    forms = set()
+    for hq, h, _, bits, params, new, past, window, sinks in t.ATTN:
+        args = (len(new), sum(new) + 3, max(n + p for n, p in zip(new, past)), window, sinks, hq, h)
+        rb, _, chunks, _ = plan_of(host, *args)
+        waves = host.tree_waves(I64(args[0]), I64(args[1]), 0, I64(args[2]), *args[3:], 256)
+        forms.add((bits, np.dtype(params).itemsize, rb, waves, chunks > 1))
+    for bits in (4, 8):
+        for size in (2, 4):
+            assert {f[2:] for f in forms if f[:2] == (bits, size)} >= {(1, 4, True), (1, 8, False), (2, 4, True)}, (bits, size)
+
+
+def test_short_runs_of_few_workgroups_stay_uncut(host):
+    def waves(B, T, run, single=0, hq=32, hkv=8, cus=256):
+        plan = plan_of(host, B, T, run, hq=hq, hkv=hkv, single=bool(single), cus=cus)
+        w = host.tree_waves(I64(B), I64(T), single, I64(run), 0, 0, hq, hkv, cus)
+        assert w in (4, 8) and plan[3] % (64 * w) == 0 and plan[2] * plan[3] >= run and (w == 4 or (plan[0] == 1 and plan[2] == 1))
+        return w
+    assert [waves(1, 16, n) for n in (1, 256, 257, 1280, 1281, 2 ** 30 - 1)] == [4, 4, 8, 8, 4, 4]
+    assert [waves(n, n, 1000, 1) for n in (1, 32, 33, 64)] == [8, 8, 4, 4]  # a workgroup for each compute unit
+    assert waves(1, 64, 1200, cus=64) == 4
+
+
 # ------------------------------------------------------------------ the oracle
 
 def test_oracle_of_a_chain_is_causal_attention():

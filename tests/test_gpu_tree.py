@@ -147,6 +147,13 @@ ATTN = [  # Hq, Hkv, page, bits, params, drafts, tokens before, window, sinks
     (64, 8, 16, 8, np.float16, [16, 7], [900, 600], 500, 20),
     (36, 12, 16, 4, np.float32, [11, 6, 23], [1200, 800, 5], 700, 3),      # rows across columns
     (8, 2, 16, 4, np.float32, [9], [7000], 0, 0),                          # many chunks
+    (8, 2, 16, 4, np.float16, [6, 3], [600, 1000], 0, 0),                  # eight waves
+    (16, 4, 32, 8, np.float32, [12, 2], [950, 300], 0, 0),
+    (8, 1, 16, 4, np.float32, [20, 1], [1255, 0], 0, 0),
+    (8, 2, 16, 8, np.float32, [5], [2500], 0, 0),                          # one column, a few chunks
+    (8, 2, 32, 8, np.float16, [3, 8], [1700, 100], 0, 0),
+    (8, 2, 16, 4, np.float16, [4, 1], [3000, 1500], 0, 0),
+    (64, 8, 16, 8, np.float16, [33, 20], [900, 1400], 0, 0),               # two columns
 ]
 
 
