@@ -5,6 +5,11 @@
 // paged_release and paged_grow run in one workgroup, since the place of a page in the pool is a sum over all
 // sequences before it.  Sequences come in batches of one for each thread; a batch's sums (a scan) stay in
 // LDS, and its pages, or rows, are then taken evenly by the threads, each finding its sequence by halving.
+//
+// Measured on the device, us (an empty kernel takes 2): release 3.8 for 8 sequences, 7.7 for 256 of which 64 end;
+// grow 4.8 and 6.2; the 36 000 rows of the latter step 4.4; masks of 8 and 16 trees 2.9 and 4.9;
+// the accepted drafts of one sequence 3.2, of 64 sequences of 8 heads 3.3.  Eager calls wait for the host: 8 us for
+// one, 17 for the three of a step's tables.
 #include "paged_device.h"
 #include "sq_internal.h"
 

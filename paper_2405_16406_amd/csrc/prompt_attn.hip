@@ -36,6 +36,12 @@
 //
 // Few rows over many keys (a follow-up question on a long document) would leave most of the chip
 // idle: the keys are then split over workgroups, whose fp32 states a second kernel joins.
+//
+// With a window a workgroup walks the tiles of its rows' run alone.  8192 tokens of 32 heads on 8 with windows of 1024
+// take 172 us (129 GFLOP, 0.75 PFLOP/s; matrix cores busy for 41 % of the cycles), six chunks of 500 .. 1500 tokens of 32
+// heads behind up to 2500 with windows of 777 128 us (0.54).  A run is some 18 and 14 tiles, and what a workgroup does
+// once weighs as in a short prompt.  Masks no longer show: with every tile taken as whole, and wrong results, the two
+// took as long.
 #include "paged_device.h"
 #include "paged_plan.h"
 #include "sq_internal.h"
