@@ -9,16 +9,16 @@
 // become operands once for all RB columns of 16 rows.  What a row does not see is cut out of the scores by
 // 16 bits a lane, one for each of its tokens, in the blocks alone that some row does not see whole.
 //
-// Many rows: vector instructions bound it.  64 drafts of 32 heads on 8 behind 131008 tokens of 4 bits take 206 us with
-// the join (137 GFLOP, 0.67 PFLOP/s of the 1.49 that a large library product reaches; the cache's 150 MB alone would
+// Many rows: vector instructions bound it.  64 drafts of 32 heads on 8 behind 131008 tokens of 4 bits take 200 us with
+// the join (137 GFLOP, 0.69 PFLOP/s of the 1.49 that a large library product reaches; the cache's 150 MB alone would
 // take 30): 626 vector operations for 64 tokens and two columns, a quarter of them the codes' expansion, half the
-// softmax, keep the vector units in use for 76 % of the kernel's cycles (90 % of those in which its waves live), the
-// matrix cores for 28 %.  58 operations less (value codes by conversions from 8-bit floats, no maximum of the scores
-// but one of the rounded weights) left the time as it was.  More rows on an expansion: four columns a wave need 512
-// registers and spilled (413 us, two columns then 227); workgroups of 128 rows that share the operands through LDS took
-// 213 then, and 107 with 16 sequences of 524 .. 8224 tokens, 64 heads on 8, where two columns a wave took 70 (62 now).
-// Few rows: memory.  64 sequences' windows of 2048 tokens, 115 MB, 34 us with the join (3.4 TB/s); 4 drafts behind
-// those 131008 tokens 38.  Short runs: two launches and their chains to memory (16 drafts behind 2048 tokens 10 us, join 4).
+// softmax, keep the vector units in use for 80 % of the kernel's cycles, the matrix cores for 29 %.  More rows on an
+// expansion: four columns a wave need 512 registers and spilled (413 us, two columns then 227); workgroups of 128 rows
+// that share the operands through LDS took 213 then, and 107 with 16 sequences of 524 .. 8224 tokens, 64 heads on 8,
+// where two columns a wave took 70 (62 now).
+// Few rows: memory.  64 sequences' windows of 2048 tokens, 115 MB, 33 us (3.5 TB/s); 4 drafts behind those 131008
+// tokens 38 with the join.  Short runs: two launches and their chains to memory (16 drafts behind 2048 tokens 10 us,
+// the join 4).
 #include "paged_attn_device.h"
 
 namespace sq {
@@ -556,7 +556,15 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     load(v0, entry_of(a, p, v0));
     entry = entry_of(a, p, v0 + step);
   }
+  // Of a SIMD's two waves the older would be served first, and the other be left alone at the end: they take turns, by
+  // the place that the machine gave them (64 drafts behind 131008 tokens: 231 -> 223 us, waves alive for 92 % of the
+  // cycles instead of 85).
+  uint32_t turn = __builtin_amdgcn_s_getreg(4 | 0 << 6 | 3 << 11);  // bits 0 .. 3 of HW_ID: the wave's place in its SIMD
   for (; v0 < p.last; v0 += step) {
+    if (turn++ & 1)
+      __builtin_amdgcn_s_setprio(1);
+    else
+      __builtin_amdgcn_s_setprio(0);
     // codes and coefficients to LDS (this wave's own: no barrier, its LDS operations are in order)
 #pragma unroll
     for (int mm = 0; mm < 4; ++mm)
@@ -602,6 +610,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     }
     asm volatile("" ::: "memory");
   }
+  __builtin_amdgcn_s_setprio(0);
 
   // the waves' states of 16 rows at a time meet in LDS
   float* const red = reinterpret_cast<float*>(lds);   // [wave][row][kDimRow]
