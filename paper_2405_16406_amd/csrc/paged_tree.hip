@@ -11,7 +11,7 @@
 //
 // Many rows: vector instructions bound it.  64 drafts of 32 heads on 8 behind 131008 tokens of 4 bits take 200 us with
 // the join (137 GFLOP, 0.69 PFLOP/s of the 1.49 that a large library product reaches; the cache's 150 MB alone would
-// take 30): 626 vector operations for 64 tokens and two columns, a quarter of them the codes' expansion, half the
+// take 30): 594 vector operations for 64 tokens and two columns, a quarter of them the codes' expansion, half the
 // softmax, keep the vector units in use for 80 % of the kernel's cycles, the matrix cores for 29 %.  More rows on an
 // expansion: four columns a wave need 512 registers and spilled (413 us, two columns then 227); workgroups of 128 rows
 // that share the operands through LDS took 213 then, and 107 with 16 sequences of 524 .. 8224 tokens, 64 heads on 8,
@@ -182,6 +182,13 @@ __device__ __forceinline__ void key_operands(const v4u (&k)[KW], v8h (&ko)[4]) {
   }
 }
 
+// Two of four codes of 4 bits, a byte each, as the numbers normal() makes: n is the 8-bit float (e4m3) of n 2^-9, and its
+// conversion exact, a mask and a product less for a pair (64 drafts behind 131008 tokens: 225 -> 219 us).
+template <bool HIGH>
+__device__ __forceinline__ uint32_t normal_pair(uint32_t bytes) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(bytes), 1.0f, HIGH));
+}
+
 // Value codes of a block in LDS, a token's 16 bytes apart from the next one's (so that a read's place is one register
 // and a constant; paged_attn.hip's exchanged units would take a register for each): dims 16 dt + i of the lane's 16
 // tokens as two operands.
@@ -196,8 +203,8 @@ __device__ __forceinline__ void value_operands(const uint8_t* codes, int dt, v8h
     const v2i c2 = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i)(uintptr_t)(codes + row * kPitch<BITS> + 8 * dt));
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const uint32_t u = static_cast<uint32_t>(c2[x]), u8 = u >> 8;
-      vo[x] = operand(normal(u & 0x000F000Fu, 0), normal(u & 0x00F000F0u, 4), normal(u8 & 0x000F000Fu, 0), normal(u8 & 0x00F000F0u, 4));
+      const uint32_t even = static_cast<uint32_t>(c2[x]) & 0x0F0F0F0Fu, odd = (static_cast<uint32_t>(c2[x]) >> 4) & 0x0F0F0F0Fu;
+      vo[x] = operand(normal_pair<false>(even), normal_pair<true>(even), normal_pair<false>(odd), normal_pair<true>(odd));
     }
   } else {
 #pragma unroll
@@ -422,8 +429,8 @@ struct TreeRows {
       const float fv[8] = {cv0.x, cv0.y, cv0.z, cv0.w, cv1.x, cv1.y, cv1.z, cv1.w};
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        // pairs of tokens: 4 bits (0, 4), (1, 5), (2, 6), (3, 7); 8 bits (0, 2), (1, 3), ..
-        const int ta = BITS == 4 ? y : 4 * (y >> 1) + (y & 1), tb = ta + (BITS == 4 ? 4 : 2);
+        // pairs of tokens: 4 bits (0, 2), (4, 6), (1, 3), (5, 7); 8 bits (0, 2), (1, 3), ..
+        const int ta = BITS == 4 ? 4 * (y & 1) + (y >> 1) : 4 * (y >> 1) + (y & 1), tb = ta + 2;
         const uint32_t p2 = f2h2(exp2_fast(s[8 * x + ta] - from), exp2_fast(s[8 * x + tb] - from));
         pw[4 * x + y] = p2;
         const v2h ph = __builtin_bit_cast(v2h, p2);
