@@ -552,8 +552,9 @@ sq_status sq_attn_prompt_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq
  *   mask       device int32 [T, ld_mask], the first `words` words of a row written: bit j % 32 of word
  *              j / 32 of draft i is 1 where j is i or an ancestor that i sees.  Drafts from 32 * words on
  *              have no bits.
- *   words, ld_mask  1 <= words <= 2^16, words <= ld_mask < 2^24
+ *   words, ld_mask  1 <= words <= 2^9, words <= ld_mask < 2^24
  *   depth      device int32 [T]
+ * A sequence's drafts from 2^14 on get depth 0 and no bits.
  * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_ALIGN (4 bytes each), SQ_ERR_ALIAS, SQ_ERR_HIP.
  */
 sq_status sq_tree_mask(const int32_t* parents, const int32_t* cu, const int32_t* lens, int64_t B, int64_t T,
@@ -593,7 +594,7 @@ sq_status sq_rope_kv_write_ex(const void* q, int64_t ldq, const void* k, int64_t
  *              of no sequence, and rows with base + i < 0, are left as they were in out.
  *   mask       device int32 [T, ld_mask] or NULL, as sq_tree_mask writes it (any bits are fine: a row need
  *              not see itself); drafts from 32 * words on are seen by none
- *   words, ld_mask  as in sq_tree_mask (ignored without mask)
+ *   words, ld_mask  1 <= words <= 2^16, words <= ld_mask < 2^24 (ignored without mask)
  *   depth      device int32 [T] or NULL (depth i in row i; must be NULL without mask); read with window > 0
  *              alone, and taken as 0 below 0 and as 2^30 above
  *   T          >= 0, T * Hq + B * Hq < 2^24 (T == 0 or B == 0 is a no-op)

@@ -242,38 +242,40 @@ paged_rows(PoolArgs p, GrowArgs g) {
   g.slots[t] = slot;
 }
 
-// A workgroup per sequence, a thread per draft: up the tree by the parents, which lie in LDS where they fit.
+// A workgroup per sequence, a thread per draft: up the tree by the parents, which lie in LDS.  The way up is as long as
+// the draft is deep, so a sequence has kMaskDrafts of them at most; those behind are written down as unseeing.
 constexpr int kMaskThreads = 128;
-constexpr int kMaskParents = 4096;
 
 __global__ void __launch_bounds__(kMaskThreads)
 tree_mask(const int32_t* parents, const int32_t* cu, const int32_t* lens, int64_t b_first, TreeMaskArgs a) {
-  __shared__ int32_t near[kMaskParents];
+  __shared__ int16_t up[kMaskDrafts];  // -1: a root
   const int64_t b = b_first + blockIdx.x;
   const int most = static_cast<int>(a.T);
-  const int q0 = min(max(cu[b], 0), most), n = max(min(cu[b + 1], most) - q0, 0);
-  const int base = lens ? min(max(lens[b], 0), (1 << 30) - 1) - n : 0;
-  const int32_t* const far = parents + q0;
-  for (int i = threadIdx.x; i < min(n, kMaskParents); i += kMaskThreads) near[i] = far[i];
+  const int q0 = min(max(cu[b], 0), most), all = max(min(cu[b + 1], most) - q0, 0), n = min(all, kMaskDrafts);
+  const int base = lens ? min(max(lens[b], 0), (1 << 30) - 1) - all : 0;
+  for (int i = threadIdx.x; i < n; i += kMaskThreads) {
+    const int p = parents[q0 + i];
+    up[i] = static_cast<int16_t>(p >= 0 && p < i ? p : -1);
+  }
   __syncthreads();
-  const auto up = [&](int i) {  // -1: a root
-    const int p = i < kMaskParents ? near[i] : far[i];
-    return p >= 0 && p < i ? p : -1;
-  };
   for (int i = threadIdx.x; i < n; i += kMaskThreads) {
     int depth = 0;
-    for (int j = up(i); j >= 0; j = up(j)) ++depth;
+    for (int j = up[i]; j >= 0; j = up[j]) ++depth;
     a.depth[q0 + i] = depth;
     int32_t* const row = a.mask + static_cast<int64_t>(q0 + i) * a.ldm;
     int j = i, d = depth;
     // two words at a time, from the last that has a bit down: parents come before their children
     for (int pair = (a.words - 1) / 2; pair >= 0; --pair) {
       uint64_t bits = 0;
-      for (; j >= 64 * pair; j = up(j), --d)
+      for (; j >= 64 * pair; j = up[j], --d)
         if (j < 64 * (pair + 1) && (a.window == 0 || depth - d < a.window || base + d < a.sinks)) bits |= uint64_t{1} << (j - 64 * pair);
       row[2 * pair] = static_cast<int32_t>(bits);
       if (2 * pair + 1 < a.words) row[2 * pair + 1] = static_cast<int32_t>(bits >> 32);
     }
+  }
+  for (int64_t i = n + static_cast<int64_t>(threadIdx.x); i < all; i += kMaskThreads) {
+    a.depth[q0 + i] = 0;
+    for (int x = 0; x < a.words; ++x) a.mask[(q0 + i) * a.ldm + x] = 0;
   }
 }
 

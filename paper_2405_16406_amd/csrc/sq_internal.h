@@ -256,6 +256,7 @@ struct TreeArgs {
 };
 hipError_t launch_attn_tree(const TreeArgs& a, hipStream_t stream);
 
+constexpr int kMaskDrafts = 1 << 14;  // of a sequence, that sq_tree_mask goes up from
 struct TreeMaskArgs {
   const int32_t* parents;  // [T]
   const int32_t* cu;       // [B + 1]

@@ -122,6 +122,7 @@ sq_status sq_tree_mask(const int32_t* parents, const int32_t* cu, const int32_t*
   if (!parents || !cu || !mask || !depth) return fail(SQ_ERR_NULL, "parents, cu, mask and depth are required");
   sq_status s = check_window(window, sinks);
   if (s != SQ_OK || (s = check_words(words, ld_mask)) != SQ_OK) return s;
+  if (words > sq::kMaskDrafts / 32) return fail(SQ_ERR_SHAPE, "words=%lld: a sequence has at most 2^14 drafts", (long long)words);
   const bool first = window > 0 && sinks > 0;
   if (first && !lens) return fail(SQ_ERR_NULL, "lens is required with window and sinks");
   if (B < 0 || T < 0 || B > kMost32 || T > kMost32) return fail(SQ_ERR_SHAPE, "B=%lld or T=%lld out of range", (long long)B, (long long)T);

@@ -761,8 +761,9 @@ def _rows_of(t, name, rows):
 def tree_mask(parents, cu, most: int, lens=None, window: int = 0, sinks: int = 0, out=None):
     """What each draft of a tree sees of the drafts, from their parents (sq_tree_mask): parents int32 [T],
     indexes within the sequence (-1: a root), cu int32 [B + 1], most: at least the drafts of any
-    sequence; lens int32 [B], drafts included, needed with window and sinks.  Returns (mask int32
-    [T, ceil(most / 32)], depth int32 [T]); out: that pair.  Rows of no sequence are left as they are."""
+    sequence, 2^14 of them at most; lens int32 [B], drafts included, needed with window and sinks.
+    Returns (mask int32 [T, ceil(most / 32)], depth int32 [T]); out: that pair.  Rows of no sequence are
+    left as they are."""
     T = _index(parents, "parents")
     B = _index(cu, "cu") - 1
     if lens is not None:

@@ -91,6 +91,11 @@ def test_tree_mask_refusals(L):  # noqa: F811
         assert mask(L, **kw) == sq.SQ_OK, kw
 
 
+def test_tree_mask_refuses_more_words_than_it_writes(L):  # noqa: F811
+    assert mask(L, T=0, words=1 << 9, ldm=1 << 9) == sq.SQ_OK
+    assert mask(L, T=0, words=(1 << 9) + 1, ldm=1 << 10) == sq.SQ_ERR_SHAPE
+
+
 def test_write_refusals(L):  # noqa: F811
     assert write_ex(L, depth=fake(13, 2)) == sq.SQ_ERR_ALIGN
     assert write_ex(L, qr=fake(13)) == write_ex(L, kr=fake(13)) == sq.SQ_ERR_ALIAS

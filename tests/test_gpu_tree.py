@@ -73,6 +73,28 @@ def test_tree_mask_of_a_long_chain():
     assert np.array_equal(bits, np.tril(np.ones((n, n), dtype=np.uint8)))
 
 
+def test_tree_mask_of_more_drafts_than_it_goes_up_from():
+    """Drafts from 2^14 on have depth 0 and no bits; those before have all that there is."""
+    n = (1 << 14) + 150
+    mask, depth = sq.tree_mask(ints([-1] + [0] * 39 + [i - 1 for i in range(40, n)]), ints([0, n]), 64)
+    want = np.minimum(np.arange(n), 1)
+    want[40:] = np.arange(40, n) - 38
+    want[1 << 14:] = 0
+    assert np.array_equal(depth.cpu().numpy(), want)
+    bits = np.unpackbits(mask.cpu().numpy().view(np.uint8), axis=1, bitorder="little")
+    sees = np.zeros((n, 64), dtype=np.uint8)
+    sees[:, 0] = sees[40:, 39] = 1
+    for i in range(1, 39):
+        sees[i, i] = 1
+    sees[39, 39] = 1
+    for i in range(40, n):
+        sees[i, 40:min(i, 63) + 1] = 1
+    sees[1 << 14:] = 0
+    assert np.array_equal(bits, sees)
+    with pytest.raises(sq.SqError):
+        sq.tree_mask(ints([-1]), ints([0, 1]), (1 << 14) + 1)
+
+
 WRITE = [  # Hq, Hkv, page, bits, params, rotary, interleaved, drafts, tokens before
     (8, 2, 16, 4, np.float32, 128, False, [5, 1, 40], [11, 0, 100]),
     (4, 4, 64, 8, np.float16, 96, True, [33], [70]),
