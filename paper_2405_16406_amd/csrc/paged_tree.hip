@@ -16,7 +16,8 @@
 // expansion: four columns a wave need 512 registers and spilled (413 us, two columns then 227); workgroups of 128 rows
 // that share the operands through LDS took 213 then, and 107 with 16 sequences of 524 .. 8224 tokens, 64 heads on 8,
 // where two columns a wave took 70 (62 now).
-// Few rows: memory.  64 sequences' windows of 2048 tokens, 115 MB, 33 us (3.5 TB/s); 4 drafts behind those 131008
+// Few rows: memory.  64 sequences' windows of 2048 tokens, 115 MB, 31 us (3.7 TB/s; three waves a SIMD, which spill four
+// registers, 41, and 50 with workgroups of six); 4 drafts behind those 131008
 // tokens 38 with the join.  Short runs: two launches and their chains to memory (16 drafts behind 2048 tokens 10 us,
 // the join 4).
 #include "paged_attn_device.h"
@@ -531,37 +532,44 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
       for (int x = 0; x < 4; ++x) qlds[(4 * rb + x) * 64 + lane] = r.qf[rb][x];
   }
 
+  // One column of 4 bits waits for memory more than for arithmetic, so the next block's values are asked for as soon as
+  // this one's lie in LDS (64 sequences' windows of 2048 tokens: 32.4 -> 31.1 us; its keys as well, in registers of
+  // their own: 32.2; two columns behind 131008 tokens 200 -> 209, one of 8 bits 33.9 -> 34.1).
+  constexpr bool EARLY = RB == 1 && BITS == 4;
   constexpr int KW = BITS == 4 ? 1 : 2;  // 16-byte loads of a lane's key codes
   v4u kc[4][KW], vc[4][KW];
   float4 par;
   bool par_ok;
   // tokens without a page, or past the chunk, read page 0 and have no weight
-  auto load = [&](int v0, int32_t entry) __attribute__((always_inline)) {
+  int64_t at[4];  // first codes of the 16 tokens of group j, which lie in one page
+  auto load_values = [&](int v0, int32_t entry) __attribute__((always_inline)) {
     const int t0 = p.run.position(v0);
     const int32_t mine = valid_page(a.cache, entry), safe = max(mine, 0);
     par_ok = mine >= 0 && v0 + lane < p.last;
-    // load j brings the 16 tokens of group j, which lie in one page: keys of token i from its byte 16 g (32 g) on, values
-    // in order, four (eight) lanes a token
+    // load j brings group j's: values in order, four (eight) lanes a token
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int64_t at = token_slot(a.cache, __builtin_amdgcn_readlane(safe, 16 * j), p.hk, t0 + 16 * j) * ROW;
-      const uint8_t* const kp = a.cache.kq + at;
-      const uint8_t* const vp = a.cache.vq + at;
+      at[j] = token_slot(a.cache, __builtin_amdgcn_readlane(safe, 16 * j), p.hk, t0 + 16 * j) * ROW;
 #pragma unroll
-      for (int x = 0; x < KW; ++x) {
-        kc[j][x] = *reinterpret_cast<const v4u*>(kp + static_cast<uint32_t>(i * ROW + (BITS == 4 ? 16 : 32) * g + 16 * x));
-        vc[j][x] = *reinterpret_cast<const v4u*>(vp + static_cast<uint32_t>(16 * lane + 1024 * x));
-      }
+      for (int x = 0; x < KW; ++x) vc[j][x] = *reinterpret_cast<const v4u*>(a.cache.vq + at[j] + static_cast<uint32_t>(16 * lane + 1024 * x));
     }
     par = token_params<P16>(a.cache, token_slot(a.cache, safe, p.hk, t0 + lane));
+  };
+  auto load_keys = [&]() __attribute__((always_inline)) {  // of the same block: token i's from its byte 16 g (32 g) on
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 0; x < KW; ++x)
+        kc[j][x] = *reinterpret_cast<const v4u*>(a.cache.kq + at[j] + static_cast<uint32_t>(i * ROW + (BITS == 4 ? 16 : 32) * g + 16 * x));
   };
 
   const int step = WAVES * kBlock;
   int v0 = p.first + w * kBlock;
   int32_t entry = -1;
   if (v0 < p.last) {
-    load(v0, entry_of(a, p, v0));
     entry = entry_of(a, p, v0 + step);
+    load_values(v0, entry_of(a, p, v0));
+    load_keys();
   }
   // Of a SIMD's two waves the older would be served first, and the other be left alone at the end: they take turns, by
   // the place that the machine gave them (64 drafts behind 131008 tokens: 231 -> 223 us, waves alive for 92 % of the
@@ -583,6 +591,15 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
     const uint64_t there = __ballot(par_ok);
     const uint64_t odd = token_coefs(par, par_ok, a.scale_log2e, r.down, coef);
     asm volatile("" ::: "memory");
+    const bool more = v0 + step < p.last;
+    if constexpr (EARLY) {
+      if (more) {
+        const int32_t next = entry;
+        entry = entry_of(a, p, v0 + 2 * step);
+        load_values(v0 + step, next);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     if constexpr (RB > 1) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
@@ -597,12 +614,12 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
       r.scores(j, ko, coef, s);
       if constexpr (RB > 1 && BITS == 4) __builtin_amdgcn_sched_barrier(0);
     }
-    // the next block's codes, when the registers of this one's are free (asked for before the scores they cost
-    // a spill, and its way through memory, with two columns)
+    // the next block's codes, when the registers of this one's are free
     __builtin_amdgcn_sched_barrier(0);
-    if (v0 + step < p.last) {
-      load(v0 + step, entry);
-      entry = entry_of(a, p, v0 + 2 * step);
+    if (more) {
+      if constexpr (!EARLY) load_values(v0 + step, entry);
+      load_keys();
+      if constexpr (!EARLY) entry = entry_of(a, p, v0 + 2 * step);
     }
     r.hide(p.run.position(v0), there, odd, coef, a, p, s);
     r.move(s);
