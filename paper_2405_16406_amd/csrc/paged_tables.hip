@@ -7,7 +7,7 @@
 // LDS, and its pages, or rows, are then taken evenly by the threads, each finding its sequence by halving.
 //
 // Measured on the device, us (an empty kernel takes 2): release 3.8 for 8 sequences, 7.7 for 256 of which 64 end;
-// grow 4.8 and 6.2; the 36 000 rows of the latter step 4.4; masks of 8 and 16 trees 2.9 and 4.9;
+// grow 4.8 and 6.2; the 36 000 rows of the latter step 4.4; masks of 8 and 16 trees 2.5 and 5.1;
 // the accepted drafts of one sequence 3.2, of 64 sequences of 8 heads 3.3.  Eager calls wait for the host: 8 us for
 // one, 17 for the three of a step's tables.
 #include "paged_device.h"
