@@ -38,10 +38,12 @@
 // idle: the keys are then split over workgroups, whose fp32 states a second kernel joins.
 //
 // With a window a workgroup walks the tiles of its rows' run alone.  8192 tokens of 32 heads on 8 with windows of 1024
-// take 172 us (129 GFLOP, 0.75 PFLOP/s; matrix cores busy for 41 % of the cycles), six chunks of 500 .. 1500 tokens of 32
-// heads behind up to 2500 with windows of 777 128 us (0.54).  A run is some 18 and 14 tiles, and what a workgroup does
-// once weighs as in a short prompt.  Masks no longer show: with every tile taken as whole, and wrong results, the two
-// took as long.
+// take 157 .. 164 us (129 GFLOP, 0.8 PFLOP/s; matrix cores busy for 45 % of the cycles), six chunks of 500 .. 1500 tokens
+// of 32 heads behind up to 2500 with windows of 777 115 .. 125 us (0.6).  A run is some 18 tiles, and what a workgroup
+// does once weighs as in a short prompt: of 43 us 0.6 go to find its place, 1.4 to the queries' addresses, 1.9 to the
+// first tile, 2.7 to the end (before rows went out whole), and 4 .. 6 pass until the next one starts.  One workgroup a
+// compute unit that takes tiles in turn was 1 % quicker for one prompt and up to 14 % slower for several.  Masks do not
+// show: with every tile taken as whole, and wrong results, the two took as long.
 #include "paged_device.h"
 #include "paged_plan.h"
 #include "sq_internal.h"
@@ -575,7 +577,8 @@ __device__ __forceinline__ bool prompt_tile(const uint16_t* q, const uint16_t* k
     up |= odds[rw * 128 + lane];
     down |= odds[rw * 128 + 64 + lane];
   }
-  if (row >= rows) return false;
+  constexpr bool kStage = !SPLIT && !CAREFUL;
+  if (!kStage && row >= rows) return false;
   bool sees = lim >= kt0 * kTile;  // a key of this part
   if constexpr (WIN) {
     const int p0 = (kt0 < head_tiles ? kt0 : kt0 + gap) * kTile;  // its first key; from the windows' first tile on, and its end
@@ -607,6 +610,27 @@ __device__ __forceinline__ bool prompt_tile(const uint16_t* q, const uint16_t* k
       for (int y = 0; y < 4; ++y)
         *reinterpret_cast<float4*>(pr + 4 + 32 * dt + 8 * y + 4 * h) =
             make_float4(acc[dt][4 * y], acc[dt][4 * y + 1], acc[dt][4 * y + 2], acc[dt][4 * y + 3]);
+  } else if constexpr (kStage) {
+    // Rows go out whole, 16 lanes each, by way of the wave's own part of LDS (all waves are done with the tiles): a store of
+    // a lane's own 8 bytes would be in 32 rows at once, and the next workgroup waits for it (8192 tokens of 32 heads on 8
+    // in windows of 1024: 170 -> 157 us, of 32: 54 -> 45 with 6 packed chunks).
+    uint8_t* const stage = lds + rw * (KG == 1 ? 8192 : 16384);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        *reinterpret_cast<v2u*>(stage + col * 256 + 16 * ((4 * dt + y) ^ swizzle(col)) + 8 * h) =
+            v2u{f2h2(acc[dt][4 * y], acc[dt][4 * y + 1]), f2h2(acc[dt][4 * y + 2], acc[dt][4 * y + 3])};
+    asm volatile("" ::: "memory");
+    const int64_t mine = qrow * a.ldo + head * 128;
+    const int left = rows - (tile * P::ROWS + 32 * rw);  // rows of the wave
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int r = 4 * x + (lane >> 4), c = lane & 15;
+      const v4u u = *reinterpret_cast<const v4u*>(stage + r * 256 + 16 * (c ^ swizzle(r)));
+      const int64_t at = __shfl(mine, r);
+      if (r < left) *reinterpret_cast<v4u*>(a.out + at + 8 * c) = u;
+    }
   } else {
     uint16_t* o = a.out + qrow * a.ldo + head * 128 + 4 * h;
 #pragma unroll
