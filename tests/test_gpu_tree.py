@@ -361,6 +361,24 @@ def test_prompt_keys_behind_the_window(Hq, nq, nk):
         assert not torch.isfinite(got[up(sees)]).any()
 
 
+@pytest.mark.parametrize("Hq,H,nq", [(2, 2, [300, 1, 37]), (130, 130, [300, 1, 37]), (24, 2, [25, 0, 3])], ids=["halves", "whole", "shared"])
+def test_prompt_window_into_a_wider_tensor(Hq, H, nq):
+    """Rows of a strided out, the last ones of a wave's 32 among them; what lies beside them and between the sequences stays."""
+    g = rng(Hq)
+    nk = [n + 40 for n in nq]
+    cu_q, cu_k = packed(nq, 2), packed(nk)
+    T = int(cu_q[-1]) + 3
+    q, k, v = up(heads_of(g, T, Hq)), up(heads_of(g, int(cu_k[-1]), H)), up(heads_of(g, int(cu_k[-1]), H))
+    wide = torch.full((T, Hq + 2, 128), 7.0, dtype=torch.float16, device=DEV)
+    want = torch.full((T, Hq, 128), 7.0, dtype=torch.float16, device=DEV)
+    for out in (wide[:, 1:-1], want):
+        sq.attn_prompt(q, k, v, ints(cu_q), ints(cu_k), window=33, sinks=2, out=out)
+    assert torch.equal(wide[:, 1:-1], want) and torch.all(wide[:, 0] == 7.0) and torch.all(wide[:, -1] == 7.0)
+    assert torch.all(want[:2] == 7.0) and torch.all(want[-3:] == 7.0)
+    ref, weight, rows = od.attn_prompt_window(*(x.cpu().numpy() for x in (q, k, v)), cu_q, cu_k, 33, 2)
+    attention_close(want[up(rows)], ref[rows], weight[rows], 2e-5)
+
+
 KEEP = [(4, np.float32, 16, 2), (8, np.float16, 32, 5), (4, np.float16, 64, 1), (8, np.float32, 16, 32)]
 
 
