@@ -11,8 +11,8 @@
 //
 // Many rows: vector instructions bound it.  64 drafts of 32 heads on 8 behind 131008 tokens of 4 bits take 200 us with
 // the join (137 GFLOP, 0.69 PFLOP/s of the 1.49 that a large library product reaches; the cache's 150 MB alone would
-// take 30): 594 vector operations for 64 tokens and two columns, a quarter of them the codes' expansion, half the
-// softmax, keep the vector units in use for 80 % of the kernel's cycles, the matrix cores for 29 %.  More rows on an
+// take 30): 564 vector operations for 64 tokens and two columns, a quarter of them the codes' expansion, half the
+// softmax, keep the vector units in use for 78 % of the kernel's cycles, the matrix cores for 30 %.  More rows on an
 // expansion: four columns a wave need 512 registers and spilled (413 us, two columns then 227); workgroups of 128 rows
 // that share the operands through LDS took 213 then, and 107 with 16 sequences of 524 .. 8224 tokens, 64 heads on 8,
 // where two columns a wave took 70 (62 now).
