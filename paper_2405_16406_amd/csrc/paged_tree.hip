@@ -140,24 +140,29 @@ __device__ __forceinline__ float4 token_params(const PagedCache& c, int64_t slot
   }
 }
 
-// Coefficients of a block's 64 tokens, one a lane, in seven rows of 64: a, b, lv, 1 / va and vb / va with the score
+// Coefficients of a block's 64 tokens, one a lane, in rows of 64: a, b, lv, 1 / va and vb / va with the score
 // s_t + log2 va_t = a_t (q . c_t) + b_t sum(q) + lv_t, as in paged_attn.hip.  A weight of 0 does not hide a
-// 1 / va or vb / va that is not finite: such tokens (the result) have zeros there, and what they are in the
-// last two rows.
-__device__ __forceinline__ uint64_t token_coefs(float4 par, bool there, float cs, float down, float* coef) {
+// 1 / va or vb / va that is not finite: such tokens (the result) have zeros there, and what they are in
+// rows 5 and 6.  With rows that are scaled apart lv is in row 7, and the third has 0 in its place.
+__device__ __forceinline__ uint64_t token_coefs(float4 par, bool there, float cs, float down, bool apart, float* coef) {
   const int lane = threadIdx.x & 63;
   par.z = par.z == 0.0f ? 1.0f : par.z;  // a slot of a zeroed cache that was never written
   float rva = there ? __fdiv_rn(1.0f, par.z) : 0.0f, rvb = there ? par.w * rva : 0.0f;
   const bool bad = !(fabsf(rva) < INFINITY) || !(fabsf(rvb) < INFINITY);
   const uint64_t odd = __ballot(bad);
-  if (__builtin_expect(odd != 0, 0)) {
+  float lv = there ? __builtin_amdgcn_logf(par.z) : -INFINITY;
+  if (__builtin_expect(odd != 0 || apart, 0)) {
     coef[5 * kBlock + lane] = rva;
     coef[6 * kBlock + lane] = rvb;
     if (bad) rva = rvb = 0.0f;
+    if (apart) {
+      coef[7 * kBlock + lane] = lv;
+      lv = there ? 0.0f : -INFINITY;
+    }
   }
   coef[0 * kBlock + lane] = there ? par.x * (cs * 16777216.0f * down) : 0.0f;  // 2^24 undoes the codes' subnormal scale
   coef[1 * kBlock + lane] = there ? par.y * cs : 0.0f;
-  coef[2 * kBlock + lane] = there ? __builtin_amdgcn_logf(par.z) : -INFINITY;
+  coef[2 * kBlock + lane] = lv;
   coef[3 * kBlock + lane] = rva;
   coef[4 * kBlock + lane] = rvb;
   return odd;
@@ -222,25 +227,32 @@ __device__ __forceinline__ void value_operands(const uint8_t* codes, int dt, v8h
 // 16 RB rows of a wave, one a lane and column: queries, what they see, and their softmax states.
 template <int BITS, int RB>
 struct TreeRows {
-  v8h qf[RB][4];    // dims 32 g .. 32 g + 31 in the codes' pair order, times 2^-down (4 bits: odd dims 1 / 16 of that)
+  v8h qf[RB][4];    // dims 32 g .. 32 g + 31 in the codes' pair order, divided by `down` (4 bits: odd dims 1 / 16 of that)
   float down;
-  float qsum[RB];   // sums over all dims
+  bool apart;       // each row is divided by its own number instead, and down is 1
+  float qsum[RB];   // sums over all dims, divided alike with `apart`
   int lo_most, hi_least;  // every row sees t where lo_most <= t < hi_least (or t < sinks)
-  int* sight;       // in LDS, out of the registers: [hi, lo, row][16] of each column
+  int* sight;       // in LDS, out of the registers: [hi, lo, row, and with `apart` its divisor][16] of each column
   float m[RB], l[RB], bsum[RB];
   uint32_t seen;    // bit rb: the row sees a token with a page
   v4f acc[RB][8];
 
-  static constexpr int SIGHT = 3 * 16 * RB;  // numbers in LDS
+  static constexpr int KIND = BITS == 4 ? 4 : 3, SIGHT = KIND * 16 * RB;  // numbers in LDS
 
-  // Rows p.r0 + first + 16 rb + i; past the last: that one again, not stored.
-  __device__ __forceinline__ void init(const uint16_t* q, int first, uint32_t magic_group, const TreeArgs& a, const TreePlace& p, int* in_lds) {
+  // The exponent of the power of two that brings a number of this size to 2^13 .. 2^14; 0 for 0 and what is not finite.
+  static __device__ __forceinline__ int lift(float size) {
+    return size > 0.0f && size < INFINITY ? 13 + 127 - static_cast<int>(__float_as_uint(size) >> 23) : 0;
+  }
+  static __device__ __forceinline__ float power(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }
+
+  // Rows p.r0 + 16 rb + i; past the last: that one again, not stored.
+  __device__ __forceinline__ void init(const uint16_t* q, uint32_t magic_group, const TreeArgs& a, const TreePlace& p, int* in_lds) {
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     sight = in_lds;
     seen = 0;
     lo_most = 0;
     hi_least = p.len;
-    float largest = 0.0f;
+    float size[RB];  // of the largest of the lane's 32 elements of the row (NaN left out)
     v4u all[RB][4];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -249,7 +261,7 @@ struct TreeRows {
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) acc[rb][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
       uint32_t tok, gh;
-      div_rem(static_cast<uint32_t>(min(p.r0 + first + 16 * rb + i, p.rows - 1)), a.group, magic_group, tok, gh);
+      div_rem(static_cast<uint32_t>(min(p.r0 + 16 * rb + i, p.rows - 1)), a.group, magic_group, tok, gh);
       const int64_t t = p.q0 + static_cast<int64_t>(tok);
       const v4u* qv = reinterpret_cast<const v4u*>(q + t * a.ldq + (static_cast<int64_t>(p.hk) * a.group + gh) * 128 + 32 * g);
       v4u raw[4];
@@ -262,33 +274,56 @@ struct TreeRows {
       hi_least = min(hi_least, hi);
       lo_most = max(lo_most, lo);
       if (g == 0) {
-        sight[(3 * rb + 0) * 16 + i] = hi;
-        sight[(3 * rb + 1) * 16 + i] = lo;
-        sight[(3 * rb + 2) * 16 + i] = static_cast<int>(t);  // (rows below 2^24)
+        sight[(KIND * rb + 0) * 16 + i] = hi;
+        sight[(KIND * rb + 1) * 16 + i] = lo;
+        sight[(KIND * rb + 2) * 16 + i] = static_cast<int>(t);  // (rows below 2^24)
       }
       float sum = 0.0f;
+      size[rb] = 0.0f;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const float u = h2f(static_cast<uint16_t>(raw[x][y])), v = h2f(static_cast<uint16_t>(raw[x][y] >> 16));
           sum += u + v;
-          largest = fmaxf(largest, fmaxf(fabsf(u), fabsf(v)));
+          size[rb] = fmaxf(size[rb], fmaxf(fabsf(u), fabsf(v)));
         }
       qsum[rb] = rows_all(sum, [](float u, float v) { return __fadd_rn(u, v); });
 #pragma unroll
       for (int x = 0; x < 4; ++x) all[rb][x] = raw[x];
     }
-    // 4 bits: the odd dims' sixteenth would lose bits of small numbers, so the wave's queries are first brought up to where
-    // the largest lies in 2^13 .. 2^14 (by a power of two, exact but for what is 2^-27 of the largest)
+    // 4 bits: the odd dims' sixteenth would lose bits of small numbers, so queries are first brought up to where the largest
+    // lies in 2^13 .. 2^14, by a power of two.  What is rounded then (fp16's steps of 2^-24 at the low end) is 2^-34 of
+    // the largest.  All rows of the wave share the power, which the coefficients undo, as long as that is 2^-24 or less
+    // of what is largest in any lane's part of a row, a 32-bit rounding; else each has its own, undone in own_scales.
+    // (Measured, us: 64 drafts of 32 heads behind 131008 tokens 192, with rows 2^-12 of the others among them 226; 16
+    // sequences of 32 drafts of 64 heads behind 4096, 113 and 130.)
     down = 1.0f;
-    float up = 1.0f;
+    apart = false;
+    float up[RB];
     if constexpr (BITS == 4) {
-      largest = wave_max(largest);
-      if (largest > 0.0f && largest < INFINITY) {
-        const int e = 13 - (static_cast<int>(__float_as_uint(largest) >> 23) - 127);
-        up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-        down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+      float most = 0.0f, least = INFINITY;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const bool counts = size[rb] > 0.0f && size[rb] < INFINITY;
+        most = counts ? fmaxf(most, size[rb]) : most;
+        least = counts ? fminf(least, size[rb]) : least;
+      }
+      most = wave_max(most);
+      apart = __ballot(least < most * 0x1p-10f) != 0;
+      if (__builtin_expect(apart, 0)) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const int e = lift(rows_all(size[rb], [](float u, float v) { return fmaxf(u, v); }));
+          up[rb] = power(e);
+          qsum[rb] *= up[rb];
+          if (g == 0) sight[(KIND * rb + 3) * 16 + i] = __float_as_int(power(-e));
+        }
+      } else {
+        const int e = lift(most);
+        down = power(-e);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) up[rb] = power(e);
       }
     }
 #pragma unroll
@@ -302,7 +337,7 @@ struct TreeRows {
         for (int x = 0; x < 4; ++x)
 #pragma unroll
           for (int y = 0; y < 4; ++y)
-            raw[x][y] = f2h2(h2f(static_cast<uint16_t>(raw[x][y])) * up, h2f(static_cast<uint16_t>(raw[x][y] >> 16)) * (0.0625f * up));
+            raw[x][y] = f2h2(h2f(static_cast<uint16_t>(raw[x][y])) * up[rb], h2f(static_cast<uint16_t>(raw[x][y] >> 16)) * (0.0625f * up[rb]));
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const v4u u = raw[2 * e], v = raw[2 * e + 1];
@@ -343,14 +378,30 @@ struct TreeRows {
       for (int r = 0; r < 4; ++r) s[rb][4 * j + r] = __fmaf_rn(fa[r], dot[rb][r], __fmaf_rn(fb[r], qsum[rb], fl[r]));
   }
 
+  // With `apart`: scores of queries that each row has divided by its own number, without lv, to those of the queries.
+  __device__ __forceinline__ void own_scales(const float* coef, float (&s)[RB][16]) const {
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 cl = *reinterpret_cast<const float4*>(coef + 7 * kBlock + 16 * j + 4 * g);
+      const float fl[4] = {cl.x, cl.y, cl.z, cl.w};
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float by = __int_as_float(sight[(KIND * rb + 3) * 16 + i]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[rb][4 * j + r] = __fmaf_rn(s[rb][4 * j + r], by, fl[r]);
+      }
+    }
+  }
+
   // Of the block's tokens t .. t + 63 those that the lane's row of column rb sees.
   __device__ __forceinline__ uint64_t visible(int rb, int t, const TreeArgs& a, const TreePlace& p) const {
     const int i = threadIdx.x & 15;
-    const int hi = sight[(3 * rb + 0) * 16 + i], lo = sight[(3 * rb + 1) * 16 + i];
+    const int hi = sight[(KIND * rb + 0) * 16 + i], lo = sight[(KIND * rb + 1) * 16 + i];
     uint64_t vis = below(hi, t) & (~below(lo, t) | below(a.sinks, t));
     if (a.mask && t + kBlock > p.base) {
       const int j = t - p.base, word = j >> 5, shift = j & 31;  // (rounded down: negative for the words before the first)
-      const int32_t* const bits = a.mask + sight[(3 * rb + 2) * 16 + i] * a.ldm;
+      const int32_t* const bits = a.mask + sight[(KIND * rb + 2) * 16 + i] * a.ldm;
       const auto at = [&](int x) { return x >= 0 && x < a.words ? static_cast<uint64_t>(static_cast<uint32_t>(bits[x])) : uint64_t{0}; };
       uint64_t sees = (at(word) | at(word + 1) << 32) >> shift;
       if (shift) sees |= at(word + 2) << (64 - shift);
@@ -365,7 +416,9 @@ struct TreeRows {
                                        float (&s)[RB][16]) {
     const uint32_t here = lane_bits(there);  // of the lane's tokens
     const bool masked = t0 + kBlock > hi_least || (t0 < lo_most && t0 + kBlock > a.sinks);
-    if (__builtin_expect(masked || odd != 0, 0)) {
+    if (__builtin_expect(masked || odd != 0 || (BITS == 4 && apart), 0)) {
+      if constexpr (BITS == 4)
+        if (apart) own_scales(coef, s);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const uint32_t vis = masked ? lane_bits(visible(rb, t0, a, p)) : 0xFFFFu;
@@ -498,7 +551,7 @@ __device__ __forceinline__ void store_row(const TreeArgs& a, const TreePlace& p,
 template <int BITS, int RB>
 struct TreeLds {
   static constexpr int CODES = kBlock * kPitch<BITS>;
-  static constexpr int SIGHT = CODES + 7 * kBlock * 4, QUERIES = SIGHT + TreeRows<BITS, RB>::SIGHT * 4;
+  static constexpr int SIGHT = CODES + (BITS == 4 ? 8 : 7) * kBlock * 4, QUERIES = SIGHT + TreeRows<BITS, RB>::SIGHT * 4;
   static constexpr int BYTES = QUERIES + (RB > 1 ? RB * 4096 : 0);
 };
 template <int BITS, int RB, int WAVES>
@@ -524,7 +577,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
   float* const coef = reinterpret_cast<float*>(vlds + W::CODES);
   v8h* const qlds = reinterpret_cast<v8h*>(vlds + W::QUERIES);
   TreeRows<BITS, RB> r;
-  r.init(q, 0, magic_group, a, p, reinterpret_cast<int*>(vlds + W::SIGHT));
+  r.init(q, magic_group, a, p, reinterpret_cast<int*>(vlds + W::SIGHT));
   if constexpr (RB > 1) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
@@ -589,7 +642,7 @@ attn_tree_part(const uint16_t* q, const int32_t* cu, const int32_t* lens, uint32
         *reinterpret_cast<v4u*>(vlds + row * kPitch<BITS> + 16 * (lane & (BITS == 4 ? 3 : 7))) = vc[mm][x];
       }
     const uint64_t there = __ballot(par_ok);
-    const uint64_t odd = token_coefs(par, par_ok, a.scale_log2e, r.down, coef);
+    const uint64_t odd = token_coefs(par, par_ok, a.scale_log2e, r.down, BITS == 4 && r.apart, coef);
     asm volatile("" ::: "memory");
     const bool more = v0 + step < p.last;
     if constexpr (EARLY) {
