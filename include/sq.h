@@ -588,7 +588,8 @@ sq_status sq_rope_kv_write_ex(const void* q, int64_t ldq, const void* k, int64_t
  *   without       the tokens j <= base + i, as far as the window at base + i lets it
  * A row that sees no token with a page gets zeros; one with a token that it sees and a query that is
  * not finite gives NaN.  What a row does not see has no part in its result, NaN and infinities among
- * the parameters included.  Precision and the range of v_alpha as in sq_attn_paged, row by row.
+ * the parameters included; of what it sees, a v_beta that is not finite makes it infinite or NaN.
+ * Precision and the range of v_alpha as in sq_attn_paged, row by row: whatever the other rows' queries.
  *   q          device fp16 [T, ldq]: Hq rotated heads of D, 16-byte aligned
  *   cu         device int32 [B + 1], ascending, within [0, T] (values beyond are taken as the end).  Rows
  *              of no sequence, and rows with base + i < 0, are left as they were in out.

@@ -459,8 +459,9 @@ struct TreeRows {
         const bool mine = top[rb] - m[rb] > kWeightBits + kSlack;
         const float mn = mine ? fmaxf(m[rb], fabsf(top[rb]) < kLargeScore ? top[rb] - kWeightBits : top[rb]) : m[rb];
         const float f = mine ? rescale(m[rb], mn) : 1.0f;
-        l[rb] *= f;
-        bsum[rb] *= f;
+        // (what hide put there stays: f is 0 before the first token's weight)
+        l[rb] = fabsf(l[rb]) < INFINITY ? l[rb] * f : l[rb];
+        bsum[rb] = fabsf(bsum[rb]) < INFINITY ? bsum[rb] * f : bsum[rb];
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) acc[rb][dt] *= f;
         m[rb] = mn;
@@ -754,7 +755,7 @@ attn_tree_combine(const float* part, const int32_t* cu, const int32_t* lens, int
   for (int c0 = w; c0 < n; c0 += J * kAhead) {
     float2 ml[kAhead], d[kAhead];
 #pragma unroll
-    for (int x = 0; x < kAhead; ++x) {  // a chunk past the last is the last again, with weight 0
+    for (int x = 0; x < kAhead; ++x) {  // (past the last chunk the last again, which is dropped)
       const float* p = pr + static_cast<int64_t>(min(c0 + J * x, n - 1)) * kAttnPart;
       ml[x] = *reinterpret_cast<const float2*>(p);
       d[x] = reinterpret_cast<const float2*>(p + 4)[lane];
@@ -762,7 +763,10 @@ attn_tree_combine(const float* part, const int32_t* cu, const int32_t* lens, int
     float top = M;
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) {
-      if (c0 + J * x >= n) ml[x].x = -INFINITY;
+      if (c0 + J * x >= n) {  // not by a weight of 0: its sums may be infinite
+        ml[x] = make_float2(-INFINITY, 0.0f);
+        d[x] = make_float2(0.0f, 0.0f);
+      }
       top = fmaxf(top, ml[x].x);
     }
     const float f0 = rescale(M, top);

@@ -17,6 +17,12 @@ def forms(host, cases, window=None):  # noqa: F811
     return out
 
 
+def test_hidden_parameters_reach_every_form(host):  # noqa: F811
+    t = pytest.importorskip("test_gpu_tree_hidden")
+    assert forms(host, t.FORMS) == {"one column": (1, 4, False), "eight waves": (1, 8, False), "two columns": (2, 4, True),
+                                    "two columns, joined": (2, 4, True), "one column, joined": (1, 4, True)}
+
+
 def test_queries_of_different_sizes_reach_every_form(host):  # noqa: F811
     t = pytest.importorskip("test_gpu_tree_queries")
     got = forms(host, t.FORMS)
