@@ -37,13 +37,6 @@ sq_status prompt_plan_here(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_
   return SQ_OK;
 }
 
-// What a window leaves of Tk keys: the run of a tile of rows holds at most its sinks and window, its rows and what
-// whole blocks of 64 add.
-int64_t window_keys(int64_t B, int64_t Tk, int32_t window, int32_t sinks) {
-  if (window <= 0) return Tk;
-  return std::min(Tk, std::max<int64_t>(B, 1) * (static_cast<int64_t>(sinks) + window + sq::kPromptRows + 2 * sq::kPromptTile));
-}
-
 sq_status check_prompt_sizes(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D) {
   const sq_status s = check_heads(Hq, Hkv, D);
   if (s != SQ_OK) return s;
@@ -61,7 +54,7 @@ sq_status prompt_workspace(int64_t B, int64_t Tq, int64_t Tk, int32_t window, in
   if (s != SQ_OK || (s = check_window(window, sinks)) != SQ_OK) return s;
   sq::PromptPlan plan{};
   uint64_t need = 0;
-  if ((s = prompt_plan_here(B, Tq, window_keys(B, Tk, window, sinks), Hq, Hkv, plan, need)) != SQ_OK) return s;
+  if ((s = prompt_plan_here(B, Tq, sq::window_keys(B, Tk, window, sinks), Hq, Hkv, plan, need)) != SQ_OK) return s;
   *bytes = need;
   return ok();
 }
@@ -88,7 +81,7 @@ sq_status attn_prompt(const void* q, int64_t ldq, const void* k, int64_t ldk, co
   sq::PromptArgs a{};
   sq::PromptPlan plan{};
   uint64_t need = 0;
-  if ((s = prompt_plan_here(B, Tq, window_keys(B, Tk, window, sinks), Hq, Hkv, plan, need)) != SQ_OK) return s;
+  if ((s = prompt_plan_here(B, Tq, sq::window_keys(B, Tk, window, sinks), Hq, Hkv, plan, need)) != SQ_OK) return s;
   a.half = plan.half;
   a.splits = plan.splits;
   a.per = plan.per;

@@ -151,6 +151,14 @@ inline PromptPlan prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int32_t hq, int
   return {0, static_cast<int32_t>(splits), static_cast<int32_t>(per)};
 }
 
+// What a window leaves of Tk keys: the run of a tile of rows holds at most its sinks and window, its rows and what
+// whole blocks of 64 add.
+inline int64_t window_keys(int64_t B, int64_t Tk, int32_t window, int32_t sinks) {
+  if (window <= 0) return Tk;
+  const int64_t most = (B > 1 ? B : 1) * (static_cast<int64_t>(sinks) + window + kPromptRows + 2 * kPromptTile);
+  return most < Tk ? most : Tk;
+}
+
 // Tiles of a part of a sequence (or of a tile of its rows) with `tiles` of them.
 SQ_HOST_DEVICE int32_t prompt_part(int32_t tiles, int32_t splits, int32_t per) {
   const int32_t least = (tiles + splits - 1) / splits;
