@@ -543,6 +543,12 @@ def _cache_args(cache, table, B):
              pages, page, heads), (row // 16, param_bits))
 
 
+def _check_window(window, sinks, where):
+    """The library gets the low 32 bits of these: more must not be cut down to a number that it takes."""
+    if (window | sinks) >> 30:
+        raise SqError(SQ_ERR_SHAPE, where, f"window={window} and sinks={sinks} must lie in [0, 2^30)")
+
+
 def _same_device(t, *others):
     """The device of t, which all other tensors must be on."""
     d = t.get_device()
@@ -642,6 +648,7 @@ def attn_paged_workspace_bytes(B, max_len, Hq, Hkv, window: int = 0, sinks: int 
     """Device bytes of attn_paged's workspace on the current device."""
     n = _U64(0)
     if window:
+        _check_window(window, sinks, "sq_attn_paged_window_workspace")
         _check(lib().sq_attn_paged_window_workspace(B, max_len, window, sinks, Hq, Hkv, 128, ctypes.byref(n)),
                "sq_attn_paged_window_workspace")
         return n.value
@@ -677,6 +684,7 @@ def attn_paged(q, cache, block_table, lens, max_len: int, scale=None, out=None, 
         size = _workspace_bytes(workspace)
     scale = 0.08838834764831845 if scale is None else scale
     if window:
+        _check_window(window, sinks, "sq_attn_paged_window")
         status = lib().sq_attn_paged_window(q.data_ptr(), ldq, lens.data_ptr(), B, window, sinks, *args, Hq, 128, *bits, max_len,
                                             scale, out.data_ptr(), ldo, _ptr(workspace), size, _stream(q))
     else:
@@ -691,6 +699,7 @@ def attn_prompt_workspace_bytes(B, Tq, Tk, Hq, Hkv, window: int = 0, sinks: int 
     """Device bytes of attn_prompt's workspace on the current device."""
     n = _U64(0)
     if window:
+        _check_window(window, sinks, "sq_attn_prompt_window_workspace")
         _check(lib().sq_attn_prompt_window_workspace(B, Tq, Tk, window, sinks, Hq, Hkv, 128, ctypes.byref(n)),
                "sq_attn_prompt_window_workspace")
         return n.value
@@ -734,6 +743,7 @@ def attn_prompt(q, k, v, cu_q, cu_k, scale=None, causal: bool = True, out=None, 
         size = _workspace_bytes(workspace)
     scale = 0.08838834764831845 if scale is None else scale
     if window:
+        _check_window(window, sinks, "sq_attn_prompt_window")
         status = lib().sq_attn_prompt_window(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, cu_q.data_ptr(),
                                              cu_k.data_ptr(), B, Tq, Tk, Hq, Hkv, 128, scale, window, sinks, out.data_ptr(), ldo,
                                              _ptr(workspace), size, _stream(q))
@@ -780,6 +790,7 @@ def tree_mask(parents, cu, most: int, lens=None, window: int = 0, sinks: int = 0
     if d != _current_device():
         with torch.cuda.device(d):
             return tree_mask(parents, cu, most, lens, window, sinks, (mask, depth))
+    _check_window(window, sinks, "sq_tree_mask")
     status = lib().sq_tree_mask(parents.data_ptr(), cu.data_ptr(), _ptr(lens), B, T, window, sinks, mask.data_ptr(), ld, words,
                                 depth.data_ptr(), _stream(parents))
     if status:
@@ -790,6 +801,7 @@ def tree_mask(parents, cu, most: int, lens=None, window: int = 0, sinks: int = 0
 def attn_tree_workspace_bytes(B, T, max_len, Hq, Hkv, window: int = 0, sinks: int = 0):
     """Device bytes of attn_tree's workspace on the current device."""
     n = _U64(0)
+    _check_window(window, sinks, "sq_attn_tree_workspace")
     _check(lib().sq_attn_tree_workspace(B, T, max_len, window, sinks, Hq, Hkv, 128, ctypes.byref(n)), "sq_attn_tree_workspace")
     return n.value
 
@@ -829,6 +841,7 @@ def attn_tree(q, cache, block_table, lens, cu, max_len: int, mask=None, depth=No
         workspace = q.new_empty(size, dtype=_U8) if size else None
     else:
         size = _workspace_bytes(workspace)
+    _check_window(window, sinks, "sq_attn_tree")
     status = lib().sq_attn_tree(q.data_ptr(), ldq, cu.data_ptr(), lens.data_ptr(), B, T, _ptr(mask), ldm, words, _ptr(depth), window,
                                 sinks, *args, Hq, 128, *bits, max_len, 0.08838834764831845 if scale is None else scale,
                                 out.data_ptr(), ldo, _ptr(workspace), size, _stream(q))
