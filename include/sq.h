@@ -673,10 +673,13 @@ sq_status sq_attn_prompt_window_workspace(int64_t B, int64_t Tq, int64_t Tk, int
  * sq_paged_release -- pages go back to the pool: of sequence b the held blocks whose positions all lie in
  * first[b] .. end[b] - 1.  end may lie past the last token: at or past the end of the last held block,
  * held[b] becomes the first block that went (what ended a sequence, first = 0, or took back its drafts,
- * first = tokens kept); below it held[b] stays (what a window has left behind: first = sinks,
- * end = position - window + 1).  Their entries become -1; one that is not a page of the pool goes
- * nowhere.  The pages join the pool by sequence, then block.  A page that two sequences share must be
- * released by one of them alone.
+ * first = tokens kept); below it held[b] stays (what a window has left behind of the tokens so far: end =
+ * tokens - window, which is below it; first = sinks in a sequence's first call, then the largest `end` so far
+ * rounded down to a whole block, but sinks at least).  Their entries become -1; one that is not a page of the
+ * pool goes nowhere.  The pages join the pool by sequence, then block.  A page that two sequences share must
+ * be released by one of them alone.  Every block of the range is looked at, those that have gone before too:
+ * with first = sinks in every call a window would look at the whole text behind it each time, for the same
+ * result.
  *   first, end device int32 [B]; first below 0 counts as 0
  * Errors: SQ_ERR_NULL, SQ_ERR_SHAPE, SQ_ERR_ALIGN, SQ_ERR_ALIAS, SQ_ERR_HIP.
  */

@@ -9,7 +9,9 @@
 // Measured on the device, us (an empty kernel takes 2): release 3.8 for 8 sequences, 7.7 for 256 of which 64 end;
 // grow 4.8 and 6.2; the 36 000 rows of the latter step 4.4; masks of 8 and 16 trees 2.5 and 5.1;
 // the accepted drafts of one sequence 3.2, of 64 sequences of 8 heads 3.3.  Eager calls wait for the host: 8 us for
-// one, 17 for the three of a step's tables.
+// one, 17 for the two of a step's tables.
+// A release looks at every block of its ranges, 1024 in 1.6 us.  64 sequences behind windows of 4096 tokens, pages of 16:
+// 3.9 us with `first` from the last end, whatever the length; from the first tokens 28 at 8192 tokens and 800 at 131072.
 #include "paged_device.h"
 #include "sq_internal.h"
 

@@ -862,7 +862,9 @@ def _pool_args(block_table, held, pool, count):
 def paged_release(block_table, page: int, first, end, held, pool, count) -> None:
     """Pages whose positions all lie in first .. end - 1 (int32 [B] each) go back to the pool
     (sq_paged_release).  In place: block_table int32 [B, blocks], held int32 [B] (blocks of each sequence
-    that have a page), pool int32 [pages] with its first count[0] entries free, count int32 [1]."""
+    that have a page), pool int32 [pages] with its first count[0] entries free, count int32 [1].  Behind a
+    window: end = tokens - window, first = (the largest end so far // page * page).clamp(min=sinks), since every
+    block of the range is looked at."""
     B, table, store = _pool_args(block_table, held, pool, count)
     _index(first, "first", B)
     _index(end, "end", B)
