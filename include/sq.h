@@ -548,7 +548,7 @@ sq_status sq_attn_prompt_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq
  *              window > 0 and sinks > 0
  *   T, B       >= 0 (0 is a no-op), < 2^31
  *   window, sinks  as above: an ancestor `window` or more steps up is left out, unless its position is
- *              below sinks
+ *              below sinks (none is with sinks 0)
  *   mask       device int32 [T, ld_mask], the first `words` words of a row written: bit j % 32 of word
  *              j / 32 of draft i is 1 where j is i or an ancestor that i sees.  Drafts from 32 * words on
  *              have no bits.

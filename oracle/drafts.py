@@ -17,7 +17,7 @@ MOST = 2 ** 31 - 1
 
 def in_window(t, p, window, sinks):
     """Whether a token at position p may see the key at position t <= p."""
-    return window == 0 or t > p - window or t < sinks
+    return window == 0 or t > p - window or (sinks > 0 and t < sinks)  # (drafts without a place have t < 0)
 
 
 def tree_mask(parents, cu, lens=None, window=0, sinks=0, words=1):
