@@ -11,8 +11,8 @@
 //
 // Many rows: vector instructions bound it.  64 drafts of 32 heads on 8 behind 131008 tokens of 4 bits take 200 us with
 // the join (137 GFLOP, 0.69 PFLOP/s of the 1.49 that a large library product reaches; the cache's 150 MB alone would
-// take 30): 564 vector operations for 64 tokens and two columns, a quarter of them the codes' expansion, half the
-// softmax, keep the vector units in use for 78 % of the kernel's cycles, the matrix cores for 30 %.  More rows on an
+// take 30): 566 vector operations for 64 tokens and two columns, a third of them the codes' expansion (80 of the keys, 112
+// of the values), half the softmax, keep the vector units in use for 78 % of the kernel's cycles, the matrix cores for 30 %.  More rows on an
 // expansion: four columns a wave need 512 registers and spilled (413 us, two columns then 227); workgroups of 128 rows
 // that share the operands through LDS took 213 then, and 107 with 16 sequences of 524 .. 8224 tokens, 64 heads on 8,
 // where two columns a wave took 70 (62 now).
@@ -469,7 +469,9 @@ struct TreeRows {
     }
   }
 
-  // Weights of column rb rounded to fp16 in the value codes' pair order; l and b sum the rounded ones.
+  // Weights of column rb in the value codes' pair order, rounded to fp16 as the second product takes them; l and b sum the
+  // rounded ones, so that what a weight is off by moves the mean, not its size.  Outputs are then off by 2.3e-4 to
+  // 2.8e-4 of their size, of which their own rounding is 2.1e-4.
   __device__ __forceinline__ void weights(int rb, const float (&s)[16], const float* coef, v8h (&pf)[2]) {
     const int g = (threadIdx.x & 63) >> 4;
     const float from = m[rb] == -INFINITY ? 0.0f : m[rb];

@@ -39,7 +39,7 @@
 //
 // With a window a workgroup walks the tiles of its rows' run alone.  8192 tokens of 32 heads on 8 with windows of 1024
 // take 157 .. 164 us (129 GFLOP, 0.8 PFLOP/s; matrix cores busy for 45 % of the cycles), six chunks of 500 .. 1500 tokens
-// of 32 heads behind up to 2500 with windows of 777 115 .. 125 us (0.6).  A run is some 18 tiles, and what a workgroup
+// of 32 heads behind up to 2500 with windows of 777 115 .. 126 us (0.6).  A run is some 18 tiles, and what a workgroup
 // does once weighs as in a short prompt: of 43 us 0.6 go to find its place, 1.4 to the queries' addresses, 1.9 to the
 // first tile, 2.7 to the end (before rows went out whole), and 4 .. 6 pass until the next one starts.  One workgroup a
 // compute unit that takes tiles in turn was 1 % quicker for one prompt and up to 14 % slower for several.  Masks do not
@@ -613,7 +613,8 @@ __device__ __forceinline__ bool prompt_tile(const uint16_t* q, const uint16_t* k
   } else if constexpr (kStage) {
     // Rows go out whole, 16 lanes each, by way of the wave's own part of LDS (all waves are done with the tiles): a store of
     // a lane's own 8 bytes would be in 32 rows at once, and the next workgroup waits for it (8192 tokens of 32 heads on 8
-    // in windows of 1024: 170 -> 157 us, of 32: 54 -> 45 with 6 packed chunks).
+    // in windows of 1024: 173 -> 160 us, 170 -> 157 at another time; 6 packed chunks in windows of 777 126 -> 122, of 32
+    // 54 -> 45).
     uint8_t* const stage = lds + rw * (KG == 1 ? 8192 : 16384);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
