@@ -57,8 +57,7 @@ def test_small_rows_beside_a_large_one(form, size, other, bits):
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("form", FORMS)
 def test_rows_of_every_size(form, bits):
-    """Rows from 2^-20 to 2^0 of the largest, each with keys that make its own scores ordinary: what one row gets beside
-    the others is what it gets where all rows are itself."""
+    """Rows from 2^-20 to 2^0 of the largest, with a scale that makes the scores of one size ordinary: these are compared."""
     g = rng(82)
     Hq, cache, lens, cu, table, T = case_of(g, form, bits)
     q = heads_of(g, T, Hq)
